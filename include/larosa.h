@@ -256,6 +256,90 @@ int larosa_sparse_gemv_w4(const void* Wq, const void* scales, const void* h, con
 int larosa_threshold_select(const void* h, int B, int d, float eps, larosa_dtype t, int32_t* idx, int32_t* count,
                             void* stream);
 
+/* ---- Key/value cache in 4 bits and the attention over it: the core that larosa_layer_qkv and
+ * larosa_layer_after_attention leave to the caller.  The method does not touch the attention core (Sec. 3.1), so the format is
+ * this library's own: pages of page_tokens tokens, shared between sequences and handed out through a page table.
+ *
+ *   data    n_layers pools one after the other, each n_pages pages of larosa_kv4_page_bytes() bytes.  A page holds, for
+ *           each key/value head, page_tokens / 32 blocks of 34 head_dim bytes (32 tokens each):
+ *           codes of K (16 head_dim bytes), codes of V (16 head_dim), scales of K (head_dim), scales of V (head_dim).
+ *   value   = code * 2^(scale - 127): code = sign (bit 3) and magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6 (bits 0..2); one scale byte for
+ *           32 neighbouring values of a head (value i belongs to group i / 32); a group with scale 255 is NaN.
+ *   layout  with D = head_dim, token t of the block, u = t / 16, W = min(16, D / 8), byte b of a lane's D / 8:
+ *           at(lane, b) = u 8 D + (b / W) 64 W + lane W + b mod W, even values in the low nibble;
+ *           K value i: lane = (i / (D/4)) 16 + t mod 16, b = (i mod D/4) / 2, at at(lane, b);
+ *           V value i: lane = (t mod 16 / 4) 16 + i / (D/16), b = (t mod 4) D/32 + (i mod D/16) / 2, at 16 D + at(lane, b);
+ *           scale of K, group g: 32 D + u D/2 + 16 g + t mod 16;
+ *           scale of V, group g: 33 D + u D/2 + ((t mod 16 / 4) D/32 + g) 4 + t mod 4.
+ *   table   [n_slots, max_pages]: page of tokens [p page_tokens, (p + 1) page_tokens) of the sequence in a slot, -1 = none
+ *   length  [n_slots]: tokens of the sequence in a slot (0: the slot is free)
+ *   refs    [n_pages]: table entries that name the page (0: the page is free)
+ * head_dim is 64, 128 or 256; page_tokens 32, 64, 128 or 256; data 16-byte aligned.  A page id outside [0, n_pages) is
+ * never followed: tokens on it are not stored and not seen.  Two calls that use one cache are ordered on one stream. */
+typedef struct {
+  int n_layers, n_pages, page_tokens, n_slots, max_pages;
+  int n_kv_heads, head_dim;
+  larosa_dtype dtype;         /* of the keys and values that go in and of the queries */
+  void* data;
+  int32_t *refs, *table, *length;
+} larosa_kv4_cache;
+
+/* Which rows of a batch are the newest tokens of which sequence.  Rows starts[s] .. starts[s+1] - 1 (starts NULL: row s alone)
+ * are the last tokens of the sequence in slots[s], whose length counts them already (larosa_kv4_grow).  A slot
+ * outside [0, n_slots) marks a sequence as padding.  Rows outside [0, n_rows), rows of no sequence and rows past the first
+ * max_new of a sequence are neither read nor written. */
+typedef struct {
+  const int32_t* slots;       /* [n_seq], device; a slot at most once */
+  const int32_t* starts;      /* [n_seq + 1], device, or NULL */
+  int n_seq, n_rows;
+  int max_new;                /* most new tokens of one sequence; 1 with starts NULL */
+} larosa_kv4_batch;
+
+/* Rotary positions.  Frequency j < rot_dim / 2 turns the pair of values (j, j + rot_dim / 2) of a head, or (2 j, 2 j + 1) if
+ * interleaved; values from rot_dim on stay.  The angle of frequency j at position p is given by its cosine table[p, j] and its sine
+ * table[p, rot_dim / 2 + j] (fp32).  Several axes (time, height, width of a picture's tokens): the first axis_pairs[0] frequencies
+ * take their position from positions[0, row], the next axis_pairs[1] from positions[1, row], and so on.  positions NULL (one axis
+ * only): a token's place in its sequence.  A position outside [0, n_positions) makes the values it turns NaN. */
+typedef struct {
+  const float* table;         /* [n_positions, rot_dim], device */
+  int n_positions, rot_dim;   /* rot_dim: multiple of 16, at most head_dim */
+  int interleaved;
+  const int32_t* positions;   /* [n_axes, n_rows], device, or NULL */
+  int n_axes;                 /* 1 to 4 */
+  int axis_pairs[4];          /* n_axes > 1: frequencies of each axis, together rot_dim / 2 */
+} larosa_rotary;
+
+/* Bytes of one page of one layer, and of a whole cache's data (0 for sizes that are not supported). */
+size_t larosa_kv4_page_bytes(int page_tokens, int n_kv_heads, int head_dim);
+size_t larosa_kv4_data_bytes(const larosa_kv4_cache* C);
+
+/* Make the cache empty: refs and length 0, table -1 (data stays as it is). */
+int larosa_kv4_clear(const larosa_kv4_cache* C, void* stream);
+
+/* New tokens of one layer into the cache.  qkv [n_rows, ld_qkv]: q | k | v of each row, n_heads, n_kv_heads and n_kv_heads heads of
+ * head_dim values (what larosa_layer_qkv writes).  q and k are turned by `rotary` (NULL: not), in fp32 with every product and sum
+ * rounded; k and v are stored in 4 bits: with m the largest magnitude of a group, e = floor(log2 m) - 2, one more if
+ * m > 7 2^e, held to [-23, 13] (F16) or [-100, 125] (BF16), the nearest code of value / 2^e, ties to the even code, 6 for more;
+ * a group that holds a NaN or infinity becomes NaN.  Tokens without a page, or whose place would be negative, are not stored.
+ * out [n_rows, ld_out] (nullable without rotary): q as turned, k and v as the cache now holds them, rounded once to the type; it
+ * may be qkv itself (with ld_out == ld_qkv).  ld_qkv, ld_out: multiples of 8.  The pages that are written must belong to one
+ * sequence (larosa_kv4_grow sees to it). */
+int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* batch, const void* qkv, int ld_qkv,
+                      int n_heads, const larosa_rotary* rotary, void* out, int ld_out, void* stream);
+
+/* Attention of the batch's rows over the cache of one layer (n_heads a multiple of n_kv_heads, query head h reads
+ * key/value head h / (n_heads / n_kv_heads)):
+ *   out[row, h, :] = sum_t w_t v_t / sum_t w_t,   w_t = exp(scale (q[row, h, :] . k_t) - max)
+ * over the tokens t <= place of the row in its sequence and, with window > 0, t > place - window.  A row that sees no token (an
+ * empty sequence, padding of a batch with starts, pages missing) gets zeros.  The 16-bit weights w_t and exact values multiply on the
+ * matrix cores, sums and the maximum are fp32.  q [n_rows, ld_q], out [n_rows, ld_out]: multiples of 8 apart, out rounded once.
+ * max_len: about the longest sequence, by which the work is divided over the chip (0: max_pages * page_tokens); longer ones are
+ * right too.  Workspace: larosa_kv4_attention_workspace_bytes of the same arguments, initialised by larosa_workspace_init. */
+size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* batch, int n_heads, int max_len);
+int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* batch, const void* q, int ld_q,
+                         int n_heads, float scale, int window, int max_len, void* out, int ld_out, void* ws, size_t ws_bytes,
+                         void* stream);
+
 /* ---- NOT part of the stable interface: launch tuning for tests and experiments.
  * Process-wide host state read by every call (launch shapes AND workspace sizes depend on it): not
  * thread-safe; change it only while no call of this library is in flight, and before sizing a workspace.

@@ -48,6 +48,23 @@ class _Trace(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in TRACE_FIELDS] + [("stage_events", ctypes.c_void_p * 8)]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_layers", "n_pages", "page_tokens", "n_slots", "max_pages", "n_kv_heads", "head_dim",
+                                            "dtype")]
+    _fields_ += [(n, ctypes.c_void_p) for n in ("data", "refs", "table", "length")]
+
+
+class _KvBatch(ctypes.Structure):
+    _fields_ = [("slots", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("n_seq", ctypes.c_int), ("n_rows", ctypes.c_int),
+                ("max_new", ctypes.c_int)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_positions", ctypes.c_int), ("rot_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("positions", ctypes.c_void_p), ("n_axes", ctypes.c_int),
+                ("axis_pairs", ctypes.c_int * 4)]
+
+
 def lib() -> ctypes.CDLL:
     """Load liblarosa.so (built in-tree by paper_2507_01299_amd.build); raise if it is missing."""
     global _lib
@@ -84,6 +101,15 @@ def lib() -> ctypes.CDLL:
         L.larosa_fold_input.argtypes = [vp, vp, i, i, i, vp, vp, sz, vp]
         L.larosa_fold_output.argtypes = [vp, vp, i, i, i, vp, vp, sz, vp]
         L.larosa_residual_adapter.argtypes = [vp, vp, i, i, vp, vp, sz, vp]
+        cache, batch, rotary = ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch), ctypes.POINTER(_Rotary)
+        L.larosa_kv4_page_bytes.restype = L.larosa_kv4_data_bytes.restype = sz
+        L.larosa_kv4_page_bytes.argtypes = [i, i, i]
+        L.larosa_kv4_data_bytes.argtypes = [cache]
+        L.larosa_kv4_clear.argtypes = [cache, vp]
+        L.larosa_kv4_append.argtypes = [cache, i, batch, vp, i, i, rotary, vp, i, vp]
+        L.larosa_kv4_attention_workspace_bytes.restype = sz
+        L.larosa_kv4_attention_workspace_bytes.argtypes = [cache, batch, i, i]
+        L.larosa_kv4_attention.argtypes = [cache, i, batch, vp, i, i, ctypes.c_float, i, i, vp, i, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -341,3 +367,89 @@ def layer_after_attention(layer: Layer, residual, attn, x_out, ws: Workspace, tr
                                               ws.ptr, ws.nbytes, _stream()),
            "larosa_layer_after_attention")
     return x_out
+
+
+class KvCache:
+    """Device tensors of a 4-bit key/value cache and the matching C struct.  Tensors that are not given are allocated, and the
+    cache is then made empty; given ones are taken as they are (all of refs, table and length, or none)."""
+
+    def __init__(self, n_layers, n_pages, page_tokens, n_slots, max_pages, n_kv_heads, head_dim, dtype, data=None, refs=None,
+                 table=None, length=None, device="cuda:0"):
+        self.dtype = dtype_code(dtype)
+        self.c = _KvCache(n_layers, n_pages, page_tokens, n_slots, max_pages, n_kv_heads, head_dim, self.dtype)
+        nbytes = lib().larosa_kv4_data_bytes(ctypes.byref(self.c))
+        if nbytes == 0:
+            raise LarosaError(EINVAL, "larosa_kv4_data_bytes")
+        state = (refs, table, length)
+        if any(t is None for t in state) and any(t is not None for t in state):
+            raise ValueError("refs, table and length are given together")
+        fresh = refs is None
+        if fresh:
+            refs = torch.empty(n_pages, dtype=torch.int32, device=device)
+            table = torch.empty(n_slots, max_pages, dtype=torch.int32, device=device)
+            length = torch.empty(n_slots, dtype=torch.int32, device=device)
+        if data is None:
+            data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        sizes = (refs.numel(), table.numel(), length.numel())
+        if sizes != (n_pages, n_slots * max_pages, n_slots) or data.numel() * data.element_size() < nbytes:
+            raise ValueError("refs [n_pages], table [n_slots, max_pages], length [n_slots], data of larosa_kv4_data_bytes")
+        if any(t.dtype != torch.int32 for t in (refs, table, length)) or not all(t.is_contiguous() for t in (data, refs, table, length)):
+            raise ValueError("refs, table and length are contiguous int32 tensors, data is contiguous")
+        self.data, self.refs, self.table, self.length = data, refs, table, length
+        self.c.data, self.c.refs, self.c.table, self.c.length = (t.data_ptr() for t in (data, refs, table, length))
+        if fresh:
+            kv4_clear(self)
+
+
+class KvBatch:
+    """Which of n_rows rows are the newest tokens of which sequence: slots [n_seq] int32, starts [n_seq + 1] int32 or None (one
+    row for each sequence), max_new the most of one sequence."""
+
+    def __init__(self, slots, n_rows: int, starts=None, max_new: int = 1):
+        self.tensors = (slots, starts)       # keep alive
+        self.c = _KvBatch(_ptr(slots), _ptr(starts), slots.numel(), n_rows, max_new)
+
+
+class Rotary:
+    """Rotary positions: table [n_positions, rot_dim] fp32 (cosines, then sines); positions [n_axes, n_rows] int32 or None (a
+    token's place in its sequence); axis_pairs: the frequencies of each axis where there are several."""
+
+    def __init__(self, table, positions=None, axis_pairs=None, interleaved: bool = False):
+        self.tensors = (table, positions)    # keep alive
+        n_axes = len(axis_pairs) if axis_pairs else 1
+        if n_axes > 4 or (positions is not None and positions.dim() == 2 and positions.shape[0] != n_axes):
+            raise ValueError("one to four axes, a row of positions and a number of frequencies for each")
+        self.c = _Rotary(_ptr(table), table.shape[0], table.shape[1], int(interleaved), _ptr(positions), n_axes)
+        for k, n in enumerate(axis_pairs or ()):
+            self.c.axis_pairs[k] = n
+
+
+def kv4_clear(cache: KvCache):
+    _check(lib().larosa_kv4_clear(ctypes.byref(cache.c), _stream()), "larosa_kv4_clear")
+
+
+def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, out=None, rotary: Rotary | None = None):
+    """The rows' new keys and values into the cache; out (may be qkv) receives q as turned and k, v as stored."""
+    _check(lib().larosa_kv4_append(ctypes.byref(cache.c), layer, ctypes.byref(batch.c), _ptr(qkv), qkv.stride(0), n_heads,
+                                   ctypes.byref(rotary.c) if rotary is not None else None, _ptr(out),
+                                   0 if out is None else out.stride(0), _stream()), "larosa_kv4_append")
+    return out
+
+
+def kv4_attention_workspace(cache: KvCache, batch: KvBatch, n_heads: int, max_len: int = 0, device="cuda:0") -> Workspace:
+    nbytes = lib().larosa_kv4_attention_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c), n_heads, max_len)
+    if nbytes == 0:
+        raise LarosaError(EINVAL, "larosa_kv4_attention_workspace_bytes")
+    return Workspace(nbytes, device)
+
+
+def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, out, ws: Workspace, scale: float | None = None,
+                  window: int = 0, max_len: int = 0):
+    """out[row] = attention of the row's query heads (the first n_heads heads of q's row) over the cache; scale defaults to
+    1 / sqrt(head_dim)."""
+    if scale is None:
+        scale = cache.c.head_dim ** -0.5
+    _check(lib().larosa_kv4_attention(ctypes.byref(cache.c), layer, ctypes.byref(batch.c), _ptr(q), q.stride(0), n_heads, scale,
+                                      window, max_len, _ptr(out), out.stride(0), ws.ptr, ws.nbytes, _stream()),
+           "larosa_kv4_attention")
+    return out

@@ -17,9 +17,6 @@ static __device__ __align__(256) unsigned char scratch[LAROSA_STATIC_SCRATCH_BYT
 
 namespace {
 
-constexpr size_t kCounterSlots = 4096;                        // arrival counters at the head of a workspace
-constexpr size_t kCounterWords = kCounterSlots * kCounterStride;
-constexpr size_t kCounterBytes = kCounterWords * sizeof(unsigned);
 constexpr int kMaxTopkD = 32768;
 constexpr size_t kHistBytes = kHistWords * sizeof(unsigned);
 

@@ -29,6 +29,9 @@ struct GemvArgs {
 };
 
 constexpr int kCounterStride = 64;   // in 32-bit words: one arrival counter per 256 bytes
+constexpr size_t kCounterSlots = 4096;                        // arrival counters at the head of a workspace
+constexpr size_t kCounterWords = kCounterSlots * kCounterStride;
+constexpr size_t kCounterBytes = kCounterWords * sizeof(unsigned);
 
 struct GemvPlan {
   int strip_cols, nstrips, chunk, G;

@@ -1,0 +1,140 @@
+// C ABI of the 4-bit key/value cache: argument checks, workspace carving, launch sequencing.
+#include "../../include/larosa.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "kernels.hpp"
+#include "kv4.hpp"
+
+using namespace larosa;
+
+namespace {
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+inline hipStream_t stream_of(void* s) { return static_cast<hipStream_t>(s); }
+inline int status_of(hipError_t e) { return e == hipSuccess ? LAROSA_OK : LAROSA_EHIP; }
+
+// Sizes of a cache; nothing of it is read.
+int check_sizes(const larosa_kv4_cache* C) {
+  if (!C || C->n_layers < 1 || C->n_pages < 1 || C->n_slots < 1 || C->max_pages < 1 || C->n_kv_heads < 1) return LAROSA_EINVAL;
+  if (C->dtype != LAROSA_F16 && C->dtype != LAROSA_BF16) return LAROSA_EINVAL;
+  if (C->page_tokens != 32 && C->page_tokens != 64 && C->page_tokens != 128 && C->page_tokens != 256) return LAROSA_EINVAL;
+  if (C->head_dim != 64 && C->head_dim != 128 && C->head_dim != 256) return LAROSA_EUNSUPPORTED;
+  // places in a sequence and numbers of pages are 32-bit
+  if (static_cast<long>(C->max_pages) * C->page_tokens >= (1L << 30) || C->n_kv_heads > 4096) return LAROSA_EUNSUPPORTED;
+  if (C->n_pages > (1 << 28) || C->n_slots > (1 << 20) || C->n_layers > 65535) return LAROSA_EUNSUPPORTED;
+  return LAROSA_OK;
+}
+
+int check_cache(const larosa_kv4_cache* C) {
+  if (int rc = check_sizes(C)) return rc;
+  if (!C->data || !C->refs || !C->table || !C->length) return LAROSA_EINVAL;
+  if (!aligned(C->data, 16) || !aligned(C->refs, 4) || !aligned(C->table, 4) || !aligned(C->length, 4)) return LAROSA_EINVAL;
+  return LAROSA_OK;
+}
+
+int check_batch(const larosa_kv4_batch* b) {
+  if (!b || !b->slots || b->n_seq < 1 || b->n_rows < 1 || b->max_new < 1) return LAROSA_EINVAL;
+  if (!aligned(b->slots, 4) || !aligned(b->starts, 4)) return LAROSA_EINVAL;
+  if (!b->starts && (b->max_new != 1 || b->n_rows < b->n_seq)) return LAROSA_EINVAL;
+  if (b->n_seq > 65535 || b->max_new > (1 << 20)) return LAROSA_EUNSUPPORTED;
+  return LAROSA_OK;
+}
+
+int check_heads(const larosa_kv4_cache* C, int n_heads) {
+  if (n_heads < 1 || n_heads % C->n_kv_heads) return LAROSA_EINVAL;
+  return n_heads > 65536 ? LAROSA_EUNSUPPORTED : LAROSA_OK;
+}
+
+int check_rotary(const larosa_rotary* r, const larosa_kv4_cache* C) {
+  if (!r->table || !aligned(r->table, 4) || !aligned(r->positions, 4) || r->n_positions < 1) return LAROSA_EINVAL;
+  if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > C->head_dim) return LAROSA_EINVAL;
+  if (r->n_axes < 1 || r->n_axes > 4 || (r->n_axes > 1 && !r->positions)) return LAROSA_EINVAL;
+  if (r->n_axes > 1) {
+    int sum = 0;
+    for (int i = 0; i < r->n_axes; ++i) {
+      if (r->axis_pairs[i] < 0 || r->axis_pairs[i] > r->rot_dim / 2) return LAROSA_EINVAL;
+      sum += r->axis_pairs[i];
+    }
+    if (sum != r->rot_dim / 2) return LAROSA_EINVAL;
+  }
+  return LAROSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t larosa_kv4_page_bytes(int page_tokens, int n_kv_heads, int head_dim) {
+  larosa_kv4_cache C{};
+  C.n_layers = C.n_pages = C.n_slots = C.max_pages = 1;
+  C.page_tokens = page_tokens; C.n_kv_heads = n_kv_heads; C.head_dim = head_dim;
+  if (check_sizes(&C) != LAROSA_OK) return 0;
+  return static_cast<size_t>(n_kv_heads) * (page_tokens / 32) * 34 * head_dim;
+}
+
+size_t larosa_kv4_data_bytes(const larosa_kv4_cache* C) {
+  if (check_sizes(C) != LAROSA_OK) return 0;
+  return static_cast<size_t>(C->n_layers) * C->n_pages * larosa_kv4_page_bytes(C->page_tokens, C->n_kv_heads, C->head_dim);
+}
+
+int larosa_kv4_clear(const larosa_kv4_cache* C, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  hipStream_t st = stream_of(stream);
+  if (launch_fill_u32(reinterpret_cast<unsigned*>(C->refs), C->n_pages, 0u, st) != hipSuccess) return LAROSA_EHIP;
+  if (launch_fill_u32(reinterpret_cast<unsigned*>(C->length), C->n_slots, 0u, st) != hipSuccess) return LAROSA_EHIP;
+  return status_of(launch_fill_u32(reinterpret_cast<unsigned*>(C->table), static_cast<size_t>(C->n_slots) * C->max_pages, ~0u, st));
+}
+
+int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* b, const void* qkv, int ld_qkv, int n_heads,
+                      const larosa_rotary* rotary, void* out, int ld_out, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (int rc = check_batch(b)) return rc;
+  if (int rc = check_heads(C, n_heads)) return rc;
+  if (layer < 0 || layer >= C->n_layers || !qkv || !aligned(qkv, 16) || !aligned(out, 16)) return LAROSA_EINVAL;
+  const long width = (static_cast<long>(n_heads) + 2 * C->n_kv_heads) * C->head_dim;
+  if (ld_qkv < width || ld_qkv % 8) return LAROSA_EINVAL;
+  if (out && (ld_out < width || ld_out % 8 || (out == qkv && ld_out != ld_qkv))) return LAROSA_EINVAL;
+  if (rotary) {
+    if (int rc = check_rotary(rotary, C)) return rc;
+    if (!out) return LAROSA_EINVAL;
+  }
+  if (static_cast<double>(b->max_new) * width / 8 >= 2147483648.0 - 256) return LAROSA_EUNSUPPORTED;
+  Kv4AppendArgs a{};
+  a.C = *C; a.b = *b; a.layer = layer; a.n_heads = n_heads;
+  if (rotary) a.r = *rotary;
+  a.qkv = static_cast<const uint16_t*>(qkv); a.ld_qkv = ld_qkv;
+  a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
+  return status_of(launch_kv4_append(a, stream_of(stream)));
+}
+
+size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int max_len) {
+  if (check_sizes(C) != LAROSA_OK || check_batch(b) != LAROSA_OK || check_heads(C, n_heads) != LAROSA_OK || max_len < 0) return 0;
+  return kCounterBytes;
+}
+
+int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* b, const void* q, int ld_q, int n_heads,
+                         float scale, int window, int max_len, void* out, int ld_out, void* ws, size_t ws_bytes, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (int rc = check_batch(b)) return rc;
+  if (int rc = check_heads(C, n_heads)) return rc;
+  if (layer < 0 || layer >= C->n_layers || !q || !out || !aligned(q, 16) || !aligned(out, 16)) return LAROSA_EINVAL;
+  const long width = static_cast<long>(n_heads) * C->head_dim;
+  if (ld_q < width || ld_q % 8 || ld_out < width || ld_out % 8 || q == out) return LAROSA_EINVAL;
+  if (!std::isfinite(scale) || window < 0 || max_len < 0) return LAROSA_EINVAL;
+  if (!ws || !aligned(ws, 256) || ws_bytes < larosa_kv4_attention_workspace_bytes(C, b, n_heads, max_len)) return LAROSA_EWORKSPACE;
+  Kv4AttentionArgs a{};
+  a.C = *C; a.b = *b; a.layer = layer; a.n_heads = n_heads; a.group = n_heads / C->n_kv_heads;
+  a.q = static_cast<const uint16_t*>(q); a.ld_q = ld_q;
+  a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.window = window;
+  const long tiles = (static_cast<long>(b->max_new) * a.group + 15) / 16;
+  if (tiles * C->n_kv_heads >= (1L << 31)) return LAROSA_EUNSUPPORTED;
+  a.row_tiles = static_cast<int>(tiles);
+  return status_of(launch_kv4_attention(a, stream_of(stream)));
+}
+
+}  // extern "C"

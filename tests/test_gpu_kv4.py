@@ -1,0 +1,279 @@
+"""The 4-bit key/value cache on the GPU against its CPU statement: append (rotary positions, quantisation) bit for bit, attention
+against fp64 softmax with a derived tolerance."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4_oracle as K
+from oracle import larosa_oracle as O
+from tests import kv4_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+def run_attention(C, slots, starts, q_bits, n_heads, window=0, scale=None, max_new=1, layer=0, ld_extra=0, max_len=0, n_rows=None):
+    from paper_2507_01299_amd import api
+    cache = U.device_cache(C)
+    D, rows = C.head_dim, q_bits.shape[0]
+    qd = torch.full((rows, n_heads * D + ld_extra), float("nan"), dtype=api.torch_dtype(C.dtype), device="cuda:0")
+    qd[:, :n_heads * D] = U.to_dev(q_bits, C.dtype)
+    out = torch.full((rows, n_heads * D + 2 * ld_extra), 77.0, dtype=api.torch_dtype(C.dtype), device="cuda:0")
+    batch = api.KvBatch(U.int32(slots), rows if n_rows is None else n_rows, starts=U.int32(starts), max_new=max_new)
+    ws = api.kv4_attention_workspace(cache, batch, n_heads, max_len)
+    api.kv4_attention(cache, layer, batch, qd, n_heads, out, ws, scale=scale, window=window, max_len=max_len)
+    torch.cuda.synchronize()
+    got = O.decode16(U.to_bits(out[:, :n_heads * D].contiguous()), C.dtype).reshape(rows, n_heads, D)
+    assert (out[:, n_heads * D:] == 77.0).all()
+    return got, cache
+
+
+def check_attention(C, slots, starts, q_bits, n_heads, window=0, scale=None, max_new=1, layer=0, **kw):
+    scale = C.head_dim ** -0.5 if scale is None else scale
+    got, _ = run_attention(C, slots, starts, q_bits, n_heads, window=window, scale=scale, max_new=max_new, layer=layer, **kw)
+    q = O.decode16(q_bits, C.dtype).reshape(q_bits.shape[0], n_heads, C.head_dim)
+    want = U.attention_want(C, layer, slots, starts, q, n_heads, scale, window, max_new)
+    for row in range(q_bits.shape[0]):
+        if row not in want:
+            assert (got[row] == 77.0).all(), f"row {row} of no sequence was written"
+            continue
+        o, tol = want[row]
+        assert np.array_equal(np.isnan(got[row]), np.isnan(o)), f"row {row}: NaN"
+        ok = ~np.isnan(o)
+        err = np.abs(got[row] - o)[ok]
+        assert (err <= tol[ok]).all(), f"row {row}: error {err.max():.3e}, {(err / tol[ok]).max():.2f} of the tolerance"
+    return got
+
+
+CASES = [
+    # dtype, head_dim, heads, kv heads, page tokens, lengths
+    ("f16", 128, 4, 4, 32, [1, 2, 15, 16, 17, 31, 32, 33]),
+    ("bf16", 128, 8, 2, 64, [63, 64, 65, 127, 128, 129]),
+    ("f16", 64, 6, 2, 32, [5, 100, 257]),
+    ("bf16", 64, 16, 1, 128, [300, 1]),
+    ("f16", 256, 4, 1, 64, [90, 33]),
+    ("bf16", 256, 3, 3, 256, [257, 40]),
+    ("bf16", 128, 34, 2, 32, [200, 64]),          # 17 rows: a second tile of one row
+    ("f16", 128, 2, 1, 32, [3000, 1100, 5]),
+    ("bf16", 128, 1, 1, 128, [5001]),
+]
+
+
+@pytest.mark.parametrize("dtype,D,heads,kv,P,lengths", CASES)
+def test_attention_one_token(gpu_device, dtype, D, heads, kv, P, lengths):
+    rng = np.random.default_rng(len(lengths) * D + heads)
+    C, slots = U.random_cache(rng, lengths, P, kv, D, dtype)
+    check_attention(C, slots, None, U.random_rows(rng, len(lengths), heads * D, dtype), heads)
+
+
+@pytest.mark.parametrize("dtype,D,heads,kv,P,window", [("f16", 128, 8, 2, 32, 0), ("bf16", 64, 4, 4, 64, 40), ("bf16", 128, 10, 2, 32, 1),
+                                                       ("f16", 256, 4, 2, 32, 64), ("f16", 128, 32, 1, 64, 33)])
+def test_attention_several_new_tokens(gpu_device, dtype, D, heads, kv, P, window):
+    rng = np.random.default_rng(D + heads + window)
+    lengths, news = [70, 9, 33, 400, 20], [5, 9, 1, 7, 3]
+    C, slots = U.random_cache(rng, lengths, P, kv, D, dtype, n_layers=2)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = U.random_rows(rng, int(starts[-1]) + 2, heads * D, dtype)      # two rows behind the last sequence
+    check_attention(C, slots, starts, q, heads, window=window, max_new=9, layer=1, ld_extra=8)
+
+
+def test_attention_prompt(gpu_device):
+    """A whole prompt's rows against its own keys: row 0 sees one token."""
+    rng = np.random.default_rng(11)
+    C, slots = U.random_cache(rng, [150], 32, 1, 128, "bf16")
+    check_attention(C, slots, [0, 150], U.random_rows(rng, 150, 2 * 128, "bf16"), 2, max_new=150)
+
+
+def test_attention_rows_that_see_nothing(gpu_device):
+    """Empty sequences, padding, more new tokens than tokens, missing pages, more rows than a batch allows."""
+    rng = np.random.default_rng(12)
+    D, heads = 128, 4
+    C, slots = U.random_cache(rng, [0, 40, 70, 100, 64, 33], 32, 2, D, "f16", headroom=32)
+    slots = slots.tolist()
+    C.table[slots[2], 0] = -1                     # a dropped page: seen as if masked
+    C.table[slots[3], :] = C.n_pages + 5          # ids outside the pool
+    C.table[slots[5], 1] = -7
+    slots[1] = -1
+    starts = [0, 1, 2, 4, 6, 11, 75, 75]
+    slots.append(C.n_slots)
+    q = U.random_rows(rng, 80, heads * D, "f16")
+    got = check_attention(C, slots, starts, q, heads, max_new=70)
+    assert not got[0].any() and not got[1].any() and not got[4:6].any()
+    assert not got[11:42].any() and got[42].any()      # 64 new rows of a sequence of 33
+    check_attention(C, slots, starts, q, heads, max_new=3)
+    # rows outside the buffer are not touched whatever `starts` says
+    got, _ = run_attention(C, slots[:2], [0, 1, 2], q[:4], heads, max_new=2, n_rows=1)
+    assert not got[0].any() and (got[1:] == 77.0).all()
+    got, _ = run_attention(C, slots[4:6], [-2, 1, 900], q[:4], heads, max_new=900)
+    assert (got[0] != 77.0).any()
+
+
+def test_attention_window_with_dropped_pages(gpu_device):
+    """A sliding window never looks at the pages it has left behind."""
+    rng = np.random.default_rng(13)
+    C, slots = U.random_cache(rng, [500], 32, 2, 64, "bf16")
+    q = U.random_rows(rng, 1, 4 * 64, "bf16")
+    want = check_attention(C, slots, None, q, 4, window=100)
+    C.table[slots[0], :12] = -1                   # tokens 0 .. 383; the window starts at 400
+    assert np.array_equal(check_attention(C, slots, None, q, 4, window=100), want)
+
+
+@pytest.mark.parametrize("dtype,D", [("f16", 128), ("bf16", 64), ("bf16", 256)])
+def test_attention_nan_reaches_the_rows_that_see_it_and_no_other(gpu_device, dtype, D):
+    rng = np.random.default_rng(14)
+    heads = 2
+    C, slots = U.random_cache(rng, [45, 45, 45], 32, 1, D, dtype)
+    for i, which in ((0, 0), (1, 1)):             # token 43 of sequences 0 (K) and 1 (V): the last group is NaN
+        C.block(0, slots[i], 43, 0)[K.scale_place(D, 43 % 32, D // 32 - 1, which)] = K.NAN_SCALE
+    q = U.random_rows(rng, 9, heads * D, dtype)
+    got = check_attention(C, slots, [0, 3, 6, 9], q, heads, max_new=3)
+    assert not np.isnan(got[0]).any() and np.isnan(got[1:3]).all()
+    assert not np.isnan(got[3]).any() and np.isnan(got[4:6, :, -32:]).all() and not np.isnan(got[4:6, :, :-32]).any()
+    assert not np.isnan(got[6:]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_scales_from_smallest_to_largest(gpu_device, dtype):
+    """Values of the smallest to the largest powers of two: the codes' conversion and the sums keep them (below what 40 of them
+    add up to in fp32)."""
+    rng = np.random.default_rng(15)
+    lowest, highest = K.EXPONENTS[dtype]
+    for e in (lowest, lowest + 5, 0, highest - 12, min(highest, 115)):
+        C, slots = U.random_cache(rng, [40], 32, 1, 128, dtype, spread=0)
+        blocks = C.data[:, C.table[slots[0]], :, :, 33 * 128:]
+        blocks[blocks == 125] = e + 127
+        C.data[:, C.table[slots[0]], :, :, 33 * 128:] = blocks
+        print(dtype, "2 **", e, flush=True)
+        check_attention(C, slots, None, U.random_rows(rng, 1, 2 * 128, dtype), 2)
+
+
+def test_attention_extreme_logits(gpu_device):
+    """One key far above the others, all equal, and differences that underflow."""
+    rng = np.random.default_rng(16)
+    C, slots = U.random_cache(rng, [700, 700], 64, 1, 64, "bf16")
+    q = U.random_rows(rng, 2, 64, "bf16", size=30.0)
+    check_attention(C, slots, None, q, 1, scale=1.0)
+    check_attention(C, slots, None, q, 1, scale=0.0)
+    check_attention(C, slots, None, q, 1, scale=-1.0)
+
+
+# ---- append ---------------------------------------------------------------------------------------------------
+
+def make_table(rng, n, rot):
+    a = rng.uniform(-np.pi, np.pi, (n, rot // 2))
+    return np.concatenate([np.cos(a), np.sin(a)], 1).astype(np.float32)
+
+
+def check_append(rng, C, slots, starts, n_heads, qkv_bits, rot=0, axis_pairs=None, positions=None, interleaved=False, n_pos=512,
+                 max_new=1, in_place=False, layer=0, ld_extra=0):
+    from paper_2507_01299_amd import api
+    D, H, dt = C.head_dim, C.n_kv_heads, C.dtype
+    heads = n_heads + 2 * H
+    rows = qkv_bits.shape[0]
+    cache = U.device_cache(C)
+    qkv = torch.zeros(rows, heads * D + ld_extra, dtype=api.torch_dtype(dt), device="cuda:0")
+    qkv[:, :heads * D] = U.to_dev(qkv_bits, dt)
+    out = qkv if in_place else torch.full((rows, heads * D + ld_extra), 77.0, dtype=api.torch_dtype(dt), device="cuda:0")
+    table = make_table(rng, n_pos, rot) if rot else None
+    rotary = api.Rotary(torch.from_numpy(table).to("cuda:0"), axis_pairs=axis_pairs, interleaved=interleaved,
+                        positions=None if positions is None else torch.from_numpy(positions).to("cuda:0")) if rot else None
+    batch = api.KvBatch(U.int32(slots), rows, starts=U.int32(starts), max_new=max_new)
+    api.kv4_append(cache, layer, batch, qkv, n_heads, out=out, rotary=rotary)
+    torch.cuda.synchronize()
+    got = U.to_bits(out[:, :heads * D].contiguous()).reshape(rows, heads, D)
+    if ld_extra:
+        assert (out[:, heads * D:] == (0.0 if in_place else 77.0)).all()
+    x = O.decode16(qkv_bits, dt).reshape(rows, heads, D)
+    done = set()
+    for i, slot in enumerate(slots):
+        _, n_new, mine = U.rows_of(starts, len(slots), i, max_new)
+        if not 0 <= slot < C.n_slots:
+            continue
+        for j, row in enumerate(mine):
+            done.add(row)
+            place = int(C.length[slot]) - n_new + j
+            for h in range(heads):
+                y32, y64 = x[row, h].astype(np.float32), x[row, h]
+                if rot and h < n_heads + H:
+                    pos = [place] if positions is None else positions[:, row]
+                    y32 = K.rotate(x[row, h], table, pos, axis_pairs, interleaved, np.float32)
+                    y64 = K.rotate(x[row, h], table, pos, axis_pairs, interleaved)
+                if h < n_heads:
+                    a, b = O.decode16(got[row, h], dt), y64
+                    assert np.array_equal(np.isnan(a), np.isnan(b))
+                    size = 2 * np.abs(np.where(np.isfinite(x[row, h]), x[row, h], 0.0)).max()
+                    ok = np.isfinite(a) & np.isfinite(b)
+                    # one store, two products and a sum in fp32; f16 subnormals are 2^-24 apart
+                    assert (np.abs(a - b)[ok] <= (U.HALF_STEP[dt] * np.abs(b) * 1.01 + 4 * 2.0 ** -24 * size + 2.0 ** -25)[ok]).all()
+                    ok = ~np.isnan(b)
+                    assert np.array_equal(got[row, h][ok], O.encode16(y32.astype(np.float64), dt)[ok])
+                else:
+                    which, kv = divmod(h - n_heads, H)
+                    codes, scales = K.quantise(y32, dt)
+                    want = O.encode16(K.stored(y32, dt), dt)
+                    a, b = O.decode16(got[row, h], dt), O.decode16(want, dt)
+                    assert np.array_equal(np.isnan(a), np.isnan(b)) and np.array_equal(a[~np.isnan(a)], b[~np.isnan(b)])
+                    block = C.block(layer, slot, place, kv) if place >= 0 else None
+                    if block is not None:
+                        K.write_token(block, D, place % 32, which, codes, scales)
+    for row in set(range(rows)) - done:
+        assert np.array_equal(got[row].reshape(-1), qkv_bits[row] if in_place else O.encode16(np.full(heads * D, 77.0), dt))
+    U.same_state(cache, C)                        # every byte: what was to be written, and nothing else
+
+
+@pytest.mark.parametrize("dtype,D,heads,kv,P,rot,interleaved", [
+    ("f16", 128, 4, 2, 32, 128, False), ("bf16", 128, 2, 1, 64, 64, False), ("bf16", 64, 4, 4, 32, 64, True),
+    ("f16", 256, 2, 1, 128, 256, False), ("bf16", 256, 1, 1, 32, 16, True), ("f16", 64, 3, 1, 32, 0, False)])
+def test_append_one_token(gpu_device, dtype, D, heads, kv, P, rot, interleaved):
+    rng = np.random.default_rng(D + rot + heads)
+    C, slots = U.random_cache(rng, [1, 16, 17, 32, 33, 90], P, kv, D, dtype)
+    check_append(rng, C, slots, None, heads, U.random_rows(rng, 6, (heads + 2 * kv) * D, dtype), rot=rot, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_prompts_with_three_axes(gpu_device, in_place):
+    rng = np.random.default_rng(21)
+    heads, kv, D = 4, 2, 128
+    C, slots = U.random_cache(rng, [70, 5, 40], 32, kv, D, "bf16", n_layers=2)
+    starts = [0, 60, 65, 70]
+    positions = rng.integers(0, 512, (3, 72)).astype(np.int32)
+    check_append(rng, C, slots, starts, heads, U.random_rows(rng, 72, (heads + 2 * kv) * D, "bf16"), rot=128, axis_pairs=(16, 24, 24),
+                 positions=positions, max_new=60, layer=1, in_place=in_place, ld_extra=16)
+
+
+def test_append_special_values_and_bad_places(gpu_device):
+    """Zeros, infinities, NaN, the largest and smallest numbers; padding, missing pages, places below zero, positions outside the table."""
+    for dtype in ("f16", "bf16"):
+        rng = np.random.default_rng(22)
+        heads, kv, D = 2, 1, 64
+        C, slots = U.random_cache(rng, [3, 40, 64, 20, 2], 32, kv, D, dtype, headroom=32)
+        slots = slots.tolist()
+        C.table[slots[1], 1] = -1
+        C.table[slots[2], 1] = C.n_pages
+        slots[3] = -5
+        starts = [0, 3, 5, 7, 9, 14]
+        bits = U.random_rows(rng, 15, (heads + 2 * kv) * D, dtype).reshape(15, -1, 32)
+        special = O.encode16(np.array([0.0, -0.0, np.inf, -np.inf, np.nan, 65504.0, -65504.0, 2.0 ** -24, 6e-5, 1.0]), dtype)
+        bits[0, :, 3] = special[2]
+        bits[1, :, 7] = special[4]
+        bits[2] = 0
+        bits[9, :, :] = special[7]
+        bits[10, :, 5] = special[5]
+        bits[11, :, 5] = special[6]
+        bits[12, :, :] = special[[0, 1, 7, 8] * 8]
+        if dtype == "bf16":
+            bits[13, :, 1] = O.encode16(np.array([3.3e38]), dtype)
+            bits[5, :, :] = O.encode16(np.array([1e-38]), dtype)
+        positions = rng.integers(0, 100, (1, 15)).astype(np.int32)
+        positions[0, [3, 4]] = -1, 100
+        check_append(rng, C, slots, starts, heads, bits.reshape(15, -1), rot=64, positions=positions, n_pos=100, max_new=5)
+
+
+def test_append_ties(gpu_device):
+    """Halves between all neighbouring codes, at several scales and both signs."""
+    for dtype in ("f16", "bf16"):
+        rng = np.random.default_rng(23)
+        x = np.tile([6.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 0.5, 1.5, 3.0, 4.0, 2.0, 1.0, 0.0], (4, 2 * 16))
+        x *= np.array([1.0, -1.0, 2.0 ** -9, -2.0 ** 5])[:, None]
+        C, slots = U.random_cache(rng, [1, 2, 3, 4], 32, 2, 64, dtype)
+        bits = np.concatenate([O.encode16(x[:, :4 * 64], dtype), U.random_rows(rng, 4, 2 * 64, dtype)], 1)
+        check_append(rng, C, slots, None, 2, np.ascontiguousarray(np.roll(bits, 128, axis=1)))

@@ -1,0 +1,133 @@
+"""Host-side checks of the 4-bit key/value cache's entry points that need no GPU: sizes, and refusals before a device is touched."""
+import ctypes
+import os
+
+import pytest
+
+FAKE, OTHER, ODD = 0x1000, 0x2000, 0x1004        # never dereferenced: checks fail first
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2507_01299_amd import api, build
+    if not os.path.exists(api.LIB_PATH):
+        build.build_library()
+    return api.lib()
+
+
+def cache(**kw):
+    from paper_2507_01299_amd import api
+    d = dict(n_layers=2, n_pages=10, page_tokens=64, n_slots=4, max_pages=8, n_kv_heads=2, head_dim=128, dtype=1, data=FAKE, refs=FAKE,
+             table=FAKE, length=FAKE)
+    d.update(kw)
+    return api._KvCache(**d)
+
+
+def batch(**kw):
+    from paper_2507_01299_amd import api
+    d = dict(slots=FAKE, starts=None, n_seq=3, n_rows=3, max_new=1)
+    d.update(kw)
+    return api._KvBatch(**d)
+
+
+def rotary(axis_pairs=(), **kw):
+    from paper_2507_01299_amd import api
+    d = dict(table=FAKE, n_positions=100, rot_dim=128, interleaved=0, positions=None, n_axes=1)
+    d.update(kw)
+    r = api._Rotary(**d)
+    for i, n in enumerate(axis_pairs):
+        r.axis_pairs[i] = n
+    return r
+
+
+BAD_CACHES = [dict(n_layers=0), dict(n_pages=0), dict(n_slots=0), dict(max_pages=0), dict(n_kv_heads=0), dict(page_tokens=16),
+              dict(page_tokens=48), dict(page_tokens=512), dict(dtype=2), dict(dtype=-1)]
+UNSUPPORTED_CACHES = [dict(head_dim=32), dict(head_dim=96), dict(head_dim=512), dict(max_pages=1 << 25), dict(n_pages=1 << 29),
+                      dict(n_slots=1 << 21), dict(n_layers=1 << 16), dict(n_kv_heads=5000)]
+BAD_POINTERS = [dict(data=None), dict(refs=None), dict(table=None), dict(length=None), dict(data=0x1008), dict(table=0x1002)]
+
+
+def test_sizes(lib):
+    ref = ctypes.byref
+    assert lib.larosa_kv4_page_bytes(64, 8, 128) == 8 * 64 * 136
+    assert lib.larosa_kv4_page_bytes(32, 1, 64) == 32 * 68 and lib.larosa_kv4_page_bytes(33, 1, 64) == 0
+    assert lib.larosa_kv4_data_bytes(ref(cache())) == 2 * 10 * 2 * 64 * 136
+    assert lib.larosa_kv4_data_bytes(ref(cache(n_layers=80, n_pages=1 << 20, n_kv_heads=8))) == 80 * (1 << 20) * 8 * 64 * 136
+    for bad in BAD_CACHES + UNSUPPORTED_CACHES:
+        assert lib.larosa_kv4_data_bytes(ref(cache(**bad))) == 0
+    n = lib.larosa_kv4_attention_workspace_bytes(ref(cache(data=None)), ref(batch()), 8, 0)
+    assert n > 0
+    assert lib.larosa_kv4_attention_workspace_bytes(ref(cache()), ref(batch(n_seq=0)), 8, 0) == 0
+    assert lib.larosa_kv4_attention_workspace_bytes(ref(cache()), ref(batch()), 7, 0) == 0
+    assert lib.larosa_kv4_attention_workspace_bytes(ref(cache()), ref(batch()), 8, -1) == 0
+
+
+def test_every_call_checks_the_cache(lib):
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+    calls = [lambda c: lib.larosa_kv4_clear(ref(c), None),
+             lambda c: lib.larosa_kv4_append(ref(c), 0, ref(batch()), FAKE, 1536, 8, None, None, 0, None),
+             lambda c: lib.larosa_kv4_attention(ref(c), 0, ref(batch()), FAKE, 1024, 8, 1.0, 0, 0, OTHER, 1024, FAKE, BIG, None)]
+    for call in calls:
+        for bad in BAD_CACHES + BAD_POINTERS:
+            assert call(cache(**bad)) == api.EINVAL, bad
+        for bad in UNSUPPORTED_CACHES:
+            assert call(cache(**bad)) == api.EUNSUPPORTED, bad
+    assert lib.larosa_kv4_clear(None, None) == api.EINVAL
+
+
+BAD_BATCHES = [dict(slots=None), dict(n_seq=0), dict(n_rows=0), dict(max_new=0), dict(max_new=2), dict(n_rows=2), dict(slots=0x1001),
+               dict(starts=0x1002)]
+
+
+def test_append_refuses(lib):
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+
+    def call(b=None, layer=0, qkv=FAKE, ld=1536, heads=8, r=None, out=OTHER, ld_out=1536):
+        return lib.larosa_kv4_append(ref(cache()), layer, ref(b or batch()), qkv, ld, heads, ref(r) if r else None, out, ld_out, None)
+
+    for bad in BAD_BATCHES:
+        assert call(batch(**bad)) == api.EINVAL, bad
+    assert call(batch(starts=FAKE, max_new=1 << 21)) == api.EUNSUPPORTED
+    assert call(batch(n_seq=70000, n_rows=70000)) == api.EUNSUPPORTED
+    for bad in (dict(layer=-1), dict(layer=2), dict(qkv=None), dict(qkv=ODD), dict(out=ODD), dict(ld=1528), dict(ld=1540), dict(ld_out=1528),
+                dict(ld_out=1537), dict(heads=0), dict(heads=7), dict(out=FAKE, ld_out=1544), dict(out=None, r=rotary()),
+                dict(r=rotary(table=None)), dict(r=rotary(n_positions=0)), dict(r=rotary(rot_dim=24)), dict(r=rotary(rot_dim=256)),
+                dict(r=rotary(rot_dim=0)), dict(r=rotary(n_axes=0)), dict(r=rotary(n_axes=5)), dict(r=rotary((32, 32), n_axes=2)),
+                dict(r=rotary((32, 31), n_axes=2, positions=FAKE)), dict(r=rotary((-1, 65), n_axes=2, positions=FAKE)),
+                dict(r=rotary(positions=0x1002))):
+        assert call(**bad) == api.EINVAL, bad
+
+
+def test_attention_refuses(lib):
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+
+    def call(b=None, layer=0, q=FAKE, ld=1024, heads=8, scale=1.0, window=0, max_len=0, out=OTHER, ld_out=1024, ws=FAKE, nbytes=BIG):
+        return lib.larosa_kv4_attention(ref(cache()), layer, ref(b or batch()), q, ld, heads, scale, window, max_len, out, ld_out, ws, nbytes,
+                                        None)
+
+    for bad in BAD_BATCHES:
+        assert call(batch(**bad)) == api.EINVAL, bad
+    for bad in (dict(layer=-1), dict(layer=2), dict(q=None), dict(q=ODD), dict(out=None), dict(out=ODD), dict(out=FAKE), dict(ld=1016),
+                dict(ld=1025), dict(ld_out=1016), dict(ld_out=1028), dict(heads=0), dict(heads=9), dict(scale=float("nan")),
+                dict(scale=float("inf")), dict(window=-1), dict(max_len=-1)):
+        assert call(**bad) == api.EINVAL, bad
+    need = lib.larosa_kv4_attention_workspace_bytes(ref(cache()), ref(batch()), 8, 0)
+    for bad in (dict(ws=None), dict(ws=0x1010), dict(nbytes=need - 1)):
+        assert call(**bad) == api.EWORKSPACE, bad
+
+
+def test_binding_refuses():
+    import torch
+    from paper_2507_01299_amd import api
+    with pytest.raises(api.LarosaError):
+        api.KvCache(1, 4, 48, 1, 1, 1, 64, "f16", device="cpu")
+    z = torch.zeros(4, dtype=torch.int32)
+    for kw in (dict(refs=z), dict(refs=z, table=z[:1], length=z), dict(refs=z, table=z[:2], length=z[:1].float())):
+        with pytest.raises(ValueError):
+            api.KvCache(1, 4, 32, 1, 2, 1, 64, "f16", device="cpu", **kw)
+    with pytest.raises(ValueError):
+        api.Rotary(torch.zeros(8, 64), positions=torch.zeros(2, 8, dtype=torch.int32), axis_pairs=(8, 8, 16))
