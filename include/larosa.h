@@ -340,6 +340,45 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
                          int n_heads, float scale, int window, int max_len, void* out, int ld_out, void* ws, size_t ws_bytes,
                          void* stream);
 
+/* ---- Pages of the cache.  The bookkeeping lives on the device and is changed in stream order; nothing returns to the host
+ * unless the caller reads it.  Lists hold slots (int32, device).  Free pages are handed out from the lowest id on, in the order of
+ * the list, so that equal calls give equal tables.  `status` (one int32, device) receives 0, or says why nothing was changed.
+ * Workspace: larosa_kv4_pages_workspace_bytes, initialised by larosa_workspace_init like any other. */
+size_t larosa_kv4_pages_workspace_bytes(const larosa_kv4_cache* C);
+
+/* Room for counts[i] more tokens (counts NULL: one) in every listed slot; length grows by as much, and the tokens are then stored by
+ * one larosa_kv4_append for each layer.  Where a slot's last page is not full and shared, the slot takes a copy of it (of
+ * all layers) first; if all that share it are in the list, the last of them keeps it.  status: 0; the number of pages that
+ * are missing; or -1: a slot out of range or listed twice, a negative count, a table row too short.  1 <= n <= n_slots. */
+int larosa_kv4_grow(const larosa_kv4_cache* C, const int32_t* slots, const int32_t* counts, int n, int32_t* status, void* ws,
+                    size_t ws_bytes, void* stream);
+
+/* The sequence of src[i] becomes that of the free slot dst[i] too; all pages are shared.  status: 0, or -1: a slot out of
+ * range, dst[i] not free, listed twice or among src.  A src may be listed several times.  1 <= n <= n_slots. */
+int larosa_kv4_fork(const larosa_kv4_cache* C, const int32_t* src, const int32_t* dst, int n, int32_t* status, void* stream);
+
+/* Every listed slot keeps its first keep[i] tokens at most (keep NULL: none, the slot is free again); pages that no table names
+ * any more are free.  Slots out of range are passed over, a negative keep counts as 0; of a slot listed several times the smallest
+ * keep counts. */
+int larosa_kv4_trim(const larosa_kv4_cache* C, const int32_t* slots, const int32_t* keep, int n, void* stream);
+
+/* Pages in use move to the lowest ids: with n of them, those with ids from n on (ascending) into the free ids below n (ascending);
+ * tables and refs follow.  live (one int32, device, nullable) receives n: pages from n on are free. */
+int larosa_kv4_compact(const larosa_kv4_cache* C, int32_t* live, void* ws, size_t ws_bytes, void* stream);
+
+/* Page src[i] of every layer into page dst[i], for a caller with bookkeeping of its own; pairs with an id out of range are passed
+ * over.  No dst twice or among src.  tables and refs are not touched. */
+int larosa_kv4_copy_pages(const larosa_kv4_cache* C, const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/* One decoder layer with this cache as its attention core: larosa_layer_qkv, larosa_kv4_append, larosa_kv4_attention and
+ * larosa_layer_after_attention over batch->n_rows rows, x [n_rows, d] -> x_out [n_rows, d].  The lengths count the rows'
+ * tokens already (larosa_kv4_grow once for all layers).  L's head_dim, d_kv and dtype are the cache's.  trace as in the split calls.
+ * Rows of no sequence come out unspecified.  Workspace: larosa_layer_kv4_workspace_bytes, initialised as ever. */
+size_t larosa_layer_kv4_workspace_bytes(const larosa_layer* L, const larosa_kv4_cache* C, const larosa_kv4_batch* batch, int max_len);
+int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* batch,
+                             const larosa_rotary* rotary, float scale, int window, int max_len, const void* x, void* x_out,
+                             const larosa_trace* trace, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- NOT part of the stable interface: launch tuning for tests and experiments.
  * Process-wide host state read by every call (launch shapes AND workspace sizes depend on it): not
  * thread-safe; change it only while no call of this library is in flight, and before sizing a workspace.

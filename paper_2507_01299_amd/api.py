@@ -110,6 +110,17 @@ def lib() -> ctypes.CDLL:
         L.larosa_kv4_attention_workspace_bytes.restype = sz
         L.larosa_kv4_attention_workspace_bytes.argtypes = [cache, batch, i, i]
         L.larosa_kv4_attention.argtypes = [cache, i, batch, vp, i, i, ctypes.c_float, i, i, vp, i, vp, sz, vp]
+        L.larosa_kv4_pages_workspace_bytes.restype = sz
+        L.larosa_kv4_pages_workspace_bytes.argtypes = [cache]
+        L.larosa_kv4_grow.argtypes = [cache, vp, vp, i, vp, vp, sz, vp]
+        L.larosa_kv4_fork.argtypes = [cache, vp, vp, i, vp, vp]
+        L.larosa_kv4_trim.argtypes = [cache, vp, vp, i, vp]
+        L.larosa_kv4_compact.argtypes = [cache, vp, vp, sz, vp]
+        L.larosa_kv4_copy_pages.argtypes = [cache, vp, vp, i, vp]
+        L.larosa_layer_kv4_workspace_bytes.restype = sz
+        L.larosa_layer_kv4_workspace_bytes.argtypes = [ctypes.POINTER(_Layer), cache, batch, i]
+        L.larosa_layer_forward_kv4.argtypes = [ctypes.POINTER(_Layer), cache, i, batch, rotary, ctypes.c_float, i, i, vp, vp,
+                                               ctypes.POINTER(_Trace), vp, sz, vp]
         _lib = L
     return _lib
 
@@ -453,3 +464,57 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
                                       window, max_len, _ptr(out), out.stride(0), ws.ptr, ws.nbytes, _stream()),
            "larosa_kv4_attention")
     return out
+
+
+def kv4_pages_workspace(cache: KvCache, device="cuda:0") -> Workspace:
+    return Workspace(lib().larosa_kv4_pages_workspace_bytes(ctypes.byref(cache.c)), device)
+
+
+def kv4_grow(cache: KvCache, slots, status, ws: Workspace, counts=None):
+    """Room for counts (default one) more tokens in every listed slot; status [1] int32: 0, pages missing, or -1."""
+    _check(lib().larosa_kv4_grow(ctypes.byref(cache.c), _ptr(slots), _ptr(counts), slots.numel(), _ptr(status), ws.ptr, ws.nbytes,
+                                 _stream()), "larosa_kv4_grow")
+    return status
+
+
+def kv4_fork(cache: KvCache, src, dst, status):
+    """The sequences of src into the free slots dst, all pages shared; status [1] int32: 0 or -1."""
+    _check(lib().larosa_kv4_fork(ctypes.byref(cache.c), _ptr(src), _ptr(dst), src.numel(), _ptr(status), _stream()),
+           "larosa_kv4_fork")
+    return status
+
+
+def kv4_trim(cache: KvCache, slots, keep=None):
+    """Listed slots keep their first keep tokens (default none)."""
+    _check(lib().larosa_kv4_trim(ctypes.byref(cache.c), _ptr(slots), _ptr(keep), slots.numel(), _stream()), "larosa_kv4_trim")
+
+
+def kv4_compact(cache: KvCache, live, ws: Workspace):
+    """Pages in use to the lowest ids; live [1] int32 (or None) receives their number."""
+    _check(lib().larosa_kv4_compact(ctypes.byref(cache.c), _ptr(live), ws.ptr, ws.nbytes, _stream()), "larosa_kv4_compact")
+    return live
+
+
+def kv4_copy_pages(cache: KvCache, src, dst):
+    """Pages src of every layer into pages dst."""
+    _check(lib().larosa_kv4_copy_pages(ctypes.byref(cache.c), _ptr(src), _ptr(dst), src.numel(), _stream()), "larosa_kv4_copy_pages")
+
+
+def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: int = 0, device="cuda:0") -> Workspace:
+    nbytes = lib().larosa_layer_kv4_workspace_bytes(ctypes.byref(layer.c), ctypes.byref(cache.c), ctypes.byref(batch.c), max_len)
+    if nbytes == 0:
+        raise LarosaError(EINVAL, "larosa_layer_kv4_workspace_bytes")
+    return Workspace(nbytes, device)
+
+
+def layer_forward_kv4(layer: Layer, cache: KvCache, index: int, batch: KvBatch, x, x_out, ws: Workspace, rotary: Rotary | None = None,
+                      scale: float | None = None, window: int = 0, max_len: int = 0, trace: dict | None = None):
+    """A decoder layer whose attention runs over layer `index` of the cache; the rows' tokens are counted in the lengths."""
+    if scale is None:
+        scale = cache.c.head_dim ** -0.5
+    tr = _trace_struct(trace)
+    _check(lib().larosa_layer_forward_kv4(ctypes.byref(layer.c), ctypes.byref(cache.c), index, ctypes.byref(batch.c),
+                                          ctypes.byref(rotary.c) if rotary is not None else None, scale, window, max_len, _ptr(x),
+                                          _ptr(x_out), ctypes.byref(tr) if tr is not None else None, ws.ptr, ws.nbytes, _stream()),
+           "larosa_layer_forward_kv4")
+    return x_out

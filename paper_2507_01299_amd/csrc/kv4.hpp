@@ -34,4 +34,23 @@ struct Kv4AttentionArgs {
 };
 hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, hipStream_t s);
 
+// ---- pages (kv4_pages.hip) -----------------------------------------------------------------------------
+// Scratch behind the arrival counters of a workspace.
+struct Kv4Scratch {
+  int32_t* n_pairs;           // [1] pages to copy
+  int32_t* pair_src;          // [n_pages]
+  int32_t* pair_dst;          // [n_pages]
+  int32_t* free_ids;          // [n_pages] grow: pages to hand out; compact: where a page moves to
+  int32_t* growing;           // [n_pages] grow: listed slots that would write into a shared page
+  int32_t* last;              // [n_pages] grow: the last of them, by its place in the list, from 1
+  int32_t* mark;              // [n_slots] grow: times listed
+  int32_t* offset;            // [n_slots] grow: pages handed out before a slot's
+};
+hipError_t launch_kv4_grow(const larosa_kv4_cache& C, const int32_t* slots, const int32_t* counts, int n, int32_t* status,
+                           const Kv4Scratch& x, hipStream_t s);
+hipError_t launch_kv4_fork(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, int n, int32_t* status, hipStream_t s);
+hipError_t launch_kv4_trim(const larosa_kv4_cache& C, const int32_t* slots, const int32_t* keep, int n, hipStream_t s);
+hipError_t launch_kv4_compact(const larosa_kv4_cache& C, int32_t* live, const Kv4Scratch& x, hipStream_t s);
+hipError_t launch_kv4_copy_pages(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, int n, hipStream_t s);
+
 }  // namespace larosa

@@ -25,6 +25,7 @@ int check_sizes(const larosa_kv4_cache* C) {
   // places in a sequence and numbers of pages are 32-bit
   if (static_cast<long>(C->max_pages) * C->page_tokens >= (1L << 30) || C->n_kv_heads > 4096) return LAROSA_EUNSUPPORTED;
   if (C->n_pages > (1 << 28) || C->n_slots > (1 << 20) || C->n_layers > 65535) return LAROSA_EUNSUPPORTED;
+  if (static_cast<long>(C->n_slots) * C->max_pages >= (1L << 31)) return LAROSA_EUNSUPPORTED;   // (counts of pages are 32-bit)
   return LAROSA_OK;
 }
 
@@ -61,6 +62,37 @@ int check_rotary(const larosa_rotary* r, const larosa_kv4_cache* C) {
     if (sum != r->rot_dim / 2) return LAROSA_EINVAL;
   }
   return LAROSA_OK;
+}
+
+inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+size_t scratch_bytes(const larosa_kv4_cache* C) {
+  return 256 + 5 * round_up(static_cast<size_t>(C->n_pages) * 4, 256) + 2 * round_up(static_cast<size_t>(C->n_slots) * 4, 256);
+}
+
+Kv4Scratch scratch_of(const larosa_kv4_cache* C, void* ws) {
+  char* p = static_cast<char*>(ws) + kCounterBytes;
+  auto take = [&](size_t words) {
+    int32_t* r = reinterpret_cast<int32_t*>(p);
+    p += round_up(words * 4, 256);
+    return r;
+  };
+  Kv4Scratch x;
+  x.n_pairs = take(1);
+  x.pair_src = take(C->n_pages);
+  x.pair_dst = take(C->n_pages);
+  x.free_ids = take(C->n_pages);
+  x.growing = take(C->n_pages);
+  x.last = take(C->n_pages);
+  x.mark = take(C->n_slots);
+  x.offset = take(C->n_slots);
+  return x;
+}
+
+// A list of slots and the status it reports to.
+int check_list(const larosa_kv4_cache* C, const int32_t* list, int n) {
+  if (!list || !aligned(list, 4) || n < 1) return LAROSA_EINVAL;
+  return n > C->n_slots ? LAROSA_EINVAL : LAROSA_OK;      // more than there are slots: one is listed twice
 }
 
 }  // namespace
@@ -135,6 +167,107 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   if (tiles * C->n_kv_heads >= (1L << 31)) return LAROSA_EUNSUPPORTED;
   a.row_tiles = static_cast<int>(tiles);
   return status_of(launch_kv4_attention(a, stream_of(stream)));
+}
+
+// ---- pages ---------------------------------------------------------------------------------------
+
+size_t larosa_kv4_pages_workspace_bytes(const larosa_kv4_cache* C) {
+  return check_sizes(C) == LAROSA_OK ? kCounterBytes + scratch_bytes(C) : 0;
+}
+
+int larosa_kv4_grow(const larosa_kv4_cache* C, const int32_t* slots, const int32_t* counts, int n, int32_t* status, void* ws,
+                    size_t ws_bytes, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (int rc = check_list(C, slots, n)) return rc;
+  if (!aligned(counts, 4) || !status || !aligned(status, 4)) return LAROSA_EINVAL;
+  if (!ws || !aligned(ws, 256) || ws_bytes < larosa_kv4_pages_workspace_bytes(C)) return LAROSA_EWORKSPACE;
+  return status_of(launch_kv4_grow(*C, slots, counts, n, status, scratch_of(C, ws), stream_of(stream)));
+}
+
+int larosa_kv4_fork(const larosa_kv4_cache* C, const int32_t* src, const int32_t* dst, int n, int32_t* status, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (int rc = check_list(C, src, n)) return rc;
+  if (int rc = check_list(C, dst, n)) return rc;
+  if (!status || !aligned(status, 4)) return LAROSA_EINVAL;
+  return status_of(launch_kv4_fork(*C, src, dst, n, status, stream_of(stream)));
+}
+
+int larosa_kv4_trim(const larosa_kv4_cache* C, const int32_t* slots, const int32_t* keep, int n, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (!slots || !aligned(slots, 4) || !aligned(keep, 4) || n < 1) return LAROSA_EINVAL;
+  if (n > (1 << 20)) return LAROSA_EUNSUPPORTED;
+  return status_of(launch_kv4_trim(*C, slots, keep, n, stream_of(stream)));
+}
+
+int larosa_kv4_compact(const larosa_kv4_cache* C, int32_t* live, void* ws, size_t ws_bytes, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (!aligned(live, 4)) return LAROSA_EINVAL;
+  if (!ws || !aligned(ws, 256) || ws_bytes < larosa_kv4_pages_workspace_bytes(C)) return LAROSA_EWORKSPACE;
+  return status_of(launch_kv4_compact(*C, live, scratch_of(C, ws), stream_of(stream)));
+}
+
+int larosa_kv4_copy_pages(const larosa_kv4_cache* C, const int32_t* src, const int32_t* dst, int n, void* stream) {
+  if (int rc = check_cache(C)) return rc;
+  if (!src || !dst || !aligned(src, 4) || !aligned(dst, 4) || n < 1 || n > C->n_pages) return LAROSA_EINVAL;
+  return status_of(launch_kv4_copy_pages(*C, src, dst, n, stream_of(stream)));
+}
+
+// ---- a decoder layer with the cache as its attention core -------------------------------------------
+
+namespace {
+
+// Whether a layer, a cache and a batch fit together (the layer's own checks are its calls').
+int check_layer_cache(const larosa_layer* L, const larosa_kv4_cache* C, const larosa_kv4_batch* b) {
+  if (!L) return LAROSA_EINVAL;
+  if (int rc = check_sizes(C)) return rc;
+  if (int rc = check_batch(b)) return rc;
+  if (L->head_dim != C->head_dim || L->dtype != C->dtype || L->d_kv != C->n_kv_heads * C->head_dim || L->d_q % C->head_dim)
+    return LAROSA_EINVAL;
+  return check_heads(C, L->d_q / C->head_dim);
+}
+
+// What the three steps use one after the other; q|k|v, the shortcut and the attention's output lie behind it.
+size_t shared_scratch(const larosa_layer* L, const larosa_kv4_cache* C, const larosa_kv4_batch* b, int max_len) {
+  const size_t layer = larosa_layer_workspace_bytes(L, b->n_rows);
+  const size_t attention = larosa_kv4_attention_workspace_bytes(C, b, L->d_q / C->head_dim, max_len);
+  if (!layer || !attention) return 0;
+  return round_up(layer > attention ? layer : attention, 256);
+}
+
+}  // namespace
+
+size_t larosa_layer_kv4_workspace_bytes(const larosa_layer* L, const larosa_kv4_cache* C, const larosa_kv4_batch* b, int max_len) {
+  if (check_layer_cache(L, C, b) != LAROSA_OK) return 0;
+  const size_t head = shared_scratch(L, C, b, max_len);
+  if (!head) return 0;
+  const size_t rows = b->n_rows;
+  return head + round_up(rows * (L->d_q + 2 * static_cast<size_t>(L->d_kv)) * 2, 256) + round_up(rows * L->d * 2, 256) +
+         round_up(rows * L->d_q * 2, 256);
+}
+
+int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* b,
+                             const larosa_rotary* rotary, float scale, int window, int max_len, const void* x, void* x_out,
+                             const larosa_trace* trace, void* ws, size_t ws_bytes, void* stream) {
+  if (int rc = check_layer_cache(L, C, b)) return rc;
+  if (int rc = check_cache(C)) return rc;
+  // everything that one of the steps could refuse, before the first of them is enqueued
+  if (layer < 0 || layer >= C->n_layers || !std::isfinite(scale) || window < 0 || max_len < 0) return LAROSA_EINVAL;
+  if (!x || !x_out || x == x_out || !aligned(x, 16) || !aligned(x_out, 16)) return LAROSA_EINVAL;
+  if (rotary)
+    if (int rc = check_rotary(rotary, C)) return rc;
+  const size_t need = larosa_layer_kv4_workspace_bytes(L, C, b, max_len);
+  if (!need) return LAROSA_EINVAL;
+  if (!ws || !aligned(ws, 256) || ws_bytes < need) return LAROSA_EWORKSPACE;
+  const size_t head = shared_scratch(L, C, b, max_len), rows = b->n_rows;
+  const int d_qkv = L->d_q + 2 * L->d_kv, heads = L->d_q / C->head_dim;
+  char* p = static_cast<char*>(ws) + head;
+  void* qkv = p;
+  void* s1 = p += round_up(rows * d_qkv * 2, 256);
+  void* attn = p += round_up(rows * L->d * 2, 256);
+  if (int rc = larosa_layer_qkv(L, x, qkv, s1, b->n_rows, trace, ws, head, stream)) return rc;
+  if (int rc = larosa_kv4_append(C, layer, b, qkv, d_qkv, heads, rotary, qkv, d_qkv, stream)) return rc;
+  if (int rc = larosa_kv4_attention(C, layer, b, qkv, d_qkv, heads, scale, window, max_len, attn, L->d_q, ws, head, stream)) return rc;
+  return larosa_layer_after_attention(L, L->shortcut_attn ? s1 : x, attn, x_out, b->n_rows, trace, ws, head, stream);
 }
 
 }  // extern "C"

@@ -44,7 +44,7 @@ def rotary(axis_pairs=(), **kw):
 BAD_CACHES = [dict(n_layers=0), dict(n_pages=0), dict(n_slots=0), dict(max_pages=0), dict(n_kv_heads=0), dict(page_tokens=16),
               dict(page_tokens=48), dict(page_tokens=512), dict(dtype=2), dict(dtype=-1)]
 UNSUPPORTED_CACHES = [dict(head_dim=32), dict(head_dim=96), dict(head_dim=512), dict(max_pages=1 << 25), dict(n_pages=1 << 29),
-                      dict(n_slots=1 << 21), dict(n_layers=1 << 16), dict(n_kv_heads=5000)]
+                      dict(n_slots=1 << 21), dict(n_slots=1 << 20, max_pages=1 << 12), dict(n_layers=1 << 16), dict(n_kv_heads=5000)]
 BAD_POINTERS = [dict(data=None), dict(refs=None), dict(table=None), dict(length=None), dict(data=0x1008), dict(table=0x1002)]
 
 
@@ -67,6 +67,11 @@ def test_every_call_checks_the_cache(lib):
     from paper_2507_01299_amd import api
     ref = ctypes.byref
     calls = [lambda c: lib.larosa_kv4_clear(ref(c), None),
+             lambda c: lib.larosa_kv4_grow(ref(c), FAKE, None, 2, FAKE, FAKE, BIG, None),
+             lambda c: lib.larosa_kv4_fork(ref(c), FAKE, OTHER, 2, FAKE, None),
+             lambda c: lib.larosa_kv4_trim(ref(c), FAKE, None, 2, None),
+             lambda c: lib.larosa_kv4_compact(ref(c), None, FAKE, BIG, None),
+             lambda c: lib.larosa_kv4_copy_pages(ref(c), FAKE, OTHER, 2, None),
              lambda c: lib.larosa_kv4_append(ref(c), 0, ref(batch()), FAKE, 1536, 8, None, None, 0, None),
              lambda c: lib.larosa_kv4_attention(ref(c), 0, ref(batch()), FAKE, 1024, 8, 1.0, 0, 0, OTHER, 1024, FAKE, BIG, None)]
     for call in calls:
@@ -117,6 +122,50 @@ def test_attention_refuses(lib):
         assert call(**bad) == api.EINVAL, bad
     need = lib.larosa_kv4_attention_workspace_bytes(ref(cache()), ref(batch()), 8, 0)
     for bad in (dict(ws=None), dict(ws=0x1010), dict(nbytes=need - 1)):
+        assert call(**bad) == api.EWORKSPACE, bad
+
+
+def test_page_calls_refuse(lib):
+    from paper_2507_01299_amd import api
+    c = ctypes.byref(cache())
+    need = lib.larosa_kv4_pages_workspace_bytes(c)
+    assert need > 1 << 20 and lib.larosa_kv4_pages_workspace_bytes(ctypes.byref(cache(page_tokens=7))) == 0
+    for slots, counts, n, status in ((None, None, 2, FAKE), (0x1001, None, 2, FAKE), (FAKE, 0x1002, 2, FAKE), (FAKE, None, 0, FAKE),
+                                     (FAKE, None, 5, FAKE), (FAKE, None, 2, None), (FAKE, None, 2, 0x1001)):
+        assert lib.larosa_kv4_grow(c, slots, counts, n, status, FAKE, BIG, None) == api.EINVAL
+    for ws, n in ((None, BIG), (0x1010, BIG), (FAKE, need - 1)):
+        assert lib.larosa_kv4_grow(c, FAKE, None, 2, FAKE, ws, n, None) == api.EWORKSPACE
+        assert lib.larosa_kv4_compact(c, None, ws, n, None) == api.EWORKSPACE
+    for src, dst, n, status in ((None, FAKE, 1, FAKE), (FAKE, None, 1, FAKE), (FAKE, OTHER, 0, FAKE), (FAKE, OTHER, 5, FAKE),
+                                (FAKE, OTHER, 1, None), (0x1001, OTHER, 1, FAKE)):
+        assert lib.larosa_kv4_fork(c, src, dst, n, status, None) == api.EINVAL
+    for slots, keep, n in ((None, None, 1), (FAKE, 0x1001, 1), (FAKE, None, 0)):
+        assert lib.larosa_kv4_trim(c, slots, keep, n, None) == api.EINVAL
+    assert lib.larosa_kv4_trim(c, FAKE, None, 1 << 21, None) == api.EUNSUPPORTED
+    assert lib.larosa_kv4_compact(c, 0x1002, FAKE, BIG, None) == api.EINVAL
+    for src, dst, n in ((None, FAKE, 1), (FAKE, None, 1), (FAKE, OTHER, 0), (FAKE, OTHER, 11), (FAKE, 0x2001, 1)):
+        assert lib.larosa_kv4_copy_pages(c, src, dst, n, None) == api.EINVAL
+
+
+def test_layer_with_cache_refuses(lib):
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+    layer = lambda **kw: api._Layer(**dict(dict(d=256, d_q=512, d_kv=256, d_ff=704, head_dim=128, K1=100, K2=100, K3=100, K4=300, Wqkv=FAKE,  # noqa: E731
+                                                Wo=FAKE, Wgu=FAKE, Wdown=FAKE, rms_eps=-1.0, dtype=1), **kw))
+    L, C, b = layer(), cache(), batch()
+    need = lib.larosa_layer_kv4_workspace_bytes(ref(L), ref(C), ref(b), 0)
+    assert need > lib.larosa_layer_workspace_bytes(ref(L), 3)
+
+    def call(L=L, C=C, b=b, layer=0, r=None, scale=1.0, window=0, max_len=0, x=FAKE, x_out=OTHER, ws=FAKE, n=BIG):
+        return lib.larosa_layer_forward_kv4(ref(L), ref(C), layer, ref(b), ref(r) if r else None, scale, window, max_len, x, x_out, None, ws, n,
+                                            None)
+
+    for bad in (dict(L=layer(head_dim=64)), dict(L=layer(dtype=0)), dict(L=layer(d_kv=128)), dict(L=layer(d_q=576)), dict(L=layer(K1=0)),
+                dict(L=layer(Wo=None)), dict(C=cache(data=None)), dict(C=cache(page_tokens=5)), dict(b=batch(n_seq=0)), dict(layer=2),
+                dict(layer=-1), dict(scale=float("inf")), dict(window=-1), dict(max_len=-1), dict(x=None), dict(x=ODD), dict(x_out=None),
+                dict(x_out=FAKE), dict(x_out=ODD), dict(r=rotary(rot_dim=8))):
+        assert call(**bad) == api.EINVAL, bad
+    for bad in (dict(ws=None), dict(ws=0x1010), dict(n=need - 1)):
         assert call(**bad) == api.EWORKSPACE, bad
 
 
