@@ -408,6 +408,7 @@ class KvCache:
             raise ValueError("refs, table and length are contiguous int32 tensors, data is contiguous")
         self.data, self.refs, self.table, self.length = data, refs, table, length
         self.c.data, self.c.refs, self.c.table, self.c.length = (t.data_ptr() for t in (data, refs, table, length))
+        self.ref = ctypes.byref(self.c)
         if fresh:
             kv4_clear(self)
 
@@ -419,6 +420,7 @@ class KvBatch:
     def __init__(self, slots, n_rows: int, starts=None, max_new: int = 1):
         self.tensors = (slots, starts)       # keep alive
         self.c = _KvBatch(_ptr(slots), _ptr(starts), slots.numel(), n_rows, max_new)
+        self.ref = ctypes.byref(self.c)
 
 
 class Rotary:
@@ -433,22 +435,23 @@ class Rotary:
         self.c = _Rotary(_ptr(table), table.shape[0], table.shape[1], int(interleaved), _ptr(positions), n_axes)
         for k, n in enumerate(axis_pairs or ()):
             self.c.axis_pairs[k] = n
+        self.ref = ctypes.byref(self.c)
 
 
 def kv4_clear(cache: KvCache):
-    _check(lib().larosa_kv4_clear(ctypes.byref(cache.c), _stream()), "larosa_kv4_clear")
+    _check(lib().larosa_kv4_clear(cache.ref, _stream()), "larosa_kv4_clear")
 
 
 def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, out=None, rotary: Rotary | None = None):
     """The rows' new keys and values into the cache; out (may be qkv) receives q as turned and k, v as stored."""
-    _check(lib().larosa_kv4_append(ctypes.byref(cache.c), layer, ctypes.byref(batch.c), _ptr(qkv), qkv.stride(0), n_heads,
-                                   ctypes.byref(rotary.c) if rotary is not None else None, _ptr(out),
+    _check(lib().larosa_kv4_append(cache.ref, layer, batch.ref, _ptr(qkv), qkv.stride(0), n_heads,
+                                   rotary.ref if rotary is not None else None, _ptr(out),
                                    0 if out is None else out.stride(0), _stream()), "larosa_kv4_append")
     return out
 
 
 def kv4_attention_workspace(cache: KvCache, batch: KvBatch, n_heads: int, max_len: int = 0, device="cuda:0") -> Workspace:
-    nbytes = lib().larosa_kv4_attention_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c), n_heads, max_len)
+    nbytes = lib().larosa_kv4_attention_workspace_bytes(cache.ref, batch.ref, n_heads, max_len)
     if nbytes == 0:
         raise LarosaError(EINVAL, "larosa_kv4_attention_workspace_bytes")
     return Workspace(nbytes, device)
@@ -460,48 +463,48 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
     1 / sqrt(head_dim)."""
     if scale is None:
         scale = cache.c.head_dim ** -0.5
-    _check(lib().larosa_kv4_attention(ctypes.byref(cache.c), layer, ctypes.byref(batch.c), _ptr(q), q.stride(0), n_heads, scale,
+    _check(lib().larosa_kv4_attention(cache.ref, layer, batch.ref, _ptr(q), q.stride(0), n_heads, scale,
                                       window, max_len, _ptr(out), out.stride(0), ws.ptr, ws.nbytes, _stream()),
            "larosa_kv4_attention")
     return out
 
 
 def kv4_pages_workspace(cache: KvCache, device="cuda:0") -> Workspace:
-    return Workspace(lib().larosa_kv4_pages_workspace_bytes(ctypes.byref(cache.c)), device)
+    return Workspace(lib().larosa_kv4_pages_workspace_bytes(cache.ref), device)
 
 
 def kv4_grow(cache: KvCache, slots, status, ws: Workspace, counts=None):
     """Room for counts (default one) more tokens in every listed slot; status [1] int32: 0, pages missing, or -1."""
-    _check(lib().larosa_kv4_grow(ctypes.byref(cache.c), _ptr(slots), _ptr(counts), slots.numel(), _ptr(status), ws.ptr, ws.nbytes,
+    _check(lib().larosa_kv4_grow(cache.ref, _ptr(slots), _ptr(counts), slots.numel(), _ptr(status), ws.ptr, ws.nbytes,
                                  _stream()), "larosa_kv4_grow")
     return status
 
 
 def kv4_fork(cache: KvCache, src, dst, status):
     """The sequences of src into the free slots dst, all pages shared; status [1] int32: 0 or -1."""
-    _check(lib().larosa_kv4_fork(ctypes.byref(cache.c), _ptr(src), _ptr(dst), src.numel(), _ptr(status), _stream()),
+    _check(lib().larosa_kv4_fork(cache.ref, _ptr(src), _ptr(dst), src.numel(), _ptr(status), _stream()),
            "larosa_kv4_fork")
     return status
 
 
 def kv4_trim(cache: KvCache, slots, keep=None):
     """Listed slots keep their first keep tokens (default none)."""
-    _check(lib().larosa_kv4_trim(ctypes.byref(cache.c), _ptr(slots), _ptr(keep), slots.numel(), _stream()), "larosa_kv4_trim")
+    _check(lib().larosa_kv4_trim(cache.ref, _ptr(slots), _ptr(keep), slots.numel(), _stream()), "larosa_kv4_trim")
 
 
 def kv4_compact(cache: KvCache, live, ws: Workspace):
     """Pages in use to the lowest ids; live [1] int32 (or None) receives their number."""
-    _check(lib().larosa_kv4_compact(ctypes.byref(cache.c), _ptr(live), ws.ptr, ws.nbytes, _stream()), "larosa_kv4_compact")
+    _check(lib().larosa_kv4_compact(cache.ref, _ptr(live), ws.ptr, ws.nbytes, _stream()), "larosa_kv4_compact")
     return live
 
 
 def kv4_copy_pages(cache: KvCache, src, dst):
     """Pages src of every layer into pages dst."""
-    _check(lib().larosa_kv4_copy_pages(ctypes.byref(cache.c), _ptr(src), _ptr(dst), src.numel(), _stream()), "larosa_kv4_copy_pages")
+    _check(lib().larosa_kv4_copy_pages(cache.ref, _ptr(src), _ptr(dst), src.numel(), _stream()), "larosa_kv4_copy_pages")
 
 
 def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: int = 0, device="cuda:0") -> Workspace:
-    nbytes = lib().larosa_layer_kv4_workspace_bytes(ctypes.byref(layer.c), ctypes.byref(cache.c), ctypes.byref(batch.c), max_len)
+    nbytes = lib().larosa_layer_kv4_workspace_bytes(ctypes.byref(layer.c), cache.ref, batch.ref, max_len)
     if nbytes == 0:
         raise LarosaError(EINVAL, "larosa_layer_kv4_workspace_bytes")
     return Workspace(nbytes, device)
@@ -513,8 +516,8 @@ def layer_forward_kv4(layer: Layer, cache: KvCache, index: int, batch: KvBatch, 
     if scale is None:
         scale = cache.c.head_dim ** -0.5
     tr = _trace_struct(trace)
-    _check(lib().larosa_layer_forward_kv4(ctypes.byref(layer.c), ctypes.byref(cache.c), index, ctypes.byref(batch.c),
-                                          ctypes.byref(rotary.c) if rotary is not None else None, scale, window, max_len, _ptr(x),
+    _check(lib().larosa_layer_forward_kv4(ctypes.byref(layer.c), cache.ref, index, batch.ref,
+                                          rotary.ref if rotary is not None else None, scale, window, max_len, _ptr(x),
                                           _ptr(x_out), ctypes.byref(tr) if tr is not None else None, ws.ptr, ws.nbytes, _stream()),
            "larosa_layer_forward_kv4")
     return x_out

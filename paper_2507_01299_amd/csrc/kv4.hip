@@ -26,6 +26,7 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kBlockTokens = 32;
 constexpr uint32_t kScaleNaN = 255;
+constexpr int kNowhere = 1 << 30;     // past every token
 
 // f(0), f(1), .. f(N - 1) with the number as a type: operands that have to be constants
 template <int I> struct Number { static constexpr int value = I; };
@@ -93,14 +94,19 @@ struct Sequence {
   bool real;                  // the slot exists
 };
 
-// Sequence s of a batch; n_new is cut to what the batch allows.
-__device__ __forceinline__ Sequence sequence(const larosa_kv4_cache& C, const larosa_kv4_batch& b, int s) {
+// Sequence s of a batch, its length left out: a load that waits for the slot's.
+__device__ __forceinline__ Sequence sequence_rows(const larosa_kv4_cache& C, const larosa_kv4_batch& b, int s) {
   Sequence q;
   q.row0 = b.starts ? b.starts[s] : s;
   q.n_new = b.starts ? b.starts[s + 1] - q.row0 : 1;
   q.slot = b.slots[s];
   q.real = q.slot >= 0 && q.slot < C.n_slots;
-  q.len = q.real ? C.length[q.slot] : 0;
+  q.len = 0;
+  return q;
+}
+__device__ __forceinline__ Sequence sequence(const larosa_kv4_cache& C, const larosa_kv4_batch& b, int s) {
+  Sequence q = sequence_rows(C, b, s);
+  if (q.real) q.len = C.length[q.slot];
   return q;
 }
 
@@ -231,19 +237,248 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
 
 // ---- attention ----------------------------------------------------------------------------------------
 
-// One workgroup: 16 rows (new token, query head of the group) of one key/value head of one sequence; its four waves take every
-// fourth block of 32 tokens each and join at the end.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4AttentionArgs a) {
-  constexpr int DW = D / 32;                                  // dwords of a lane's codes in a tile of 16 tokens
-  constexpr int NG = D / 32;                                  // scale groups of a head
-  constexpr int LW = DW < 4 ? DW : 4;                         // dwords of one load
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// What a wave holds of one block of 32 tokens.
+template <int D> struct Block {
+  static constexpr int DW = D / 32;                           // dwords of a lane's codes in a tile of 16 tokens
+  static constexpr int KG = D > 128 ? 2 : 1;                  // scale groups of a lane's part of a key
+  uint32_t kc[2][DW], vc[2][DW];
+  uint32_t kb[2][KG], vs[2];                                  // scale bytes: of the lane's token; of its four tokens
+};
+
+template <int D> using Piece = uint32_t __attribute__((ext_vector_type(D < 128 ? D / 32 : 4)));
+
+// The wave's codes of one block: 16 tokens' keys or values in runs of 64 pieces, one of each lane.  ONCE: no other workgroup
+// reads them, so they pass the caches by (64 sequences of up to 16384 tokens: 87.7 -> 79.5 us, 4.7 TB/s).
+template <int D, bool ONCE>
+__device__ __forceinline__ void load_codes(uint32_t (&c)[2][D / 32], const uint8_t* codes, int lane) {
+  constexpr int LW = sizeof(Piece<D>) / 4;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int p = 0; p < D / 32 / LW; ++p) {
+      const Piece<D>* at = reinterpret_cast<const Piece<D>*>(codes + u * 8 * D + (p * 64 + lane) * LW * 4);
+const Piece<D> v = ONCE ? __builtin_nontemporal_load(at) : *at;
+#pragma unroll
+      for (int i = 0; i < LW; ++i) c[u][p * LW + i] = v[i];
+    }
+}
+template <int D, bool ONCE>
+__device__ __forceinline__ void load_keys(Block<D>& x, const uint8_t* block, int lane) {
+  load_codes<D, ONCE>(x.kc, block, lane);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int h = 0; h < Block<D>::KG; ++h) x.kb[u][h] = block[32 * D + u * (D / 2) + 16 * ((lane >> 4) * (D / 32) / 4 + h) + (lane & 15)];
+}
+template <int D, bool ONCE>
+__device__ __forceinline__ void load_values(Block<D>& x, const uint8_t* block, int lane) {
+  load_codes<D, ONCE>(x.vc, block + 16 * D, lane);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    x.vs[u] = *reinterpret_cast<const uint32_t*>(block + 33 * D + u * (D / 2) + ((lane >> 4) * (D / 32) + (lane & 15) * (D / 32) / 16) * 4);
+}
+
+// What a lane knows of its row, and its tile of the others.
+struct Seen {
+  int from, to;               // the row sees tokens [from, to)
+  int lo, hi;                 // no row of the tile sees a token outside
+  int all_from, all_to;       // every row of the tile sees all in between
+};
+
+// A reference for a row's exponentials need not be its maximum: it moves only when a logit exceeds it by more than this (a power
+// of two, so weights stay below 2^8 and the 16-bit formats as exact as ever), which spares most blocks the exchange between
+// lanes and the rescaling of the accumulators.
+constexpr float kSlack = 8.f;
+
+// The running state of a lane: row lane mod 16, values [kq D/4, (kq + 1) D/4) of its output in o[k][i] = value i D/16 + k.
+template <int D> struct Running {
+  floatx4 o[D / 16];
+  float ref, total;           // total: the lane's own tokens
+};
+
+// One block of tokens t0 .. t0 + 31, in x.  As soon as x's keys are used up those of the block at `next` (null: none) are on
+// their way into the same registers, and so are the values.
+template <typename T, int D, bool ONCE>
+__device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, const uint8_t* next, int t0, const u32x4_t (&qf)[D / 32], const Seen& see,
+                                             float scale_log2, int lane, Running<D>& r) {
+  constexpr int DW = D / 32, NG = D / 32;
+  const int kq = lane >> 4;
+  const bool cut = t0 < see.all_from || t0 + kBlockTokens > see.all_to;       // some row does not see some token
+  uint32_t odd = any_nan_byte(x.vs[0]) | any_nan_byte(x.vs[1]);
+#pragma unroll
+  for (int h = 0; h < Block<D>::KG; ++h) odd |= (x.kb[0][h] == kScaleNaN) | (x.kb[1][h] == kScaleNaN);
+  const bool nan_groups = __any(odd != 0);
+
+  float p[8];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    floatx4 sc = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < DW; ++k) {
+      const float f = scale_of(x.kb[u][k / 4]);
+      const u32x4_t kv = {Mat<T>::template pair<0>(x.kc[u][k], f), Mat<T>::template pair<1>(x.kc[u][k], f),
+                          Mat<T>::template pair<2>(x.kc[u][k], f), Mat<T>::template pair<3>(x.kc[u][k], f)};
+      sc = Mat<T>::mfma(kv, qf[k], sc);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[4 * u + i] = sc[i] * scale_log2;
+  }
+  if (next) load_keys<D, ONCE>(x, next, lane);
+  uint64_t nan_v = 0;                                         // groups with a NaN value that this lane's row sees
+  if (nan_groups || cut) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = t0 + 16 * (i / 4) + 4 * kq + i % 4;
+      if (nan_groups)
+        for (int g = 0; g < NG; ++g)
+          if (block[32 * D + i / 4 * (D / 2) + 16 * g + 4 * kq + i % 4] == kScaleNaN) p[i] = __uint_as_float(0x7FC00000u);
+      if (t < see.from || t >= see.to) p[i] = -INFINITY;
+      // what no row of the tile sees may hold anything: its values count as zeros
+      if (t < see.lo || t >= see.hi) x.vs[i / 4] &= ~(0xFFu << (8 * (i % 4)));
+    }
+    if (nan_groups) {
+      for (int t = 0; t < kBlockTokens; ++t)
+        for (int g = 0; g < NG; ++g) {
+          const uint8_t sb = block[33 * D + t / 16 * (D / 2) + (t % 16 / 4 * NG + g) * 4 + t % 4];
+          if (sb == kScaleNaN && t0 + t >= see.from && t0 + t < see.to) nan_v |= 1ull << g;
+        }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if ((x.vs[i / 4] >> (8 * (i % 4)) & 0xFFu) == kScaleNaN) x.vs[i / 4] &= ~(0xFFu << (8 * (i % 4)));
+    }
+  }
+  float m = p[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, p[i]);
+  if (__any(m > r.ref + kSlack)) {                            // (nothing seen yet: ref is -inf)
+    const float now = fmaxf(r.ref, over_quarters_max(m));
+    const float back = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.ref - now);
+    r.ref = now;
+    r.total *= back;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.o[k][i] *= back;
+  }
+  const float ref = r.ref == -INFINITY ? 0.f : r.ref;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
+    r.total += p[i];
+  }
+  // weights to 16 bits: half a step of 2^-8 (bf16) or 2^-11 (f16) relative on each, independent over the tokens
+  const u32x4_t pf = {Mat<T>::round2(p[0], p[1]), Mat<T>::round2(p[2], p[3]), Mat<T>::round2(p[4], p[5]), Mat<T>::round2(p[6], p[7])};
+  float vf[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) vf[i] = scale_of(x.vs[i / 4] >> (8 * (i % 4)) & 0xFFu);
+  static_for<D / 32>([&](auto jb) {                           // two values of the lane's eight tokens
+    constexpr int J = decltype(jb)::value;
+    uint32_t y[8];
+    static_for<8>([&](auto ii) {
+      constexpr int I = decltype(ii)::value, B = I % 4 * (D / 32) + J;
+      y[I] = Mat<T>::template pair<B % 4>(x.vc[I / 4][B / 4], vf[I]);
+    });
+    u32x4_t even, odd2;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      even[h] = __builtin_amdgcn_perm(y[2 * h + 1], y[2 * h], 0x05040100u);
+      odd2[h] = __builtin_amdgcn_perm(y[2 * h + 1], y[2 * h], 0x07060302u);
+    }
+    r.o[2 * J] = Mat<T>::mfma(even, pf, r.o[2 * J]);
+    r.o[2 * J + 1] = Mat<T>::mfma(odd2, pf, r.o[2 * J + 1]);
+  });
+  if (next) load_values<D, ONCE>(x, next, lane);
+  if (nan_v) {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (nan_v >> (((4 * kq + i) * (D / 16) + k) / 32) & 1) r.o[k][i] = __uint_as_float(0x7FC00000u);
+  }
+}
+
+constexpr int kWaves = 4;
+template <int D> struct JoinShared {
+  float ref[kWaves][16], total[kWaves][16];
+  float o[kWaves - 1][64][D / 4 + 1];
+};
+
+// The workgroup's waves into wave 0 (every lane calls; only wave 0's r is then of use).  total is a row's on entry and on return.
+template <int D>
+__device__ __forceinline__ void join_waves(Running<D>& r, JoinShared<D>& sh, int lane, int wave) {
+  const int n = lane & 15, kq = lane >> 4;
+  if (kq == 0) {
+    sh.ref[wave][n] = r.ref;
+    sh.total[wave][n] = r.total;
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sh.o[wave - 1][lane][4 * k + i] = r.o[k][i];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float best = sh.ref[0][n];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) best = fmaxf(best, sh.ref[w][n]);
+  const float ref = best == -INFINITY ? 0.f : best;
+  r.ref = best;
+  float f = __builtin_amdgcn_exp2f(sh.ref[0][n] - ref);
+  r.total *= f;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.o[k][i] *= f;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    f = __builtin_amdgcn_exp2f(sh.ref[w][n] - ref);
+    r.total += sh.total[w][n] * f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.o[k][i] += sh.o[w - 1][lane][4 * k + i] * f;
+  }
+}
+
+// A tile of 16 rows (new token, query head of the group) of one key/value head of one sequence, and its splits.
+struct Tile {
+  int base;                   // place of the sequence's first new token
+  Seen see;                   // from and to are a row's own
+  int b_lo, b_hi, splits;     // blocks that some row sees, and the workgroups they are divided among (1 where there are none)
+};
+__device__ __forceinline__ Tile find_tile(const Kv4AttentionArgs& a, const Sequence& sq, int news, int tile) {
+  Tile t;
+  t.base = sq.len - sq.n_new;
+  const int first_j = tile * 16 / a.group, last_j = min(news - 1, (tile * 16 + 15) / a.group);
+  t.see.hi = max(0, min(sq.len, t.base + last_j + 1));
+  t.see.lo = a.window > 0 ? max(0, t.base + first_j + 1 - a.window) : 0;
+  t.see.all_to = t.base + first_j + 1;
+  t.see.all_from = a.window > 0 ? t.base + last_j + 1 - a.window : 0;
+  t.b_lo = t.see.lo / kBlockTokens;
+  t.b_hi = (t.see.hi + kBlockTokens - 1) / kBlockTokens;
+  t.splits = max(1, min(a.splits, (t.b_hi - t.b_lo + a.chunk - 1) / a.chunk));
+  return t;
+}
+
+// Floats of a split's sums: [rows][D], then the rows' references and totals.
+__device__ __forceinline__ float* split_sums(const Kv4AttentionArgs& a, int s, int unit_in_seq, int split, int D) {
+  const size_t unit = static_cast<size_t>(s) * a.row_tiles * a.C.n_kv_heads + unit_in_seq;
+  return a.partial + (unit * a.splits + split) * (static_cast<size_t>(a.partial_rows) * (D + 2));
+}
+
+// One workgroup: a tile of 16 rows and one split of the tokens that they see; its four waves take every fourth block of 32 tokens
+// each.  Where a tile has several splits, each leaves its sums for kv4_combine_kernel.  Bound by HBM where there is work for all
+// compute units (about 230 vector instructions for a block of 4352 bytes at head_dim 128: 1000 cycles of a SIMD, and 2300 at the rate
+// of a large copy); a short call is a chain of loads: slot, length and page, keys, output.
+template <typename T, int D, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_attention_kernel(Kv4AttentionArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, kq = lane >> 4;
   const int head = blockIdx.x % a.C.n_kv_heads;
   const int tile = blockIdx.x / a.C.n_kv_heads;
-  const int s = blockIdx.y;
-  Sequence sq = sequence(a.C, a.b, s);
+  const int split = blockIdx.z;
+  Sequence sq = sequence_rows(a.C, a.b, blockIdx.y);
   const int news = min(sq.n_new, a.b.max_new);
   if (tile * 16 >= news * a.group) return;
   // this lane's row
@@ -251,172 +486,200 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4AttentionArgs a) 
   const int j = r / a.group, hq = head * a.group + r % a.group;
   const int row = sq.row0 + j;
   const bool has_row = j < news && row >= 0 && row < a.b.n_rows;
-  const int base = sq.len - sq.n_new;                         // place of the sequence's first new token
-  const int first_j = tile * 16 / a.group, last_j = min(news - 1, (tile * 16 + 15) / a.group);
-  const int seen_to = base + j + 1, seen_from = a.window > 0 ? max(0, seen_to - a.window) : 0;
-  const int hi = max(0, min(sq.len, base + last_j + 1));
-  const int lo = a.window > 0 ? max(0, base + first_j + 1 - a.window) : 0;
-  // every row of the tile sees the tokens in [all_from, all_to)
-  const int all_to = base + first_j + 1, all_from = a.window > 0 ? base + last_j + 1 - a.window : 0;
-
-  u32x4_t qf[DW];
+  u32x4_t qf[D / 32];
 #pragma unroll
-  for (int k = 0; k < DW; ++k) {
+  for (int k = 0; k < D / 32; ++k) {
     qf[k] = u32x4_t{0, 0, 0, 0};
     if (has_row)
       qf[k] = *reinterpret_cast<const u32x4_t*>(a.q + static_cast<size_t>(row) * a.ld_q + static_cast<size_t>(hq) * D + kq * (D / 4) + 8 * k);
   }
-  floatx4 o[D / 16];
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k) o[k] = floatx4{0, 0, 0, 0};
-  float top = -INFINITY, total = 0.f;
+  // 64 blocks' pages at a time, one to a lane; without a window the first of them do not have to wait for the length
+  const int page_shift = __builtin_ctz(a.C.page_tokens / kBlockTokens);
+  auto pages_from = [&](int c0) { return sq.real ? page_of(a.C, sq.slot, (c0 + lane * kWaves) >> page_shift) : -1; };
+  int my_page = -1;
+  if (a.window == 0) my_page = pages_from(split * a.chunk + wave);
+  if (sq.real) sq.len = a.C.length[sq.slot];
+  Tile t = find_tile(a, sq, news, tile);
+  if (split >= t.splits) return;
+  Seen& see = t.see;
+  see.to = t.base + j + 1;
+  see.from = a.window > 0 ? max(0, see.to - a.window) : 0;
+  // the last split takes whatever is left
+  const int b0 = t.b_lo + split * a.chunk, b1 = split == t.splits - 1 ? t.b_hi : b0 + a.chunk;
+  if (a.window > 0) my_page = pages_from(b0 + wave);
 
-  const int per_page = a.C.page_tokens / kBlockTokens;
-  for (int b = lo / kBlockTokens + wave; b * kBlockTokens < hi; b += 4) {
-    const int page = page_of(a.C, sq.slot, b / per_page);
-    if (page < 0) continue;
-    const uint8_t* block = static_cast<const uint8_t*>(a.C.data) + block_at(a.C, a.layer, page, head, b % per_page, D);
-    uint32_t kc[2][DW], vc[2][DW], kb[2][2], vs[2];
+  Running<D> run;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int k = 0; k < DW; ++k) {
-        kc[u][k] = *reinterpret_cast<const uint32_t*>(block + u * 8 * D + k / LW * 64 * LW * 4 + lane * LW * 4 + k % LW * 4);
-        vc[u][k] = *reinterpret_cast<const uint32_t*>(block + 16 * D + u * 8 * D + k / LW * 64 * LW * 4 + lane * LW * 4 + k % LW * 4);
-      }
-#pragma unroll
-      for (int h = 0; h < (D > 128 ? 2 : 1); ++h) kb[u][h] = block[32 * D + u * (D / 2) + 16 * (kq * NG / 4 + h) + n];
-      vs[u] = *reinterpret_cast<const uint32_t*>(block + 33 * D + u * (D / 2) + (kq * NG + n * NG / 16) * 4);
-    }
-    const int t0 = b * kBlockTokens;
-    const bool cut = t0 < all_from || t0 + kBlockTokens > all_to;      // some row does not see some token
-    uint32_t odd = any_nan_byte(vs[0]) | any_nan_byte(vs[1]) | (kb[0][0] == kScaleNaN) | (kb[1][0] == kScaleNaN);
-    if constexpr (D > 128) odd |= (kb[0][1] == kScaleNaN) | (kb[1][1] == kScaleNaN);
-    const bool nan_groups = __any(odd != 0);
+  for (int k = 0; k < D / 16; ++k) run.o[k] = floatx4{0, 0, 0, 0};
+  run.ref = -INFINITY;
+  run.total = 0.f;
 
-    float p[8];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      floatx4 sc = {0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < DW; ++k) {
-        const float f = scale_of(kb[u][k / 4]);
-        const u32x4_t kv = {Mat<T>::template pair<0>(kc[u][k], f), Mat<T>::template pair<1>(kc[u][k], f),
-                            Mat<T>::template pair<2>(kc[u][k], f), Mat<T>::template pair<3>(kc[u][k], f)};
-        sc = Mat<T>::mfma(kv, qf[k], sc);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[4 * u + i] = sc[i] * a.scale_log2;
+  for (int c0 = b0 + wave; c0 < b1; c0 += 64 * kWaves) {
+    const int mine = min(64, (b1 - c0 + kWaves - 1) / kWaves);
+    if (c0 != b0 + wave) my_page = pages_from(c0);
+    auto address = [&](int i) {                               // (a block without a page: any will do, nobody sees it)
+      const int page = max(0, __builtin_amdgcn_readlane(my_page, i));
+      return static_cast<const uint8_t*>(a.C.data) + block_at(a.C, a.layer, page, head, (c0 + i * kWaves) & ((1 << page_shift) - 1), D);
+    };
+    // two blocks in registers; each is replaced by the one after the next as it is used up
+    auto ahead = [&](int i) { return i < mine ? address(i) : nullptr; };
+    auto work = [&](Block<D>& x, const uint8_t* block, const uint8_t* next, int i) {
+      const int t0 = __builtin_amdgcn_readlane(my_page, i) >= 0 ? (c0 + i * kWaves) * kBlockTokens : kNowhere;
+      attend_block<T, D, ONCE>(x, block, next, t0, qf, see, a.scale_log2, lane, run);
+    };
+    Block<D> x, y;
+    const uint8_t *bx = address(0), *by = ahead(1);
+    load_keys<D, ONCE>(x, bx, lane);
+    load_values<D, ONCE>(x, bx, lane);
+    if (by) {
+      load_keys<D, ONCE>(y, by, lane);
+      load_values<D, ONCE>(y, by, lane);
     }
-    uint64_t nan_v = 0;                                       // of this lane's row: groups with a NaN value that the row sees
-    if (nan_groups || cut) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = t0 + 16 * (i / 4) + 4 * kq + i % 4;
-        if (nan_groups)
-          for (int g = 0; g < NG; ++g)
-            if (block[32 * D + i / 4 * (D / 2) + 16 * g + 4 * kq + i % 4] == kScaleNaN) p[i] = __uint_as_float(0x7FC00000u);
-        if (t < seen_from || t >= seen_to) p[i] = -INFINITY;
-        // what no row of the tile sees may hold anything: its values count as zeros
-        if (t < lo || t >= hi) vs[i / 4] &= ~(0xFFu << (8 * (i % 4)));
-      }
-      if (nan_groups) {
-        for (int t = 0; t < kBlockTokens; ++t)
-          for (int g = 0; g < NG; ++g) {
-            const uint8_t sb = block[33 * D + t / 16 * (D / 2) + (t % 16 / 4 * NG + g) * 4 + t % 4];
-            if (sb == kScaleNaN && t0 + t >= seen_from && t0 + t < seen_to) nan_v |= 1ull << g;
-          }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((vs[i / 4] >> (8 * (i % 4)) & 0xFFu) == kScaleNaN) vs[i / 4] &= ~(0xFFu << (8 * (i % 4)));
-      }
-    }
-    float m = p[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) m = fmaxf(m, p[i]);
-    const float now = fmaxf(top, over_quarters_max(m));
-    const float ref = now == -INFINITY ? 0.f : now;
-    const float back = __builtin_amdgcn_exp2f(top - ref);     // nothing seen so far: 2^-inf = 0
-    top = now;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
-      sum += p[i];
-    }
-    total = total * back + sum;
-    // weights to 16 bits: half a step of 2^-8 (bf16) or 2^-11 (f16) relative on each, independent over the tokens
-    const u32x4_t pf = {Mat<T>::round2(p[0], p[1]), Mat<T>::round2(p[2], p[3]), Mat<T>::round2(p[4], p[5]), Mat<T>::round2(p[6], p[7])};
-    float vf[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) vf[i] = scale_of(vs[i / 4] >> (8 * (i % 4)) & 0xFFu);
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[k][i] *= back;
-    static_for<D / 32>([&](auto jb) {                         // two values of the lane's eight tokens
-      constexpr int J = decltype(jb)::value;
-      uint32_t x[8];
-      static_for<8>([&](auto ii) {
-        constexpr int I = decltype(ii)::value, B = I % 4 * (D / 32) + J;
-        x[I] = Mat<T>::template pair<B % 4>(vc[I / 4][B / 4], vf[I]);
-      });
-      u32x4_t even, odd2;
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        even[h] = __builtin_amdgcn_perm(x[2 * h + 1], x[2 * h], 0x05040100u);
-        odd2[h] = __builtin_amdgcn_perm(x[2 * h + 1], x[2 * h], 0x07060302u);
-      }
-      o[2 * J] = Mat<T>::mfma(even, pf, o[2 * J]);
-      o[2 * J + 1] = Mat<T>::mfma(odd2, pf, o[2 * J + 1]);
-    });
-    if (nan_v) {
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (nan_v >> (((4 * kq + i) * (D / 16) + k) / 32) & 1) o[k][i] = __uint_as_float(0x7FC00000u);
+    for (int i = 0; i < mine; i += 2) {
+      const uint8_t* nx = ahead(i + 2);
+      work(x, bx, nx, i);
+      if (i + 1 >= mine) break;
+      const uint8_t* ny = ahead(i + 3);
+      work(y, by, ny, i + 1);
+      bx = nx;
+      by = ny;
     }
   }
-  total = over_quarters_sum(total);
+  run.total = over_quarters_sum(run.total);
 
-  // join the four waves: a lane's values [kq D/4, (kq+1) D/4) of row n
-  __shared__ float s_top[4][16], s_total[4][16];
-  __shared__ float s_o[3][64][D / 4 + 1];
-  if (kq == 0) {
-    s_top[wave][n] = top;
-    s_total[wave][n] = total;
-  }
-  if (wave > 0) {
+  __shared__ JoinShared<D> sh;
+  join_waves<D>(run, sh, lane, wave);
+  if (t.splits > 1) {
+    if (wave > 0 || n >= a.partial_rows) return;
+    float* sums = split_sums(a, blockIdx.y, blockIdx.x, split, D);
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k)
+    for (int c = 0; c < D / 16; ++c) {
+      floatx4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s_o[wave - 1][lane][i * (D / 16) + k] = o[k][i];
+      for (int e = 0; e < 4; ++e) {
+        const int d = 4 * c + e;
+        v[e] = run.o[d % (D / 16)][d / (D / 16)];
+      }
+      *reinterpret_cast<floatx4*>(sums + n * D + kq * (D / 4) + 4 * c) = v;
+    }
+    if (kq == 0) {
+      sums[a.partial_rows * D + n] = run.ref;
+      sums[a.partial_rows * (D + 1) + n] = run.total;
+    }
+    return;
   }
-  __syncthreads();
   if (wave > 0 || !has_row) return;
-  float best = s_top[0][n];
-  for (int w = 1; w < 4; ++w) best = fmaxf(best, s_top[w][n]);
-  const float ref = best == -INFINITY ? 0.f : best;
-  float f[4], sum = 0.f;
-  for (int w = 0; w < 4; ++w) {
-    f[w] = __builtin_amdgcn_exp2f(s_top[w][n] - ref);
-    sum += s_total[w][n] * f[w];
-  }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  const float inv = run.total == 0.f ? 0.f : 1.0f / run.total;
   uint16_t* dst = a.out + static_cast<size_t>(row) * a.ld_out + static_cast<size_t>(hq) * D + kq * (D / 4);
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int d = 8 * c + e, i = d / (D / 16), k = d % (D / 16);
-      float x = o[k][i] * f[0];
-      for (int w = 1; w < 4; ++w) x += s_o[w - 1][lane][d] * f[w];
-      v[e] = x * inv;
+      const int d = 8 * c + e;
+      v[e] = run.o[d % (D / 16)][d / (D / 16)] * inv;
     }
     *reinterpret_cast<uint4*>(dst + 8 * c) = pack8<T>(v);
   }
+}
+
+// A row's splits into its output: WR waves to a row, each with up to 64 of its splits (their references and totals one to a
+// lane, the sums 16 bytes to a lane).  Latency-bound: two round trips to what the other launch wrote.
+template <typename T, int D, int WR>
+__global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
+  constexpr int PL = D / 4 < 64 ? D / 4 : 64, GL = 64 / PL;   // lanes to a split's sums, splits at a time
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int unit = blockIdx.x;                                // as in kv4_attention_kernel
+  const int head = unit % a.C.n_kv_heads, tile = unit / a.C.n_kv_heads;
+  const int n = blockIdx.z * (4 / WR) + wave / WR;            // row of the tile
+  const int first = wave % WR;
+  // what a split of the plan may have left is read before it is known whether it did: the length takes as long to come
+  const size_t stride = static_cast<size_t>(a.partial_rows) * (D + 2) * WR;
+  const float* sums = split_sums(a, blockIdx.y, unit, first, D);
+  float ref = -INFINITY, total = 0.f;
+  const int most = n < a.partial_rows ? (a.splits - first + WR - 1) / WR : 0;
+  if (lane < most) {
+    ref = sums[lane * stride + a.partial_rows * D + n];
+    total = sums[lane * stride + a.partial_rows * (D + 1) + n];
+  }
+  const int c = lane % PL;
+  constexpr int kEarly = 4;
+  floatx4 early[kEarly];
+#pragma unroll
+  for (int e = 0; e < kEarly; ++e) {
+    const int k = lane / PL + e * GL;
+    early[e] = floatx4{0, 0, 0, 0};
+    if (k < most) early[e] = *reinterpret_cast<const floatx4*>(sums + k * stride + n * D + 4 * c);
+  }
+  const Sequence sq = sequence(a.C, a.b, blockIdx.y);
+  const int news = min(sq.n_new, a.b.max_new);
+  if (tile * 16 >= news * a.group) return;                    // (uniform over the workgroup, as is the next)
+  const Tile t = find_tile(a, sq, news, tile);
+  if (t.splits == 1) return;
+  const int r = tile * 16 + n, j = r / a.group, row = sq.row0 + j;
+  const bool has_row = n < a.partial_rows && j < news && row >= 0 && row < a.b.n_rows;
+  const int mine = has_row ? (t.splits - first + WR - 1) / WR : 0;
+  if (lane >= mine) {
+    ref = -INFINITY;
+    total = 0.f;
+  }
+  float best = ref;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) best = fmaxf(best, __shfl_xor(best, m));
+  const float weight = best == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - best);
+  total = wave_sum(total * weight);
+  floatx4 o = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < kEarly; ++e) {
+    const int k = lane / PL + e * GL;
+    const float w = __shfl(weight, k & 63);
+    if (k < mine) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += w * early[e][i];
+    }
+  }
+#pragma unroll 8
+  for (int k0 = kEarly * GL; k0 < mine; k0 += GL) {           // (uniform over the wave: every lane has its weight to give)
+    const int k = k0 + lane / PL;
+    const float w = __shfl(weight, k & 63);
+    floatx4 v = {0, 0, 0, 0};
+    if (k < mine) v = *reinterpret_cast<const floatx4*>(sums + k * stride + n * D + 4 * c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += w * v[e];
+  }
+#pragma unroll
+  for (int m = PL; m < 64; m *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m);
+  if constexpr (WR > 1) {
+    __shared__ floatx4 s_o[4][PL];
+    __shared__ float s_best[4], s_total[4];
+    if (lane < PL) s_o[wave][lane] = o;
+    if (lane == 0) {
+      s_best[wave] = best;
+      s_total[wave] = total;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < WR; ++w) best = fmaxf(best, s_best[w]);
+    const float all = best == -INFINITY ? 0.f : best;
+    total = 0.f;
+    o = floatx4{0, 0, 0, 0};
+    for (int w = 0; w < WR; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_best[w] - all);
+      total += f * s_total[w];
+      const floatx4 v = s_o[w][c];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += f * v[e];
+    }
+  }
+  if (!has_row || lane >= PL) return;
+  const float inv = total == 0.f ? 0.f : 1.0f / total;
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = o[e] * inv;
+  *reinterpret_cast<uint2*>(a.out + static_cast<size_t>(row) * a.ld_out + static_cast<size_t>(head * a.group + r % a.group) * D + 4 * c) =
+      pack4<T>(v);
 }
 
 template <typename F>
@@ -444,8 +707,18 @@ struct AttentionLaunch {
   const Kv4AttentionArgs& a;
   hipStream_t s;
   template <typename T, int D> hipError_t operator()() const {
-    const dim3 grid(static_cast<unsigned>(a.row_tiles * a.C.n_kv_heads), static_cast<unsigned>(a.b.n_seq));
-    hipLaunchKernelGGL((kv4_attention_kernel<T, D>), grid, dim3(256), 0, s, a);
+    const dim3 grid(static_cast<unsigned>(a.row_tiles * a.C.n_kv_heads), static_cast<unsigned>(a.b.n_seq), static_cast<unsigned>(a.splits));
+    if (a.row_tiles == 1)
+      hipLaunchKernelGGL((kv4_attention_kernel<T, D, true>), grid, dim3(64 * kWaves), 0, s, a);
+    else
+      hipLaunchKernelGGL((kv4_attention_kernel<T, D, false>), grid, dim3(64 * kWaves), 0, s, a);
+    if (a.splits == 1) return hipGetLastError();
+    if (hipError_t e = hipGetLastError()) return e;
+    const unsigned rows = static_cast<unsigned>(a.partial_rows);
+    if (a.splits <= 16)
+      hipLaunchKernelGGL((kv4_combine_kernel<T, D, 1>), dim3(grid.x, grid.y, (rows + 3) / 4), dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((kv4_combine_kernel<T, D, 4>), dim3(grid.x, grid.y, rows), dim3(256), 0, s, a);
     return hipGetLastError();
   }
 };

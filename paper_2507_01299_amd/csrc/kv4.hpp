@@ -31,7 +31,12 @@ struct Kv4AttentionArgs {
   float scale_log2;           // scale * log2(e): the exponentials are powers of two
   int window;                 // 0: none
   int row_tiles;              // of 16 (new token, query head of the group) pairs
+  // the split of the tokens: `chunk` blocks of 32 to a workgroup, up to `splits` workgroups for a tile
+  int chunk, splits;
+  float* partial;             // [n_seq][row_tiles * n_kv_heads][splits][partial_rows * (head_dim + 2)] fp32
+  int partial_rows;           // rows that a tile can have
 };
+constexpr int kKv4SplitsMax = 256;            // that one row's sums are joined from
 hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, hipStream_t s);
 
 // ---- pages (kv4_pages.hip) -----------------------------------------------------------------------------

@@ -66,6 +66,51 @@ int check_rotary(const larosa_rotary* r, const larosa_kv4_cache* C) {
 
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// How an attention call is divided.  A tile of 16 rows sees `blocks` blocks of 32 tokens; its workgroups take `chunk` each, four waves
+// one block at a time, and a second launch adds up what several workgroups of a tile left.  That launch takes 4 us and a
+// workgroup 5 us to come to its first block, a block 1 us, so
+//  - up to 24 blocks are one workgroup's (333 tokens of an 8B model: 6.3 us, with two workgroups a tile 8.4);
+//  - one sequence, or few, are cut into as many pieces as are resident at once, three to a compute unit (100003 tokens of a 70B
+//    model: 31 us with 760 pieces, 37 with 784, 38 with 1024), of eight blocks at least;
+//  - else into pieces of 32 blocks, since lengths differ and a piece past a sequence's end costs nothing (9 sequences of up to
+//    8191 tokens, 7 new each: 23.5 us; pieces of 49 27.0), longer ones past 4096 of them (64 sequences of up to 16384
+//    tokens: 87 us; up to 8192 pieces 96).
+constexpr long kWholeBlocks = 24, kLeastBlocks = 8, kPieceBlocks = 32, kResident = 768, kMostWorkgroups = 4096;
+struct AttentionPlan {
+  long row_tiles, units;      // tiles of 16 rows of a key/value head; such tiles of all sequences
+  int chunk, splits, partial_rows;
+  size_t partial_bytes;
+};
+AttentionPlan plan_attention(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int window, int max_len) {
+  AttentionPlan p{};
+  const long rows = static_cast<long>(b->max_new) * (n_heads / C->n_kv_heads);
+  p.row_tiles = (rows + 15) / 16;
+  p.units = p.row_tiles * C->n_kv_heads * b->n_seq;
+  p.partial_rows = rows < 16 ? static_cast<int>(rows) : 16;
+  const long most = static_cast<long>(C->max_pages) * C->page_tokens;
+  long span = max_len > 0 && max_len < most ? max_len : most;
+  if (window > 0 && window < span) span = window + b->max_new < span ? window + b->max_new : span;
+  const long blocks = (span + 31) / 32 + (window > 0 ? 1 : 0);
+  long chunk = blocks;
+  if (blocks > kWholeBlocks) {
+    if (b->n_seq == 1 || p.units * ((blocks + kPieceBlocks - 1) / kPieceBlocks) < kResident) {
+      const long splits = kResident / p.units > 1 ? kResident / p.units : 1;
+      chunk = (blocks + splits - 1) / splits;
+      if (chunk < kLeastBlocks) chunk = kLeastBlocks;
+    } else {
+      chunk = (blocks * p.units + kMostWorkgroups - 1) / kMostWorkgroups;
+      if (chunk < kPieceBlocks) chunk = kPieceBlocks;
+    }
+    if (chunk * kKv4SplitsMax < blocks) chunk = (blocks + kKv4SplitsMax - 1) / kKv4SplitsMax;
+    if (chunk > blocks) chunk = blocks;
+  }
+  const long splits = (blocks + chunk - 1) / chunk;
+  p.chunk = static_cast<int>(chunk);
+  p.splits = static_cast<int>(splits);
+  p.partial_bytes = splits > 1 ? static_cast<size_t>(p.units) * splits * p.partial_rows * (C->head_dim + 2) * 4 : 0;
+  return p;
+}
+
 size_t scratch_bytes(const larosa_kv4_cache* C) {
   return 256 + 5 * round_up(static_cast<size_t>(C->n_pages) * 4, 256) + 2 * round_up(static_cast<size_t>(C->n_slots) * 4, 256);
 }
@@ -144,7 +189,7 @@ int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_bat
 
 size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int max_len) {
   if (check_sizes(C) != LAROSA_OK || check_batch(b) != LAROSA_OK || check_heads(C, n_heads) != LAROSA_OK || max_len < 0) return 0;
-  return kCounterBytes;
+  return kCounterBytes + round_up(plan_attention(C, b, n_heads, 0, max_len).partial_bytes, 256);
 }
 
 int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* b, const void* q, int ld_q, int n_heads,
@@ -163,9 +208,13 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.window = window;
-  const long tiles = (static_cast<long>(b->max_new) * a.group + 15) / 16;
-  if (tiles * C->n_kv_heads >= (1L << 31)) return LAROSA_EUNSUPPORTED;
-  a.row_tiles = static_cast<int>(tiles);
+  AttentionPlan p = plan_attention(C, b, n_heads, window, max_len);
+  const AttentionPlan all = plan_attention(C, b, n_heads, 0, max_len);      // what the workspace is sized for
+  if (p.splits > all.splits) p = all;
+  if (p.row_tiles * C->n_kv_heads >= (1L << 31)) return LAROSA_EUNSUPPORTED;
+  a.row_tiles = static_cast<int>(p.row_tiles);
+  a.chunk = p.chunk; a.splits = p.splits; a.partial_rows = p.partial_rows;
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
   return status_of(launch_kv4_attention(a, stream_of(stream)));
 }
 
