@@ -124,115 +124,188 @@ __device__ __forceinline__ size_t block_at(const larosa_kv4_cache& C, int layer,
 
 // ---- append -----------------------------------------------------------------------------------------
 
-// One lane takes 8 neighbouring values of a head, so four neighbouring lanes a group of 32 with one scale.  Bound by the bytes of
-// the rows in and out (prompts) or by latency (a decode step).  The partners of a rotation are loaded a second time from the
-// cache line's neighbours rather than exchanged between lanes.
-template <typename T, int D>
+// Cosines and sines for the eight values [8 c, 8 c + 8) of a head at a row's positions.
+template <int D>
+__device__ __forceinline__ void turn_of(const Kv4AppendArgs& a, int c, int row, int place, float (&cs)[8], float (&sn)[8]) {
+  const larosa_rotary& r = a.r;
+  const int half = r.rot_dim / 2;
+  const int f0 = r.interleaved ? 4 * c : (8 * c >= half ? 8 * c - half : 8 * c), nf = r.interleaved ? 4 : 8;
+  auto axis_of = [&](int f) {
+    int axis = 0;
+    for (int end = r.axis_pairs[0]; axis + 1 < r.n_axes && f >= end; end += r.axis_pairs[axis]) ++axis;
+    return axis;
+  };
+  const int axis = r.n_axes > 1 ? axis_of(f0) : 0;
+  const bool one = r.n_axes == 1 || axis_of(f0 + nf - 1) == axis;
+  auto position = [&](int ax) { return r.positions ? r.positions[static_cast<size_t>(ax) * a.b.n_rows + row] : place; };
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = sn[i] = __uint_as_float(0x7FC00000u);       // outside the table
+  if (one) {
+    const int p = position(axis);
+    if (p < 0 || p >= r.n_positions) return;
+    const float4* t = reinterpret_cast<const float4*>(r.table + static_cast<size_t>(p) * r.rot_dim + f0);
+    const float4* u = reinterpret_cast<const float4*>(r.table + static_cast<size_t>(p) * r.rot_dim + half + f0);
+    const float4 c0 = t[0], s0 = u[0];
+    if (r.interleaved) {
+      cs[0] = cs[1] = c0.x; cs[2] = cs[3] = c0.y; cs[4] = cs[5] = c0.z; cs[6] = cs[7] = c0.w;
+      sn[0] = sn[1] = s0.x; sn[2] = sn[3] = s0.y; sn[4] = sn[5] = s0.z; sn[6] = sn[7] = s0.w;
+    } else {
+      const float4 c1 = t[1], s1 = u[1];
+      cs[0] = c0.x; cs[1] = c0.y; cs[2] = c0.z; cs[3] = c0.w; cs[4] = c1.x; cs[5] = c1.y; cs[6] = c1.z; cs[7] = c1.w;
+      sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {                               // the axis changes among the eight
+    const int f = f0 + (r.interleaved ? i / 2 : i);
+    const int p = position(axis_of(f));
+    if (p < 0 || p >= r.n_positions) continue;
+    cs[i] = r.table[static_cast<size_t>(p) * r.rot_dim + f];
+    sn[i] = r.table[static_cast<size_t>(p) * r.rot_dim + half + f];
+  }
+}
+
+// y = v turned; w: the partners (the other half's values), or v itself where they are neighbours.  Products and sums are rounded one by
+// one, so that k is quantised from values that any fp32 program gets.
+__device__ __forceinline__ void turn(const larosa_rotary& r, int c, const float (&cs)[8], const float (&sn)[8], const float (&w)[8],
+                                     float (&v)[8]) {
+#pragma clang fp contract(off)
+  const bool upper = 8 * c >= r.rot_dim / 2;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float other = r.interleaved ? v[i ^ 1] : w[i];
+    const bool second = r.interleaved ? (i & 1) != 0 : upper;
+    const float p0 = v[i] * cs[i], p1 = other * sn[i];
+    y[i] = second ? p0 + p1 : p0 - p1;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = y[i];
+}
+
+__device__ __forceinline__ uint32_t largest_of_four(uint32_t v) {
+  const int i = static_cast<int>(v);
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(i, i, 0xB1, 0xF, 0xF, false)));      // quad_perm 1, 0, 3, 2
+  const int k = static_cast<int>(v);
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(k, k, 0x4E, 0xF, 0xF, false)));   // quad_perm 2, 3, 0, 1
+}
+
+// Eight values to codes (value i in nibble i); scale: the byte that the four lanes of a group share.
+template <typename T>
+__device__ __forceinline__ uint32_t quantise8(const float (&v)[8], uint32_t& scale) {
+  // the group's largest magnitude as an integer, so that a NaN is the largest
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  top = largest_of_four(top);
+  if (top >= 0x7F800000u) {
+    scale = kScaleNaN;
+    uint32_t signs = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) signs |= (__float_as_uint(v[i]) >> 31) << (4 * i + 3);
+    return signs;
+  }
+  // exponent of the largest less 2, one more where its mantissa exceeds 1.75: nothing is then further off than half a step
+  constexpr bool kBf = __is_same(T, BF16);
+  int e = static_cast<int>((top + 0x1FFFFFu) >> 23) - 127 - 2;
+  e = min(max(e, kBf ? -100 : -23), kBf ? 125 : 13);
+  scale = static_cast<uint32_t>(e + 127);
+  // a division by a power of two and a rounding to the nearest code, ties to the even one, more than 6 to 6: one instruction a pair
+  const float unit = scale_of(scale);
+  uint32_t codes = 0;
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[0], v[1], unit, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[2], v[3], unit, 1);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[4], v[5], unit, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[6], v[7], unit, 3);
+}
+
+// A lane takes 8 neighbouring values of HPL heads of a token, four neighbouring lanes a group of 32 with one scale; the cosines and
+// sines of its frequencies serve all its heads.  A workgroup takes TW tokens that share a tile of 16 places, so that a tile's
+// bytes are written from one place, or one token (TW = 1).  Bound by the rows in and out (prompts) or by latency (a decode step).
+template <typename T, int D, int TW, int HPL>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   constexpr int LP = D / 8;                                   // lanes of a head
-  const int s = blockIdx.y;
-  const int item = (blockIdx.x * 256 + threadIdx.x) / LP;
+  constexpr int HS = 256 / LP / TW;                           // heads at a time
   const int c = threadIdx.x % LP;                             // values [8 c, 8 c + 8)
+  const int hs = threadIdx.x / LP % HS, tok = threadIdx.x / LP / HS;
   const int H = a.C.n_kv_heads, heads = a.n_heads + 2 * H;
-  const int j = item / heads, head = item - j * heads;
-  const Sequence q = sequence(a.C, a.b, s);
+  const Sequence q = sequence(a.C, a.b, blockIdx.y);
+  const int base = q.len - q.n_new;
+  // j: the token among the sequence's new ones
+  const int j = TW == 1 ? static_cast<int>(blockIdx.z) : static_cast<int>(blockIdx.z) * TW + tok - (base & (TW - 1));
   const int row = q.row0 + j;
-  if (!q.real || j >= q.n_new || j >= a.b.max_new || row < 0 || row >= a.b.n_rows) return;
-  const int place = q.len - q.n_new + j;
+  if (!q.real || j < 0 || j >= q.n_new || j >= a.b.max_new || row < 0 || row >= a.b.n_rows) return;
+  const int place = base + j;
 
-  const uint16_t* x = a.qkv + static_cast<size_t>(row) * a.ld_qkv + static_cast<size_t>(head) * D;
-  float v[8];
-  unpack8<T>(*reinterpret_cast<const uint4*>(x + 8 * c), v);
+  const uint16_t* x = a.qkv + static_cast<size_t>(row) * a.ld_qkv;
   const int half = a.r.rot_dim / 2;
-  if (a.r.table && head < a.n_heads + H && 8 * c < a.r.rot_dim) {
-    // products and sums rounded one by one, so that k is quantised from values that any fp32 program gets
-#pragma clang fp contract(off)
-    float w[8];                                               // the partners
-    const bool upper = !a.r.interleaved && 8 * c >= half;
-    if (!a.r.interleaved) unpack8<T>(*reinterpret_cast<const uint4*>(x + 8 * c + (upper ? -half : half)), w);
-    float y[8];
+  const bool turned = a.r.table && 8 * c < a.r.rot_dim;
+  const int partner = a.r.interleaved ? 0 : (8 * c >= half ? -half : half);
+  uint4 raw[HPL], other[HPL];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int f = a.r.interleaved ? 4 * c + i / 2 : 8 * c + i - (upper ? half : 0);
-      int p = place;
-      if (a.r.positions) {
-        int axis = 0;
-        for (int end = a.r.axis_pairs[0]; axis + 1 < a.r.n_axes && f >= end; end += a.r.axis_pairs[axis]) ++axis;
-        p = a.r.positions[static_cast<size_t>(axis) * a.b.n_rows + row];
-      }
-      float cs = __uint_as_float(0x7FC00000u), sn = cs;
-      if (p >= 0 && p < a.r.n_positions) {
-        const float* t = a.r.table + static_cast<size_t>(p) * a.r.rot_dim + f;
-        cs = t[0];
-        sn = t[half];
-      }
-      const float other = a.r.interleaved ? v[i ^ 1] : w[i];
-      const bool second = a.r.interleaved ? (i & 1) : upper;
-      const float p0 = v[i] * cs, p1 = other * sn;
-      y[i] = second ? p0 + p1 : p0 - p1;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = y[i];
+  for (int k = 0; k < HPL; ++k) {
+    const int head = (blockIdx.x * HPL + k) * HS + hs;
+    if (head < heads) raw[k] = *reinterpret_cast<const uint4*>(x + static_cast<size_t>(head) * D + 8 * c);
+    if (turned && !a.r.interleaved && head < a.n_heads + H)
+      other[k] = *reinterpret_cast<const uint4*>(x + static_cast<size_t>(head) * D + 8 * c + partner);
   }
-
-  if (head >= a.n_heads) {
-    // the group's largest magnitude as an integer, so that a NaN is the largest
-    uint32_t top = 0;
+  float cs[8], sn[8];
+  if (turned) turn_of<D>(a, c, row, place, cs, sn);
+  const int page = place >= 0 ? page_of(a.C, q.slot, place / a.C.page_tokens) : -1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
-    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
-    // exponent of the largest less 2, one more where its mantissa exceeds 1.75: nothing is then further off than half a step
-    constexpr bool kBf = sizeof(T) && __is_same(T, BF16);
-    int e = static_cast<int>((top + 0x1FFFFFu) >> 23) - 127 - 2;
-    e = min(max(e, kBf ? -100 : -23), kBf ? 125 : 13);
-    const bool whole = top < 0x7F800000u;
-    const float unit = __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
-    const uint32_t scale = whole ? static_cast<uint32_t>(e + 127) : kScaleNaN;
-    uint32_t codes = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // the borders between neighbouring codes are exact multiples of the unit
-      const float m = fabsf(v[i]);
-      uint32_t code = 0;
-      if (whole)
-        code = (m > 0.25f * unit) + (m >= 0.75f * unit) + (m > 1.25f * unit) + (m >= 1.75f * unit) + (m > 2.5f * unit) +
-               (m >= 3.5f * unit) + (m > 5.0f * unit);
-      // 0, 1/2, 1, 3/2, 2, 3, 4, 6
-      const float level = code < 4 ? 0.5f * code : (code == 4 ? 2.f : code == 5 ? 3.f : code == 6 ? 4.f : 6.f);
-      const uint32_t sign = __float_as_uint(v[i]) >> 31;
-      codes |= (code | sign << 3) << (4 * i);
-      v[i] = whole ? (sign ? -level : level) * unit : __uint_as_float(0x7FC00000u);
+  for (int k = 0; k < HPL; ++k) {
+    const int head = (blockIdx.x * HPL + k) * HS + hs;
+    if (head >= heads) break;
+    float v[8], w[8];
+    unpack8<T>(raw[k], v);
+    if (turned && head < a.n_heads + H) {
+      if (!a.r.interleaved) unpack8<T>(other[k], w);
+      turn(a.r, c, cs, sn, w, v);
     }
-    const int page = place >= 0 ? page_of(a.C, q.slot, place / a.C.page_tokens) : -1;
-    if (page >= 0) {
-      constexpr int LB = D / 8, W = LB < 16 ? LB : 16;        // a lane's bytes of a tile, and those of one load
-      const int t = place % kBlockTokens, u = t / 16, m = t % 16;
-      const bool is_v = head >= a.n_heads + H;
-      const int kv = head - a.n_heads - (is_v ? H : 0);
-      uint8_t* block = static_cast<uint8_t*>(a.C.data) +
-                       block_at(a.C, a.layer, page, kv, place % a.C.page_tokens / kBlockTokens, D);
-      auto at = [&](int lane, int byte) { return u * 8 * D + byte / W * 64 * W + lane * W + byte % W; };
-      const int g = c / 4;
-      if (!is_v) {
-        const int i0 = 8 * c;
-        *reinterpret_cast<uint32_t*>(block + at(i0 / (D / 4) * 16 + m, i0 % (D / 4) / 2)) = codes;
-        if (c % 4 == 0) block[32 * D + u * (D / 2) + 16 * g + m] = static_cast<uint8_t>(scale);
-      } else {
-        constexpr int PV = D / 16;                            // values of a lane
-        const int kq = m / 4, i = m % 4, i0 = 8 * c;
-        uint8_t* vb = block + 16 * D;
-        if constexpr (PV >= 8) {
-          *reinterpret_cast<uint32_t*>(vb + at(kq * 16 + i0 / PV, i * (D / 32) + i0 % PV / 2)) = codes;
+    uint4 result;
+    if (head < a.n_heads) {
+      result = uint4{Mat<T>::round2(v[0], v[1]), Mat<T>::round2(v[2], v[3]), Mat<T>::round2(v[4], v[5]), Mat<T>::round2(v[6], v[7])};
+    } else {
+      uint32_t scale;
+      const uint32_t codes = quantise8<T>(v, scale);
+      // what the codes stand for is exact in 16 bits
+      const float unit = scale_of(scale);
+      result = uint4{Mat<T>::template pair<0>(codes, unit), Mat<T>::template pair<1>(codes, unit), Mat<T>::template pair<2>(codes, unit),
+                     Mat<T>::template pair<3>(codes, unit)};
+      if (scale == kScaleNaN) {
+        const uint32_t nan2 = Mat<T>::round2(__uint_as_float(0x7FC00000u), __uint_as_float(0x7FC00000u));
+        result = uint4{nan2, nan2, nan2, nan2};
+      }
+      if (page >= 0) {
+        constexpr int LB = D / 8, W = LB < 16 ? LB : 16;      // a lane's bytes of a tile in the attention, and those of one load
+        const int t = place % kBlockTokens, u = t / 16, m = t % 16;
+        const bool is_v = head >= a.n_heads + H;
+        const int kv = head - a.n_heads - (is_v ? H : 0);
+        uint8_t* block = static_cast<uint8_t*>(a.C.data) +
+                         block_at(a.C, a.layer, page, kv, place % a.C.page_tokens / kBlockTokens, D);
+        auto at = [&](int lane, int byte) { return u * 8 * D + byte / W * 64 * W + lane * W + byte % W; };
+        const int g = c / 4;
+        if (!is_v) {
+          const int i0 = 8 * c;
+          *reinterpret_cast<uint32_t*>(block + at(i0 / (D / 4) * 16 + m, i0 % (D / 4) / 2)) = codes;
+          if (c % 4 == 0) block[32 * D + u * (D / 2) + 16 * g + m] = static_cast<uint8_t>(scale);
         } else {
-          *reinterpret_cast<uint16_t*>(vb + at(kq * 16 + i0 / PV, i * (D / 32))) = static_cast<uint16_t>(codes);
-          *reinterpret_cast<uint16_t*>(vb + at(kq * 16 + i0 / PV + 1, i * (D / 32))) = static_cast<uint16_t>(codes >> 16);
+          constexpr int PV = D / 16;                          // values of a lane
+          const int kq = m / 4, i = m % 4, i0 = 8 * c;
+          uint8_t* vb = block + 16 * D;
+          if constexpr (PV >= 8) {
+            *reinterpret_cast<uint32_t*>(vb + at(kq * 16 + i0 / PV, i * (D / 32) + i0 % PV / 2)) = codes;
+          } else {
+            *reinterpret_cast<uint16_t*>(vb + at(kq * 16 + i0 / PV, i * (D / 32))) = static_cast<uint16_t>(codes);
+            *reinterpret_cast<uint16_t*>(vb + at(kq * 16 + i0 / PV + 1, i * (D / 32))) = static_cast<uint16_t>(codes >> 16);
+          }
+          if (c % 4 == 0) block[33 * D + u * (D / 2) + (kq * (D / 32) + g) * 4 + i] = static_cast<uint8_t>(scale);
         }
-        if (c % 4 == 0) block[33 * D + u * (D / 2) + (kq * (D / 32) + g) * 4 + i] = static_cast<uint8_t>(scale);
       }
     }
+    if (a.out) *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(row) * a.ld_out + static_cast<size_t>(head) * D + 8 * c) = result;
   }
-  if (a.out) *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(row) * a.ld_out + static_cast<size_t>(head) * D + 8 * c) = pack8<T>(v);
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
@@ -696,9 +769,16 @@ struct AppendLaunch {
   const Kv4AppendArgs& a;
   hipStream_t s;
   template <typename T, int D> hipError_t operator()() const {
-    const long lanes = static_cast<long>(a.b.max_new) * (a.n_heads + 2 * a.C.n_kv_heads) * (D / 8);
-    const dim3 grid(static_cast<unsigned>((lanes + 255) / 256), static_cast<unsigned>(a.b.n_seq));
-    hipLaunchKernelGGL((kv4_append_kernel<T, D>), grid, dim3(256), 0, s, a);
+    const int heads = a.n_heads + 2 * a.C.n_kv_heads;
+    constexpr int kSlots = 256 / (D / 8), TW = kSlots < 16 ? kSlots : 16, HPL = 4;
+    if (a.b.max_new < TW) {
+      const dim3 grid((heads + kSlots - 1) / kSlots, a.b.n_seq, a.b.max_new);
+      hipLaunchKernelGGL((kv4_append_kernel<T, D, 1, 1>), grid, dim3(256), 0, s, a);
+    } else {
+      constexpr int kHeads = HPL * (kSlots / TW);
+      const dim3 grid((heads + kHeads - 1) / kHeads, a.b.n_seq, (a.b.max_new + TW - 1 + TW - 1) / TW);
+      hipLaunchKernelGGL((kv4_append_kernel<T, D, TW, HPL>), grid, dim3(256), 0, s, a);
+    }
     return hipGetLastError();
   }
 };

@@ -40,7 +40,7 @@ int check_batch(const larosa_kv4_batch* b) {
   if (!b || !b->slots || b->n_seq < 1 || b->n_rows < 1 || b->max_new < 1) return LAROSA_EINVAL;
   if (!aligned(b->slots, 4) || !aligned(b->starts, 4)) return LAROSA_EINVAL;
   if (!b->starts && (b->max_new != 1 || b->n_rows < b->n_seq)) return LAROSA_EINVAL;
-  if (b->n_seq > 65535 || b->max_new > (1 << 20)) return LAROSA_EUNSUPPORTED;
+  if (b->n_seq > 65535 || b->max_new > (1 << 19)) return LAROSA_EUNSUPPORTED;
   return LAROSA_OK;
 }
 
@@ -50,7 +50,7 @@ int check_heads(const larosa_kv4_cache* C, int n_heads) {
 }
 
 int check_rotary(const larosa_rotary* r, const larosa_kv4_cache* C) {
-  if (!r->table || !aligned(r->table, 4) || !aligned(r->positions, 4) || r->n_positions < 1) return LAROSA_EINVAL;
+  if (!r->table || !aligned(r->table, 16) || !aligned(r->positions, 4) || r->n_positions < 1) return LAROSA_EINVAL;
   if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > C->head_dim) return LAROSA_EINVAL;
   if (r->n_axes < 1 || r->n_axes > 4 || (r->n_axes > 1 && !r->positions)) return LAROSA_EINVAL;
   if (r->n_axes > 1) {
@@ -178,7 +178,6 @@ int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_bat
     if (int rc = check_rotary(rotary, C)) return rc;
     if (!out) return LAROSA_EINVAL;
   }
-  if (static_cast<double>(b->max_new) * width / 8 >= 2147483648.0 - 256) return LAROSA_EUNSUPPORTED;
   Kv4AppendArgs a{};
   a.C = *C; a.b = *b; a.layer = layer; a.n_heads = n_heads;
   if (rotary) a.r = *rotary;

@@ -99,7 +99,7 @@ def test_append_refuses(lib):
     assert call(batch(n_seq=70000, n_rows=70000)) == api.EUNSUPPORTED
     for bad in (dict(layer=-1), dict(layer=2), dict(qkv=None), dict(qkv=ODD), dict(out=ODD), dict(ld=1528), dict(ld=1540), dict(ld_out=1528),
                 dict(ld_out=1537), dict(heads=0), dict(heads=7), dict(out=FAKE, ld_out=1544), dict(out=None, r=rotary()),
-                dict(r=rotary(table=None)), dict(r=rotary(n_positions=0)), dict(r=rotary(rot_dim=24)), dict(r=rotary(rot_dim=256)),
+                dict(r=rotary(table=None)), dict(r=rotary(table=0x1008)), dict(r=rotary(n_positions=0)), dict(r=rotary(rot_dim=24)), dict(r=rotary(rot_dim=256)),
                 dict(r=rotary(rot_dim=0)), dict(r=rotary(n_axes=0)), dict(r=rotary(n_axes=5)), dict(r=rotary((32, 32), n_axes=2)),
                 dict(r=rotary((32, 31), n_axes=2, positions=FAKE)), dict(r=rotary((-1, 65), n_axes=2, positions=FAKE)),
                 dict(r=rotary(positions=0x1002))):
