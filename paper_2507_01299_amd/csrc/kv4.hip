@@ -711,14 +711,21 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
       for (int i = 0; i < 4; ++i) o[i] += w * early[e][i];
     }
   }
-#pragma unroll 8
-  for (int k0 = kEarly * GL; k0 < mine; k0 += GL) {           // (uniform over the wave: every lane has its weight to give)
-    const int k = k0 + lane / PL;
-    const float w = __shfl(weight, k & 63);
-    floatx4 v = {0, 0, 0, 0};
-    if (k < mine) v = *reinterpret_cast<const floatx4*>(sums + k * stride + n * D + 4 * c);
+  constexpr int kMore = 8;
+  for (int k0 = kEarly * GL; k0 < mine; k0 += kMore * GL) {   // (uniform over the wave: every lane has its weight to give)
+    floatx4 more[kMore];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += w * v[e];
+    for (int e = 0; e < kMore; ++e) {
+      const int k = k0 + e * GL + lane / PL;
+      more[e] = floatx4{0, 0, 0, 0};
+      if (k < mine) more[e] = *reinterpret_cast<const floatx4*>(sums + k * stride + n * D + 4 * c);
+    }
+#pragma unroll
+    for (int e = 0; e < kMore; ++e) {
+      const float w = __shfl(weight, (k0 + e * GL + lane / PL) & 63);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += w * more[e][i];
+    }
   }
 #pragma unroll
   for (int m = PL; m < 64; m *= 2)

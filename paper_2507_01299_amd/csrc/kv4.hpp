@@ -48,9 +48,11 @@ struct Kv4Scratch {
   int32_t* free_ids;          // [n_pages] grow: pages to hand out; compact: where a page moves to
   int32_t* growing;           // [n_pages] grow: listed slots that would write into a shared page
   int32_t* last;              // [n_pages] grow: the last of them, by its place in the list, from 1
-  int32_t* mark;              // [n_slots] grow: times listed
-  int32_t* offset;            // [n_slots] grow: pages handed out before a slot's
+  int32_t* offset;            // [n_slots] grow: pages handed out before those of a slot of the list
+  int32_t* pair;              // [n_slots] grow: its pair of pages to copy, or -1
+  int32_t* n_live;            // [1] compact: pages in use
 };
+constexpr int kKv4SlotsMax = 1 << 18;         // (a bit each in LDS)
 hipError_t launch_kv4_grow(const larosa_kv4_cache& C, const int32_t* slots, const int32_t* counts, int n, int32_t* status,
                            const Kv4Scratch& x, hipStream_t s);
 hipError_t launch_kv4_fork(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, int n, int32_t* status, hipStream_t s);

@@ -24,7 +24,7 @@ int check_sizes(const larosa_kv4_cache* C) {
   if (C->head_dim != 64 && C->head_dim != 128 && C->head_dim != 256) return LAROSA_EUNSUPPORTED;
   // places in a sequence and numbers of pages are 32-bit
   if (static_cast<long>(C->max_pages) * C->page_tokens >= (1L << 30) || C->n_kv_heads > 4096) return LAROSA_EUNSUPPORTED;
-  if (C->n_pages > (1 << 28) || C->n_slots > (1 << 20) || C->n_layers > 65535) return LAROSA_EUNSUPPORTED;
+  if (C->n_pages > (1 << 28) || C->n_slots > kKv4SlotsMax || C->n_layers > 65535) return LAROSA_EUNSUPPORTED;
   if (static_cast<long>(C->n_slots) * C->max_pages >= (1L << 31)) return LAROSA_EUNSUPPORTED;   // (counts of pages are 32-bit)
   return LAROSA_OK;
 }
@@ -112,7 +112,7 @@ AttentionPlan plan_attention(const larosa_kv4_cache* C, const larosa_kv4_batch* 
 }
 
 size_t scratch_bytes(const larosa_kv4_cache* C) {
-  return 256 + 5 * round_up(static_cast<size_t>(C->n_pages) * 4, 256) + 2 * round_up(static_cast<size_t>(C->n_slots) * 4, 256);
+  return 512 + 5 * round_up(static_cast<size_t>(C->n_pages) * 4, 256) + 2 * round_up(static_cast<size_t>(C->n_slots) * 4, 256);
 }
 
 Kv4Scratch scratch_of(const larosa_kv4_cache* C, void* ws) {
@@ -129,8 +129,9 @@ Kv4Scratch scratch_of(const larosa_kv4_cache* C, void* ws) {
   x.free_ids = take(C->n_pages);
   x.growing = take(C->n_pages);
   x.last = take(C->n_pages);
-  x.mark = take(C->n_slots);
   x.offset = take(C->n_slots);
+  x.pair = take(C->n_slots);
+  x.n_live = take(1);
   return x;
 }
 

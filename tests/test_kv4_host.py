@@ -44,7 +44,7 @@ def rotary(axis_pairs=(), **kw):
 BAD_CACHES = [dict(n_layers=0), dict(n_pages=0), dict(n_slots=0), dict(max_pages=0), dict(n_kv_heads=0), dict(page_tokens=16),
               dict(page_tokens=48), dict(page_tokens=512), dict(dtype=2), dict(dtype=-1)]
 UNSUPPORTED_CACHES = [dict(head_dim=32), dict(head_dim=96), dict(head_dim=512), dict(max_pages=1 << 25), dict(n_pages=1 << 29),
-                      dict(n_slots=1 << 21), dict(n_slots=1 << 20, max_pages=1 << 12), dict(n_layers=1 << 16), dict(n_kv_heads=5000)]
+                      dict(n_slots=(1 << 18) + 1), dict(n_slots=1 << 18, max_pages=1 << 14), dict(n_layers=1 << 16), dict(n_kv_heads=5000)]
 BAD_POINTERS = [dict(data=None), dict(refs=None), dict(table=None), dict(length=None), dict(data=0x1008), dict(table=0x1002)]
 
 
