@@ -351,9 +351,8 @@ __device__ __forceinline__ void load_values(Block<D>& x, const uint8_t* block, i
     x.vs[u] = *reinterpret_cast<const uint32_t*>(block + 33 * D + u * (D / 2) + ((lane >> 4) * (D / 32) + (lane & 15) * (D / 32) / 16) * 4);
 }
 
-// What a lane knows of its row, and its tile of the others.
+// What the rows of a tile see together.
 struct Seen {
-  int from, to;               // the row sees tokens [from, to)
   int lo, hi;                 // no row of the tile sees a token outside
   int all_from, all_to;       // every row of the tile sees all in between
 };
@@ -363,17 +362,20 @@ struct Seen {
 // lanes and the rescaling of the accumulators.
 constexpr float kSlack = 8.f;
 
-// The running state of a lane: row lane mod 16, values [kq D/4, (kq + 1) D/4) of its output in o[k][i] = value i D/16 + k.
-template <int D> struct Running {
+// One of a lane's rows: lane mod 16 of 16 rows, values [kq D/4, (kq + 1) D/4) of its query and of its output, the latter in
+// o[k][i] = value i D/16 + k.
+template <int D> struct Row {
+  u32x4_t q[D / 32];
+  int from, to;               // the row sees tokens [from, to)
   floatx4 o[D / 16];
-  float ref, total;           // total: the lane's own tokens
+  float ref, total;           // total: of the lane's own tokens
 };
 
-// One block of tokens t0 .. t0 + 31, in x.  As soon as x's keys are used up those of the block at `next` (null: none) are on
-// their way into the same registers, and so are the values.
-template <typename T, int D, bool ONCE>
-__device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, const uint8_t* next, int t0, const u32x4_t (&qf)[D / 32], const Seen& see,
-                                             float scale_log2, int lane, Running<D>& r) {
+// One block of tokens t0 .. t0 + 31, in x, for NT times 16 rows: the codes are converted once for all of them.  As soon as x's
+// keys are used up those of the block at `next` (null: none) are on their way into the same registers, and so are the values.
+template <typename T, int D, int NT, bool ONCE>
+__device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, const uint8_t* next, int t0, const Seen& see,
+                                             float scale_log2, int lane, Row<D> (&rows)[NT]) {
   constexpr int DW = D / 32, NG = D / 32;
   const int kq = lane >> 4;
   const bool cut = t0 < see.all_from || t0 + kBlockTokens > see.all_to;       // some row does not see some token
@@ -382,30 +384,39 @@ __device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, 
   for (int h = 0; h < Block<D>::KG; ++h) odd |= (x.kb[0][h] == kScaleNaN) | (x.kb[1][h] == kScaleNaN);
   const bool nan_groups = __any(odd != 0);
 
-  float p[8];
+  float p[NT][8];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    floatx4 sc = {0, 0, 0, 0};
+    floatx4 sc[NT];
+#pragma unroll
+    for (int z = 0; z < NT; ++z) sc[z] = floatx4{0, 0, 0, 0};
 #pragma unroll
     for (int k = 0; k < DW; ++k) {
       const float f = scale_of(x.kb[u][k / 4]);
       const u32x4_t kv = {Mat<T>::template pair<0>(x.kc[u][k], f), Mat<T>::template pair<1>(x.kc[u][k], f),
                           Mat<T>::template pair<2>(x.kc[u][k], f), Mat<T>::template pair<3>(x.kc[u][k], f)};
-      sc = Mat<T>::mfma(kv, qf[k], sc);
+#pragma unroll
+      for (int z = 0; z < NT; ++z) sc[z] = Mat<T>::mfma(kv, rows[z].q[k], sc[z]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[4 * u + i] = sc[i] * scale_log2;
+    for (int z = 0; z < NT; ++z)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[z][4 * u + i] = sc[z][i] * scale_log2;
   }
   if (next) load_keys<D, ONCE>(x, next, lane);
-  uint64_t nan_v = 0;                                         // groups with a NaN value that this lane's row sees
+  uint32_t nan_v[NT] = {};                                    // groups with a NaN value that the lane's row sees
   if (nan_groups || cut) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int t = t0 + 16 * (i / 4) + 4 * kq + i % 4;
+      bool nan_k = false;
       if (nan_groups)
-        for (int g = 0; g < NG; ++g)
-          if (block[32 * D + i / 4 * (D / 2) + 16 * g + 4 * kq + i % 4] == kScaleNaN) p[i] = __uint_as_float(0x7FC00000u);
-      if (t < see.from || t >= see.to) p[i] = -INFINITY;
+        for (int g = 0; g < NG; ++g) nan_k |= block[32 * D + i / 4 * (D / 2) + 16 * g + 4 * kq + i % 4] == kScaleNaN;
+#pragma unroll
+      for (int z = 0; z < NT; ++z) {
+        if (nan_k) p[z][i] = __uint_as_float(0x7FC00000u);
+        if (t < rows[z].from || t >= rows[z].to) p[z][i] = -INFINITY;
+      }
       // what no row of the tile sees may hold anything: its values count as zeros
       if (t < see.lo || t >= see.hi) x.vs[i / 4] &= ~(0xFFu << (8 * (i % 4)));
     }
@@ -413,34 +424,42 @@ __device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, 
       for (int t = 0; t < kBlockTokens; ++t)
         for (int g = 0; g < NG; ++g) {
           const uint8_t sb = block[33 * D + t / 16 * (D / 2) + (t % 16 / 4 * NG + g) * 4 + t % 4];
-          if (sb == kScaleNaN && t0 + t >= see.from && t0 + t < see.to) nan_v |= 1ull << g;
+#pragma unroll
+          for (int z = 0; z < NT; ++z)
+            if (sb == kScaleNaN && t0 + t >= rows[z].from && t0 + t < rows[z].to) nan_v[z] |= 1u << g;
         }
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if ((x.vs[i / 4] >> (8 * (i % 4)) & 0xFFu) == kScaleNaN) x.vs[i / 4] &= ~(0xFFu << (8 * (i % 4)));
     }
   }
-  float m = p[0];
+  u32x4_t pf[NT];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) m = fmaxf(m, p[i]);
-  if (__any(m > r.ref + kSlack)) {                            // (nothing seen yet: ref is -inf)
-    const float now = fmaxf(r.ref, over_quarters_max(m));
-    const float back = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.ref - now);
-    r.ref = now;
-    r.total *= back;
+  for (int z = 0; z < NT; ++z) {
+    Row<D>& r = rows[z];
+    float m = p[z][0];
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k)
+    for (int i = 1; i < 8; ++i) m = fmaxf(m, p[z][i]);
+    if (__any(m > r.ref + kSlack)) {                          // (nothing seen yet: ref is -inf)
+      const float now = fmaxf(r.ref, over_quarters_max(m));
+      const float back = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.ref - now);
+      r.ref = now;
+      r.total *= back;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r.o[k][i] *= back;
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.o[k][i] *= back;
+    }
+    const float ref = r.ref == -INFINITY ? 0.f : r.ref;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[z][i] = __builtin_amdgcn_exp2f(p[z][i] - ref);
+      r.total += p[z][i];
+    }
+    // weights to 16 bits: half a step of 2^-8 (bf16) or 2^-11 (f16) relative on each, independent over the tokens
+    pf[z] = u32x4_t{Mat<T>::round2(p[z][0], p[z][1]), Mat<T>::round2(p[z][2], p[z][3]), Mat<T>::round2(p[z][4], p[z][5]),
+                    Mat<T>::round2(p[z][6], p[z][7])};
   }
-  const float ref = r.ref == -INFINITY ? 0.f : r.ref;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
-    r.total += p[i];
-  }
-  // weights to 16 bits: half a step of 2^-8 (bf16) or 2^-11 (f16) relative on each, independent over the tokens
-  const u32x4_t pf = {Mat<T>::round2(p[0], p[1]), Mat<T>::round2(p[2], p[3]), Mat<T>::round2(p[4], p[5]), Mat<T>::round2(p[6], p[7])};
   float vf[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) vf[i] = scale_of(x.vs[i / 4] >> (8 * (i % 4)) & 0xFFu);
@@ -457,17 +476,22 @@ __device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, 
       even[h] = __builtin_amdgcn_perm(y[2 * h + 1], y[2 * h], 0x05040100u);
       odd2[h] = __builtin_amdgcn_perm(y[2 * h + 1], y[2 * h], 0x07060302u);
     }
-    r.o[2 * J] = Mat<T>::mfma(even, pf, r.o[2 * J]);
-    r.o[2 * J + 1] = Mat<T>::mfma(odd2, pf, r.o[2 * J + 1]);
+#pragma unroll
+    for (int z = 0; z < NT; ++z) {
+      rows[z].o[2 * J] = Mat<T>::mfma(even, pf[z], rows[z].o[2 * J]);
+      rows[z].o[2 * J + 1] = Mat<T>::mfma(odd2, pf[z], rows[z].o[2 * J + 1]);
+    }
   });
   if (next) load_values<D, ONCE>(x, next, lane);
-  if (nan_v) {
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k)
+  for (int z = 0; z < NT; ++z)
+    if (nan_v[z]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (nan_v >> (((4 * kq + i) * (D / 16) + k) / 32) & 1) r.o[k][i] = __uint_as_float(0x7FC00000u);
-  }
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (nan_v[z] >> (((4 * kq + i) * (D / 16) + k) / 32) & 1) rows[z].o[k][i] = __uint_as_float(0x7FC00000u);
+    }
 }
 
 constexpr int kWaves = 4;
@@ -478,7 +502,7 @@ template <int D> struct JoinShared {
 
 // The workgroup's waves into wave 0 (every lane calls; only wave 0's r is then of use).  total is a row's on entry and on return.
 template <int D>
-__device__ __forceinline__ void join_waves(Running<D>& r, JoinShared<D>& sh, int lane, int wave) {
+__device__ __forceinline__ void join_waves(Row<D>& r, JoinShared<D>& sh, int lane, int wave) {
   const int n = lane & 15, kq = lane >> 4;
   if (kq == 0) {
     sh.ref[wave][n] = r.ref;
@@ -514,16 +538,16 @@ __device__ __forceinline__ void join_waves(Running<D>& r, JoinShared<D>& sh, int
   }
 }
 
-// A tile of 16 rows (new token, query head of the group) of one key/value head of one sequence, and its splits.
+// A tile of rows (new token, query head of the group) of one key/value head of one sequence, and its splits.
 struct Tile {
   int base;                   // place of the sequence's first new token
-  Seen see;                   // from and to are a row's own
+  Seen see;
   int b_lo, b_hi, splits;     // blocks that some row sees, and the workgroups they are divided among (1 where there are none)
 };
-__device__ __forceinline__ Tile find_tile(const Kv4AttentionArgs& a, const Sequence& sq, int news, int tile) {
+__device__ __forceinline__ Tile find_tile(const Kv4AttentionArgs& a, const Sequence& sq, int news, int tile, int tile_rows) {
   Tile t;
   t.base = sq.len - sq.n_new;
-  const int first_j = tile * 16 / a.group, last_j = min(news - 1, (tile * 16 + 15) / a.group);
+  const int first_j = tile * tile_rows / a.group, last_j = min(news - 1, (tile * tile_rows + tile_rows - 1) / a.group);
   t.see.hi = max(0, min(sq.len, t.base + last_j + 1));
   t.see.lo = a.window > 0 ? max(0, t.base + first_j + 1 - a.window) : 0;
   t.see.all_to = t.base + first_j + 1;
@@ -540,65 +564,82 @@ __device__ __forceinline__ float* split_sums(const Kv4AttentionArgs& a, int s, i
   return a.partial + (unit * a.splits + split) * (static_cast<size_t>(a.partial_rows) * (D + 2));
 }
 
-// One workgroup: a tile of 16 rows and one split of the tokens that they see; its four waves take every fourth block of 32 tokens
+// Waves of each SIMD that the registers are shared out for.
+constexpr int attention_waves(int D, int NT) { return D == 64 ? (NT == 1 ? 4 : 3) : D == 128 ? (NT == 1 ? 3 : 2) : 2; }
+
+// One workgroup: a tile of 16 NT rows and one split of the tokens that they see; its four waves take every fourth block of 32 tokens
 // each.  Where a tile has several splits, each leaves its sums for kv4_combine_kernel.  Bound by HBM where there is work for all
 // compute units (about 230 vector instructions for a block of 4352 bytes at head_dim 128: 1000 cycles of a SIMD, and 2300 at the rate
 // of a large copy); a short call is a chain of loads: slot, length and page, keys, output.
-template <typename T, int D, bool ONCE>
-__global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_attention_kernel(Kv4AttentionArgs a) {
+template <typename T, int D, int NT, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_attention_kernel(Kv4AttentionArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, kq = lane >> 4;
   const int head = blockIdx.x % a.C.n_kv_heads;
   const int tile = blockIdx.x / a.C.n_kv_heads;
   const int split = blockIdx.z;
+  // Until the first keys are asked for, time goes into loads that wait for one another.  So what depends on the slot (length, pages) and the
+  // queries are asked for before any of them is looked at, from addresses that are made valid instead of branches.
   Sequence sq = sequence_rows(a.C, a.b, blockIdx.y);
   const int news = min(sq.n_new, a.b.max_new);
-  if (tile * 16 >= news * a.group) return;
-  // this lane's row
-  const int r = tile * 16 + n;
-  const int j = r / a.group, hq = head * a.group + r % a.group;
-  const int row = sq.row0 + j;
-  const bool has_row = j < news && row >= 0 && row < a.b.n_rows;
-  u32x4_t qf[D / 32];
-#pragma unroll
-  for (int k = 0; k < D / 32; ++k) {
-    qf[k] = u32x4_t{0, 0, 0, 0};
-    if (has_row)
-      qf[k] = *reinterpret_cast<const u32x4_t*>(a.q + static_cast<size_t>(row) * a.ld_q + static_cast<size_t>(hq) * D + kq * (D / 4) + 8 * k);
-  }
+  if (tile * 16 * NT >= news * a.group) return;
+  const int slot = sq.real ? sq.slot : 0;
+  const int length = a.C.length[slot];
   // 64 blocks' pages at a time, one to a lane; without a window the first of them do not have to wait for the length
   const int page_shift = __builtin_ctz(a.C.page_tokens / kBlockTokens);
-  auto pages_from = [&](int c0) { return sq.real ? page_of(a.C, sq.slot, (c0 + lane * kWaves) >> page_shift) : -1; };
-  int my_page = -1;
+  const int32_t* table = a.C.table + static_cast<size_t>(slot) * a.C.max_pages;
+  auto pages_from = [&](int c0) { return table[min((c0 + lane * kWaves) >> page_shift, a.C.max_pages - 1)]; };
+  int my_page = 0;
   if (a.window == 0) my_page = pages_from(split * a.chunk + wave);
-  if (sq.real) sq.len = a.C.length[sq.slot];
-  Tile t = find_tile(a, sq, news, tile);
+  // this lane's rows: the z-th is row 16 z + n of the tile
+  Row<D> rows[NT];
+  int row[NT], hq[NT];        // row of the batch (-1: none) and query head
+#pragma unroll
+  for (int z = 0; z < NT; ++z) {
+    const int r = tile * 16 * NT + 16 * z + n, j = r / a.group;
+    hq[z] = head * a.group + r - j * a.group;
+    row[z] = sq.row0 + j;
+    if (j >= news || row[z] >= a.b.n_rows) row[z] = -1;
+    rows[z].to = j + 1;       // (from the place of the first new token on, until the length is known)
+    const uint16_t* q = a.q + static_cast<size_t>(max(0, row[z])) * a.ld_q + static_cast<size_t>(hq[z]) * D + kq * (D / 4);
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) rows[z].q[k] = *reinterpret_cast<const u32x4_t*>(q + 8 * k);
+  }
+  sq.len = sq.real ? length : 0;
+  const Tile t = find_tile(a, sq, news, tile, 16 * NT);
   if (split >= t.splits) return;
-  Seen& see = t.see;
-  see.to = t.base + j + 1;
-  see.from = a.window > 0 ? max(0, see.to - a.window) : 0;
   // the last split takes whatever is left
   const int b0 = t.b_lo + split * a.chunk, b1 = split == t.splits - 1 ? t.b_hi : b0 + a.chunk;
   if (a.window > 0) my_page = pages_from(b0 + wave);
-
-  Running<D> run;
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) run.o[k] = floatx4{0, 0, 0, 0};
-  run.ref = -INFINITY;
-  run.total = 0.f;
+  for (int z = 0; z < NT; ++z) {
+    if (row[z] < 0)
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) rows[z].q[k] = u32x4_t{0, 0, 0, 0};
+    rows[z].to += t.base;
+    rows[z].from = a.window > 0 ? max(0, rows[z].to - a.window) : 0;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) rows[z].o[k] = floatx4{0, 0, 0, 0};
+    rows[z].ref = -INFINITY;
+    rows[z].total = 0.f;
+  }
 
   for (int c0 = b0 + wave; c0 < b1; c0 += 64 * kWaves) {
     const int mine = min(64, (b1 - c0 + kWaves - 1) / kWaves);
     if (c0 != b0 + wave) my_page = pages_from(c0);
-    auto address = [&](int i) {                               // (a block without a page: any will do, nobody sees it)
-      const int page = max(0, __builtin_amdgcn_readlane(my_page, i));
+    auto page_at = [&](int i) {                               // -1: a block without a page, which nobody sees
+      const int page = __builtin_amdgcn_readlane(my_page, i);
+      return page < a.C.n_pages && (c0 + i * kWaves) >> page_shift < a.C.max_pages ? page : -1;
+    };
+    auto address = [&](int i) {                               // (without a page any will do)
+      const int page = max(0, page_at(i));
       return static_cast<const uint8_t*>(a.C.data) + block_at(a.C, a.layer, page, head, (c0 + i * kWaves) & ((1 << page_shift) - 1), D);
     };
     // two blocks in registers; each is replaced by the one after the next as it is used up
     auto ahead = [&](int i) { return i < mine ? address(i) : nullptr; };
     auto work = [&](Block<D>& x, const uint8_t* block, const uint8_t* next, int i) {
-      const int t0 = __builtin_amdgcn_readlane(my_page, i) >= 0 ? (c0 + i * kWaves) * kBlockTokens : kNowhere;
-      attend_block<T, D, ONCE>(x, block, next, t0, qf, see, a.scale_log2, lane, run);
+      const int t0 = page_at(i) >= 0 ? (c0 + i * kWaves) * kBlockTokens : kNowhere;
+      attend_block<T, D, NT, ONCE>(x, block, next, t0, t.see, a.scale_log2, lane, rows);
     };
     Block<D> x, y;
     const uint8_t *bx = address(0), *by = ahead(1);
@@ -618,41 +659,47 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 4 : D == 128 ? 3 : 2) void k
       by = ny;
     }
   }
-  run.total = over_quarters_sum(run.total);
 
   __shared__ JoinShared<D> sh;
-  join_waves<D>(run, sh, lane, wave);
-  if (t.splits > 1) {
-    if (wave > 0 || n >= a.partial_rows) return;
-    float* sums = split_sums(a, blockIdx.y, blockIdx.x, split, D);
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-      floatx4 v;
+  for (int z = 0; z < NT; ++z) {
+    Row<D>& r = rows[z];
+    r.total = over_quarters_sum(r.total);
+    if (z > 0) __syncthreads();                               // wave 0 has read the rows before
+    join_waves<D>(r, sh, lane, wave);
+    if (wave > 0) continue;
+    if (t.splits > 1) {
+      if (16 * z + n >= a.partial_rows) continue;
+      float* sums = split_sums(a, blockIdx.y, blockIdx.x, split, D);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int d = 4 * c + e;
-        v[e] = run.o[d % (D / 16)][d / (D / 16)];
+      for (int c = 0; c < D / 16; ++c) {
+        floatx4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = 4 * c + e;
+          v[e] = r.o[d % (D / 16)][d / (D / 16)];
+        }
+        *reinterpret_cast<floatx4*>(sums + (16 * z + n) * D + kq * (D / 4) + 4 * c) = v;
       }
-      *reinterpret_cast<floatx4*>(sums + n * D + kq * (D / 4) + 4 * c) = v;
+      if (kq == 0) {
+        sums[a.partial_rows * D + 16 * z + n] = r.ref;
+        sums[a.partial_rows * (D + 1) + 16 * z + n] = r.total;
+      }
+      continue;
     }
-    if (kq == 0) {
-      sums[a.partial_rows * D + n] = run.ref;
-      sums[a.partial_rows * (D + 1) + n] = run.total;
-    }
-    return;
-  }
-  if (wave > 0 || !has_row) return;
-  const float inv = run.total == 0.f ? 0.f : 1.0f / run.total;
-  uint16_t* dst = a.out + static_cast<size_t>(row) * a.ld_out + static_cast<size_t>(hq) * D + kq * (D / 4);
+    if (row[z] < 0) continue;
+    const float inv = r.total == 0.f ? 0.f : 1.0f / r.total;
+    uint16_t* dst = a.out + static_cast<size_t>(row[z]) * a.ld_out + static_cast<size_t>(hq[z]) * D + kq * (D / 4);
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    float v[8];
+    for (int c = 0; c < D / 32; ++c) {
+      float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int d = 8 * c + e;
-      v[e] = run.o[d % (D / 16)][d / (D / 16)] * inv;
+      for (int e = 0; e < 8; ++e) {
+        const int d = 8 * c + e;
+        v[e] = r.o[d % (D / 16)][d / (D / 16)] * inv;
+      }
+      *reinterpret_cast<uint4*>(dst + 8 * c) = pack8<T>(v);
     }
-    *reinterpret_cast<uint4*>(dst + 8 * c) = pack8<T>(v);
   }
 }
 
@@ -686,10 +733,10 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
   }
   const Sequence sq = sequence(a.C, a.b, blockIdx.y);
   const int news = min(sq.n_new, a.b.max_new);
-  if (tile * 16 >= news * a.group) return;                    // (uniform over the workgroup, as is the next)
-  const Tile t = find_tile(a, sq, news, tile);
+  if (tile * a.tile_rows >= news * a.group) return;           // (uniform over the workgroup, as is the next)
+  const Tile t = find_tile(a, sq, news, tile, a.tile_rows);
   if (t.splits == 1) return;
-  const int r = tile * 16 + n, j = r / a.group, row = sq.row0 + j;
+  const int r = tile * a.tile_rows + n, j = r / a.group, row = sq.row0 + j;
   const bool has_row = n < a.partial_rows && j < news && row >= 0 && row < a.b.n_rows;
   const int mine = has_row ? (t.splits - first + WR - 1) / WR : 0;
   if (lane >= mine) {
@@ -795,10 +842,17 @@ struct AttentionLaunch {
   hipStream_t s;
   template <typename T, int D> hipError_t operator()() const {
     const dim3 grid(static_cast<unsigned>(a.row_tiles * a.C.n_kv_heads), static_cast<unsigned>(a.b.n_seq), static_cast<unsigned>(a.splits));
-    if (a.row_tiles == 1)
-      hipLaunchKernelGGL((kv4_attention_kernel<T, D, true>), grid, dim3(64 * kWaves), 0, s, a);
-    else
-      hipLaunchKernelGGL((kv4_attention_kernel<T, D, false>), grid, dim3(64 * kWaves), 0, s, a);
+    const dim3 block(64 * kWaves);
+    if constexpr (D <= 128) {
+      if (a.tile_rows == 32 && a.row_tiles == 1)
+        hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, true>), grid, block, 0, s, a);
+      else if (a.tile_rows == 32)
+        hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, false>), grid, block, 0, s, a);
+    }
+    if (a.tile_rows == 16 && a.row_tiles == 1)
+      hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, true>), grid, block, 0, s, a);
+    else if (a.tile_rows == 16)
+      hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, false>), grid, block, 0, s, a);
     if (a.splits == 1) return hipGetLastError();
     if (hipError_t e = hipGetLastError()) return e;
     const unsigned rows = static_cast<unsigned>(a.partial_rows);

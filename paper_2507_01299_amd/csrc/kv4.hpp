@@ -30,7 +30,7 @@ struct Kv4AttentionArgs {
   int ld_out;
   float scale_log2;           // scale * log2(e): the exponentials are powers of two
   int window;                 // 0: none
-  int row_tiles;              // of 16 (new token, query head of the group) pairs
+  int tile_rows, row_tiles;   // 16 or 32 (new token, query head of the group) pairs to a tile, and tiles of a sequence's head
   // the split of the tokens: `chunk` blocks of 32 to a workgroup, up to `splits` workgroups for a tile
   int chunk, splits;
   float* partial;             // [n_seq][row_tiles * n_kv_heads][splits][partial_rows * (head_dim + 2)] fp32

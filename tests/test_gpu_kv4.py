@@ -76,6 +76,60 @@ def test_attention_several_new_tokens(gpu_device, dtype, D, heads, kv, P, window
     check_attention(C, slots, starts, q, heads, window=window, max_new=9, layer=1, ld_extra=8)
 
 
+WIDE = 256000         # tokens that the page tables have room for: enough work by the plan for tiles of 32 rows and 250 splits
+
+
+@pytest.mark.parametrize("dtype,D,heads,kv,window", [("f16", 128, 12, 4, 0), ("bf16", 64, 32, 2, 0), ("bf16", 128, 8, 2, 37),
+                                                     ("f16", 64, 20, 4, 300)])
+def test_attention_tiles_of_32_rows(gpu_device, dtype, D, heads, kv, window):
+    rng = np.random.default_rng(D + heads + window)
+    lengths, news = [170, 9, 1100, 40, 0], [41, 9, 33, 17, 6]
+    C, slots = U.random_cache(rng, lengths, 256, kv, D, dtype, headroom=WIDE)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    q = U.random_rows(rng, int(starts[-1]) + 1, heads * D, dtype)
+    wide = check_attention(C, slots, starts, q, heads, window=window, max_new=41)
+    C.block(0, slots[0], 160, 0)[K.scale_place(D, 160 % 32, 1, 1)] = K.NAN_SCALE         # tokens 160 (V) and 165 (K) of the first
+    C.block(0, slots[0], 165, 0)[K.scale_place(D, 165 % 32, 0, 0)] = K.NAN_SCALE
+    got = check_attention(C, slots, starts, q, heads, window=window, max_new=41)
+    assert np.array_equal(got[41:], wide[41:]) and np.array_equal(got[:31], wide[:31]) and np.isnan(got[31:41]).any((1, 2)).all()
+
+
+def test_attention_past_4_gib(gpu_device):
+    """Pages whose bytes lie past 32-bit offsets: the same output and the same stored bytes as low ones."""
+    from paper_2507_01299_amd import api
+    rng = np.random.default_rng(17)
+    C, slots = U.random_cache(rng, [500, 300], 256, 8, 128, "bf16")
+    q = U.random_rows(rng, 2, (16 + 16) * 128, "bf16")
+    page = C.data[0, 0].nbytes
+    n_pages = (5 << 30) // page
+    far = np.where(C.table >= 0, n_pages - 1 - C.table, -1)
+    big = api.KvCache(1, n_pages, 256, C.n_slots, C.max_pages, 8, 128, "bf16")
+    big.table.copy_(torch.from_numpy(far))
+    big.length.copy_(torch.from_numpy(C.length))
+    pages = big.data[:n_pages * page].view(n_pages, page)
+    ids = C.table[C.table >= 0]
+    for p in ids:
+        pages[n_pages - 1 - int(p)] = torch.from_numpy(C.data[0, p].reshape(-1)).to("cuda:0")
+    small = U.device_cache(C)
+    outs = []
+    for cache in (small, big):
+        batch = api.KvBatch(U.int32(slots), 2)
+        qkv = U.to_dev(q, "bf16")
+        turned, out = torch.zeros_like(qkv), torch.zeros(2, 16 * 128, dtype=qkv.dtype, device="cuda:0")
+        api.kv4_append(cache, 0, batch, qkv, 16, out=turned)
+        api.kv4_attention(cache, 0, batch, turned, 16, out, api.kv4_attention_workspace(cache, batch, 16))
+        torch.cuda.synchronize()
+        outs.append((turned.view(torch.int16), out.view(torch.int16)))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    low = small.data.view(-1, page)
+    for p in ids:
+        assert torch.equal(low[int(p)], pages[n_pages - 1 - int(p)])
+    # and copied from there
+    api.kv4_copy_pages(big, U.int32([n_pages - 1 - int(ids[0])]), U.int32([n_pages - 1 - C.n_pages]))
+    torch.cuda.synchronize()
+    assert torch.equal(pages[n_pages - 1 - C.n_pages], low[int(ids[0])])
+
+
 def test_attention_prompt(gpu_device):
     """A whole prompt's rows against its own keys: row 0 sees one token."""
     rng = np.random.default_rng(11)
