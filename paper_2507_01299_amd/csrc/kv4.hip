@@ -318,37 +318,52 @@ template <int D> struct Block {
   uint32_t kb[2][KG], vs[2];                                  // scale bytes: of the lane's token; of its four tokens
 };
 
-template <int D> using Piece = uint32_t __attribute__((ext_vector_type(D < 128 ? D / 32 : 4)));
+// A block's bytes as a buffer.  Where there is none (present false) its size is zero: loads are issued all the same and come back
+// with zeros from no memory, so that the compiler, which counts loads under way, never has to wait for younger ones than it needs.
+template <int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t block_buffer(const uint8_t* block, bool present) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(block), 0, present ? 34 * D : 0, 0x00027000);
+}
 
 // The wave's codes of one block: 16 tokens' keys or values in runs of 64 pieces, one of each lane.  ONCE: no other workgroup
 // reads them, so they pass the caches by (64 sequences of up to 16384 tokens: 87.7 -> 79.5 us, 4.7 TB/s).
 template <int D, bool ONCE>
-__device__ __forceinline__ void load_codes(uint32_t (&c)[2][D / 32], const uint8_t* codes, int lane) {
-  constexpr int LW = sizeof(Piece<D>) / 4;
+__device__ __forceinline__ void load_codes(uint32_t (&c)[2][D / 32], __amdgpu_buffer_rsrc_t block, int at, int lane) {
+  constexpr int LW = D < 128 ? D / 32 : 4, kPolicy = ONCE ? 2 : 0;     // 2: nt
+  static_assert(LW == 2 || LW == 4, "8 or 16 bytes to a load");
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int p = 0; p < D / 32 / LW; ++p) {
-      const Piece<D>* at = reinterpret_cast<const Piece<D>*>(codes + u * 8 * D + (p * 64 + lane) * LW * 4);
-const Piece<D> v = ONCE ? __builtin_nontemporal_load(at) : *at;
+      const int offset = at + u * 8 * D + p * 64 * LW * 4;
+      if constexpr (LW == 4) {
+        const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(block, lane * 16, offset, kPolicy);
 #pragma unroll
-      for (int i = 0; i < LW; ++i) c[u][p * LW + i] = v[i];
+        for (int i = 0; i < 4; ++i) c[u][4 * p + i] = v[i];
+      } else {
+        typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+        const u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(block, lane * 8, offset, kPolicy);
+        c[u][0] = v[0];
+        c[u][1] = v[1];
+      }
     }
 }
 template <int D, bool ONCE>
-__device__ __forceinline__ void load_keys(Block<D>& x, const uint8_t* block, int lane) {
-  load_codes<D, ONCE>(x.kc, block, lane);
+__device__ __forceinline__ void load_keys(Block<D>& x, __amdgpu_buffer_rsrc_t block, int lane) {
+  load_codes<D, ONCE>(x.kc, block, 0, lane);
+  const int mine = (lane >> 4) * (D / 32) / 4 * 16 + (lane & 15);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int h = 0; h < Block<D>::KG; ++h) x.kb[u][h] = block[32 * D + u * (D / 2) + 16 * ((lane >> 4) * (D / 32) / 4 + h) + (lane & 15)];
+    for (int h = 0; h < Block<D>::KG; ++h)
+      x.kb[u][h] = static_cast<uint8_t>(__builtin_amdgcn_raw_buffer_load_b8(block, mine, 32 * D + u * (D / 2) + 16 * h, 0));
 }
 template <int D, bool ONCE>
-__device__ __forceinline__ void load_values(Block<D>& x, const uint8_t* block, int lane) {
-  load_codes<D, ONCE>(x.vc, block + 16 * D, lane);
+__device__ __forceinline__ void load_values(Block<D>& x, __amdgpu_buffer_rsrc_t block, int lane) {
+  load_codes<D, ONCE>(x.vc, block, 16 * D, lane);
+  const int mine = ((lane >> 4) * (D / 32) + (lane & 15) * (D / 32) / 16) * 4;
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
-    x.vs[u] = *reinterpret_cast<const uint32_t*>(block + 33 * D + u * (D / 2) + ((lane >> 4) * (D / 32) + (lane & 15) * (D / 32) / 16) * 4);
+  for (int u = 0; u < 2; ++u) x.vs[u] = __builtin_amdgcn_raw_buffer_load_b32(block, mine, 33 * D + u * (D / 2), 0);
 }
 
 // What the rows of a tile see together.
@@ -372,9 +387,9 @@ template <int D> struct Row {
 };
 
 // One block of tokens t0 .. t0 + 31, in x, for NT times 16 rows: the codes are converted once for all of them.  As soon as x's
-// keys are used up those of the block at `next` (null: none) are on their way into the same registers, and so are the values.
+// keys are used up those of the block `next` are on their way into the same registers, and so are the values.
 template <typename T, int D, int NT, bool ONCE>
-__device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, const uint8_t* next, int t0, const Seen& see,
+__device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, __amdgpu_buffer_rsrc_t next, int t0, const Seen& see,
                                              float scale_log2, int lane, Row<D> (&rows)[NT]) {
   constexpr int DW = D / 32, NG = D / 32;
   const int kq = lane >> 4;
@@ -403,7 +418,7 @@ __device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, 
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[z][4 * u + i] = sc[z][i] * scale_log2;
   }
-  if (next) load_keys<D, ONCE>(x, next, lane);
+  load_keys<D, ONCE>(x, next, lane);
   uint32_t nan_v[NT] = {};                                    // groups with a NaN value that the lane's row sees
   if (nan_groups || cut) {
 #pragma unroll
@@ -482,7 +497,7 @@ __device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, 
       rows[z].o[2 * J + 1] = Mat<T>::mfma(odd2, pf[z], rows[z].o[2 * J + 1]);
     }
   });
-  if (next) load_values<D, ONCE>(x, next, lane);
+  load_values<D, ONCE>(x, next, lane);
 #pragma unroll
   for (int z = 0; z < NT; ++z)
     if (nan_v[z]) {
@@ -636,28 +651,22 @@ __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_atten
       return static_cast<const uint8_t*>(a.C.data) + block_at(a.C, a.layer, page, head, (c0 + i * kWaves) & ((1 << page_shift) - 1), D);
     };
     // two blocks in registers; each is replaced by the one after the next as it is used up
-    auto ahead = [&](int i) { return i < mine ? address(i) : nullptr; };
-    auto work = [&](Block<D>& x, const uint8_t* block, const uint8_t* next, int i) {
+    auto buffer = [&](int i) { return block_buffer<D>(address(min(i, mine - 1)), i < mine); };
+    auto work = [&](Block<D>& x, int i) {
       const int t0 = page_at(i) >= 0 ? (c0 + i * kWaves) * kBlockTokens : kNowhere;
-      attend_block<T, D, NT, ONCE>(x, block, next, t0, t.see, a.scale_log2, lane, rows);
+      attend_block<T, D, NT, ONCE>(x, address(i), buffer(i + 2), t0, t.see, a.scale_log2, lane, rows);
     };
     Block<D> x, y;
-    const uint8_t *bx = address(0), *by = ahead(1);
-    load_keys<D, ONCE>(x, bx, lane);
-    load_values<D, ONCE>(x, bx, lane);
-    if (by) {
-      load_keys<D, ONCE>(y, by, lane);
-      load_values<D, ONCE>(y, by, lane);
+    load_keys<D, ONCE>(x, buffer(0), lane);
+    load_values<D, ONCE>(x, buffer(0), lane);
+    load_keys<D, ONCE>(y, buffer(1), lane);
+    load_values<D, ONCE>(y, buffer(1), lane);
+    int i = 0;                                                // (pairs, and a last one by itself: no way out between the two)
+    for (; i + 1 < mine; i += 2) {
+      work(x, i);
+      work(y, i + 1);
     }
-    for (int i = 0; i < mine; i += 2) {
-      const uint8_t* nx = ahead(i + 2);
-      work(x, bx, nx, i);
-      if (i + 1 >= mine) break;
-      const uint8_t* ny = ahead(i + 3);
-      work(y, by, ny, i + 1);
-      bx = nx;
-      by = ny;
-    }
+    if (i < mine) work(x, i);
   }
 
   __shared__ JoinShared<D> sh;
