@@ -639,6 +639,9 @@ __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_atten
     rows[z].total = 0.f;
   }
 
+  // the head's part of page 0 and the distance to the next page's
+  const unsigned part = (34u * D) << page_shift, page_bytes = part * static_cast<unsigned>(a.C.n_kv_heads);
+  const uint8_t* first_page = static_cast<const uint8_t*>(a.C.data) + static_cast<size_t>(a.layer) * a.C.n_pages * page_bytes + static_cast<size_t>(head) * part;
   for (int c0 = b0 + wave; c0 < b1; c0 += 64 * kWaves) {
     const int mine = min(64, (b1 - c0 + kWaves - 1) / kWaves);
     if (c0 != b0 + wave) my_page = pages_from(c0);
@@ -647,8 +650,8 @@ __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_atten
       return page < a.C.n_pages && (c0 + i * kWaves) >> page_shift < a.C.max_pages ? page : -1;
     };
     auto address = [&](int i) {                               // (without a page any will do)
-      const int page = max(0, page_at(i));
-      return static_cast<const uint8_t*>(a.C.data) + block_at(a.C, a.layer, page, head, (c0 + i * kWaves) & ((1 << page_shift) - 1), D);
+      return first_page + static_cast<size_t>(static_cast<unsigned>(max(0, page_at(i)))) * page_bytes +
+             ((c0 + i * kWaves) & ((1 << page_shift) - 1)) * (34 * D);
     };
     // two blocks in registers; each is replaced by the one after the next as it is used up
     auto buffer = [&](int i) { return block_buffer<D>(address(min(i, mine - 1)), i < mine); };

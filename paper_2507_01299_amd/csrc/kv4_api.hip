@@ -70,12 +70,12 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // one block at a time, and a second launch adds up what several workgroups of a tile left.  That launch takes 4 us and a
 // workgroup 5 us to come to its first block, a block 1 us, so
 //  - up to 24 blocks are one workgroup's (333 tokens of an 8B model: 6.3 us, with two workgroups a tile 8.4);
-//  - one sequence, or few, are cut into as many pieces as are resident at once, three to a compute unit (100003 tokens of a 70B
-//    model: 31 us with 760 pieces, 37 with 784, 38 with 1024), of eight blocks at least;
+//  - one sequence, or few, are cut into two pieces for each compute unit, of eight blocks at least (100003 tokens of a 70B model: 26.6 us;
+//    with three, which are resident at once, 27.1, with 640 or 1024 pieces, which leave compute units idle at the end, 29.3);
 //  - else into pieces of 32 blocks, since lengths differ and a piece past a sequence's end costs nothing (9 sequences of up to
-//    8191 tokens, 7 new each: 23.5 us; pieces of 49 27.0), longer ones past 4096 of them (64 sequences of up to 16384
-//    tokens: 87 us; up to 8192 pieces 96).
-constexpr long kWholeBlocks = 24, kLeastBlocks = 8, kPieceBlocks = 32, kResident = 768, kMostWorkgroups = 4096;
+//    8191 tokens, 7 new each: 22.9 us; pieces of 24 25.5, of 40 24.6, of 64 27.7), longer ones past 4096 of them (64 sequences of up
+//    to 16384 tokens: 75.5 us; past 2048 80.1).
+constexpr long kWholeBlocks = 24, kLeastBlocks = 8, kPieceBlocks = 32, kResident = 512, kMostWorkgroups = 4096;
 struct AttentionPlan {
   int tile_rows;
   long row_tiles, units;      // tiles of a key/value head's rows; such tiles of all sequences
