@@ -134,7 +134,8 @@ typedef struct {
   int attn_mode;              /* 0: context-length-1 attention (softmax over one key = 1, so each query
                                     head outputs the value head of its group); must be 0.  A caller with an
                                     attention core of its own uses larosa_layer_qkv and
-                                    larosa_layer_after_attention instead of larosa_layer_forward. */
+                                    larosa_layer_after_attention instead of larosa_layer_forward, one that
+                                    wants the library's uses larosa_layer_forward_kv4. */
   larosa_dtype dtype;
   /* Residual adapters on the two shortcuts (Sec. 4.2; with block-level rotations, Sec. 5.4, there is
    * one per block), each [d,d] or NULL = identity: the stream that skips the attention block is taken
@@ -292,7 +293,7 @@ typedef struct {
   const int32_t* slots;       /* [n_seq], device; a slot at most once */
   const int32_t* starts;      /* [n_seq + 1], device, or NULL */
   int n_seq, n_rows;
-  int max_new;                /* most new tokens of one sequence; 1 with starts NULL */
+  int max_new;                /* most new tokens of one sequence, up to 2^18; 1 with starts NULL */
 } larosa_kv4_batch;
 
 /* Rotary positions.  Frequency j < rot_dim / 2 turns the pair of values (j, j + rot_dim / 2) of a head, or (2 j, 2 j + 1) if

@@ -418,7 +418,10 @@ class KvBatch:
     row for each sequence), max_new the most of one sequence."""
 
     def __init__(self, slots, n_rows: int, starts=None, max_new: int = 1):
+        if slots.dtype != torch.int32 or (starts is not None and (starts.dtype != torch.int32 or starts.numel() != slots.numel() + 1)):
+            raise ValueError("slots [n_seq] and starts [n_seq + 1] are int32")
         self.tensors = (slots, starts)       # keep alive
+        self.n_rows = n_rows
         self.c = _KvBatch(_ptr(slots), _ptr(starts), slots.numel(), n_rows, max_new)
         self.ref = ctypes.byref(self.c)
 
@@ -430,12 +433,21 @@ class Rotary:
     def __init__(self, table, positions=None, axis_pairs=None, interleaved: bool = False):
         self.tensors = (table, positions)    # keep alive
         n_axes = len(axis_pairs) if axis_pairs else 1
-        if n_axes > 4 or (positions is not None and positions.dim() == 2 and positions.shape[0] != n_axes):
+        if n_axes > 4 or (positions is not None and positions.shape[0] != n_axes):
             raise ValueError("one to four axes, a row of positions and a number of frequencies for each")
+        if table.dtype != torch.float32 or not table.is_contiguous() or (
+                positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous())):
+            raise ValueError("table [n_positions, rot_dim] is contiguous float32, positions [n_axes, n_rows] contiguous int32")
+        self.n_rows = None if positions is None else positions.shape[1]
         self.c = _Rotary(_ptr(table), table.shape[0], table.shape[1], int(interleaved), _ptr(positions), n_axes)
         for k, n in enumerate(axis_pairs or ()):
             self.c.axis_pairs[k] = n
         self.ref = ctypes.byref(self.c)
+
+
+def _check_rows(t, n_rows: int):
+    if t.shape[0] < n_rows or t.stride(1) != 1:
+        raise ValueError(f"a tensor of at least {n_rows} rows, whose values lie next to one another")
 
 
 def kv4_clear(cache: KvCache):
@@ -444,6 +456,11 @@ def kv4_clear(cache: KvCache):
 
 def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, out=None, rotary: Rotary | None = None):
     """The rows' new keys and values into the cache; out (may be qkv) receives q as turned and k, v as stored."""
+    if rotary is not None and rotary.n_rows is not None and rotary.n_rows != batch.n_rows:
+        raise ValueError("positions have a column for every row of the batch")
+    _check_rows(qkv, batch.n_rows)
+    if out is not None:
+        _check_rows(out, batch.n_rows)
     _check(lib().larosa_kv4_append(cache.ref, layer, batch.ref, _ptr(qkv), qkv.stride(0), n_heads,
                                    rotary.ref if rotary is not None else None, _ptr(out),
                                    0 if out is None else out.stride(0), _stream()), "larosa_kv4_append")
@@ -463,6 +480,8 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
     1 / sqrt(head_dim)."""
     if scale is None:
         scale = cache.c.head_dim ** -0.5
+    _check_rows(q, batch.n_rows)
+    _check_rows(out, batch.n_rows)
     _check(lib().larosa_kv4_attention(cache.ref, layer, batch.ref, _ptr(q), q.stride(0), n_heads, scale,
                                       window, max_len, _ptr(out), out.stride(0), ws.ptr, ws.nbytes, _stream()),
            "larosa_kv4_attention")
@@ -513,6 +532,10 @@ def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: i
 def layer_forward_kv4(layer: Layer, cache: KvCache, index: int, batch: KvBatch, x, x_out, ws: Workspace, rotary: Rotary | None = None,
                       scale: float | None = None, window: int = 0, max_len: int = 0, trace: dict | None = None):
     """A decoder layer whose attention runs over layer `index` of the cache; the rows' tokens are counted in the lengths."""
+    if rotary is not None and rotary.n_rows is not None and rotary.n_rows != batch.n_rows:
+        raise ValueError("positions have a column for every row of the batch")
+    if x.shape[0] != batch.n_rows or x_out.shape[0] != batch.n_rows:
+        raise ValueError("x and x_out have the batch's rows")
     if scale is None:
         scale = cache.c.head_dim ** -0.5
     tr = _trace_struct(trace)

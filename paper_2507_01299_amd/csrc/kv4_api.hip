@@ -40,7 +40,7 @@ int check_batch(const larosa_kv4_batch* b) {
   if (!b || !b->slots || b->n_seq < 1 || b->n_rows < 1 || b->max_new < 1) return LAROSA_EINVAL;
   if (!aligned(b->slots, 4) || !aligned(b->starts, 4)) return LAROSA_EINVAL;
   if (!b->starts && (b->max_new != 1 || b->n_rows < b->n_seq)) return LAROSA_EINVAL;
-  if (b->n_seq > 65535 || b->max_new > (1 << 19)) return LAROSA_EUNSUPPORTED;
+  if (b->n_seq > 65535 || b->max_new > (1 << 18)) return LAROSA_EUNSUPPORTED;      // (sides of a launch)
   return LAROSA_OK;
 }
 
@@ -311,7 +311,10 @@ int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, i
   if (rotary)
     if (int rc = check_rotary(rotary, C)) return rc;
   const size_t need = larosa_layer_kv4_workspace_bytes(L, C, b, max_len);
-  if (!need) return LAROSA_EINVAL;
+  if (!need) {                // the layer is at fault: its own call says how, before it looks at a workspace
+    const int rc = larosa_layer_qkv(L, x, x_out, x_out, b->n_rows, nullptr, nullptr, 0, stream);
+    return rc == LAROSA_OK || rc == LAROSA_EWORKSPACE ? LAROSA_EINVAL : rc;
+  }
   if (!ws || !aligned(ws, 256) || ws_bytes < need) return LAROSA_EWORKSPACE;
   const size_t head = shared_scratch(L, C, b, max_len), rows = b->n_rows;
   const int d_qkv = L->d_q + 2 * L->d_kv, heads = L->d_q / C->head_dim;

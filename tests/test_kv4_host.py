@@ -95,7 +95,7 @@ def test_append_refuses(lib):
 
     for bad in BAD_BATCHES:
         assert call(batch(**bad)) == api.EINVAL, bad
-    assert call(batch(starts=FAKE, max_new=1 << 21)) == api.EUNSUPPORTED
+    assert call(batch(starts=FAKE, max_new=(1 << 18) + 1)) == api.EUNSUPPORTED
     assert call(batch(n_seq=70000, n_rows=70000)) == api.EUNSUPPORTED
     for bad in (dict(layer=-1), dict(layer=2), dict(qkv=None), dict(qkv=ODD), dict(out=ODD), dict(ld=1528), dict(ld=1540), dict(ld_out=1528),
                 dict(ld_out=1537), dict(heads=0), dict(heads=7), dict(out=FAKE, ld_out=1544), dict(out=None, r=rotary()),
@@ -167,6 +167,7 @@ def test_layer_with_cache_refuses(lib):
         assert call(**bad) == api.EINVAL, bad
     for bad in (dict(ws=None), dict(ws=0x1010), dict(n=need - 1)):
         assert call(**bad) == api.EWORKSPACE, bad
+    assert call(L=layer(attn_mode=1)) == api.EUNSUPPORTED
 
 
 def test_binding_refuses():
@@ -180,3 +181,18 @@ def test_binding_refuses():
             api.KvCache(1, 4, 32, 1, 2, 1, 64, "f16", device="cpu", **kw)
     with pytest.raises(ValueError):
         api.Rotary(torch.zeros(8, 64), positions=torch.zeros(2, 8, dtype=torch.int32), axis_pairs=(8, 8, 16))
+    for bad in (lambda: api.Rotary(torch.zeros(8, 64, dtype=torch.float64)), lambda: api.Rotary(torch.zeros(64, 8).T),
+                lambda: api.Rotary(torch.zeros(8, 64), positions=torch.zeros(1, 8)), lambda: api.KvBatch(z.long(), 4),
+                lambda: api.KvBatch(z, 4, starts=z)):
+        with pytest.raises(ValueError):
+            bad()
+    # shapes that the C call cannot see
+    c = api.KvCache(1, 4, 32, 1, 4, 1, 64, "f16", data=torch.zeros(4 * 32 * 68, dtype=torch.uint8), refs=z, table=z, length=z[:1])
+    b = api.KvBatch(z[:3], 3)
+    few, enough, turned = torch.zeros(2, 256), torch.zeros(3, 256), torch.zeros(256, 3).T
+    rot = api.Rotary(torch.zeros(8, 64), positions=torch.zeros(1, 2, dtype=torch.int32))
+    for call in (lambda: api.kv4_append(c, 0, b, few, 2), lambda: api.kv4_append(c, 0, b, turned, 2), lambda: api.kv4_append(c, 0, b, enough, 2, out=few),
+                 lambda: api.kv4_append(c, 0, b, enough, 2, out=enough, rotary=rot), lambda: api.kv4_attention(c, 0, b, few, 2, enough, None),
+                 lambda: api.kv4_attention(c, 0, b, enough, 2, turned, None), lambda: api.layer_forward_kv4(None, c, 0, b, few, enough, None)):
+        with pytest.raises(ValueError):
+            call()
