@@ -445,9 +445,11 @@ class Rotary:
         self.ref = ctypes.byref(self.c)
 
 
-def _check_rows(t, n_rows: int):
-    if t.shape[0] < n_rows or t.stride(1) != 1:
+def _row_stride(t, n_rows: int) -> int:
+    ld, one = t.stride()
+    if one != 1 or t.shape[0] < n_rows:
         raise ValueError(f"a tensor of at least {n_rows} rows, whose values lie next to one another")
+    return ld
 
 
 def kv4_clear(cache: KvCache):
@@ -458,12 +460,11 @@ def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, ou
     """The rows' new keys and values into the cache; out (may be qkv) receives q as turned and k, v as stored."""
     if rotary is not None and rotary.n_rows is not None and rotary.n_rows != batch.n_rows:
         raise ValueError("positions have a column for every row of the batch")
-    _check_rows(qkv, batch.n_rows)
-    if out is not None:
-        _check_rows(out, batch.n_rows)
-    _check(lib().larosa_kv4_append(cache.ref, layer, batch.ref, _ptr(qkv), qkv.stride(0), n_heads,
-                                   rotary.ref if rotary is not None else None, _ptr(out),
-                                   0 if out is None else out.stride(0), _stream()), "larosa_kv4_append")
+    ld_qkv = _row_stride(qkv, batch.n_rows)
+    ld_out = 0 if out is None else _row_stride(out, batch.n_rows)
+    _check(lib().larosa_kv4_append(cache.ref, layer, batch.ref, _ptr(qkv), ld_qkv, n_heads,
+                                   rotary.ref if rotary is not None else None, _ptr(out), ld_out,
+                                   _stream()), "larosa_kv4_append")
     return out
 
 
@@ -480,10 +481,9 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
     1 / sqrt(head_dim)."""
     if scale is None:
         scale = cache.c.head_dim ** -0.5
-    _check_rows(q, batch.n_rows)
-    _check_rows(out, batch.n_rows)
-    _check(lib().larosa_kv4_attention(cache.ref, layer, batch.ref, _ptr(q), q.stride(0), n_heads, scale,
-                                      window, max_len, _ptr(out), out.stride(0), ws.ptr, ws.nbytes, _stream()),
+    ld_q, ld_out = _row_stride(q, batch.n_rows), _row_stride(out, batch.n_rows)
+    _check(lib().larosa_kv4_attention(cache.ref, layer, batch.ref, _ptr(q), ld_q, n_heads, scale,
+                                      window, max_len, _ptr(out), ld_out, ws.ptr, ws.nbytes, _stream()),
            "larosa_kv4_attention")
     return out
 
