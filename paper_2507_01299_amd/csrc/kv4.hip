@@ -38,8 +38,6 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-__device__ __forceinline__ size_t block_bytes(int D) { return 34u * static_cast<size_t>(D); }
-
 // ---- 16-bit types on the matrix cores -----------------------------------------------------------
 
 template <typename T> struct Mat;
@@ -94,32 +92,22 @@ struct Sequence {
   bool real;                  // the slot exists
 };
 
-// Sequence s of a batch, its length left out: a load that waits for the slot's.
-__device__ __forceinline__ Sequence sequence_rows(const larosa_kv4_cache& C, const larosa_kv4_batch& b, int s) {
+// Sequence s of a batch (Args: of either kernel), its length left out: a load that waits for the slot's.
+template <typename Args>
+__device__ __forceinline__ Sequence sequence_rows(const Args& a, int s) {
   Sequence q;
-  q.row0 = b.starts ? b.starts[s] : s;
-  q.n_new = b.starts ? b.starts[s + 1] - q.row0 : 1;
-  q.slot = b.slots[s];
-  q.real = q.slot >= 0 && q.slot < C.n_slots;
+  q.row0 = a.starts ? a.starts[s] : s;
+  q.n_new = a.starts ? a.starts[s + 1] - q.row0 : 1;
+  q.slot = a.slots[s];
+  q.real = q.slot >= 0 && q.slot < static_cast<int>(a.n_slots);
   q.len = 0;
   return q;
 }
-__device__ __forceinline__ Sequence sequence(const larosa_kv4_cache& C, const larosa_kv4_batch& b, int s) {
-  Sequence q = sequence_rows(C, b, s);
-  if (q.real) q.len = C.length[q.slot];
+template <typename Args>
+__device__ __forceinline__ Sequence sequence(const Args& a, int s) {
+  Sequence q = sequence_rows(a, s);
+  if (q.real) q.len = a.length[q.slot];
   return q;
-}
-
-// Page of token t of a slot, or -1.
-__device__ __forceinline__ int page_of(const larosa_kv4_cache& C, int slot, int page_index) {
-  if (page_index < 0 || page_index >= C.max_pages) return -1;
-  const int p = C.table[static_cast<size_t>(slot) * C.max_pages + page_index];
-  return p >= 0 && p < C.n_pages ? p : -1;
-}
-
-__device__ __forceinline__ size_t block_at(const larosa_kv4_cache& C, int layer, int page, int head, int block_in_page, int D) {
-  const int per_page = C.page_tokens / kBlockTokens;
-  return (((static_cast<size_t>(layer) * C.n_pages + page) * C.n_kv_heads + head) * per_page + block_in_page) * block_bytes(D);
 }
 
 // ---- append -----------------------------------------------------------------------------------------
@@ -127,24 +115,25 @@ __device__ __forceinline__ size_t block_at(const larosa_kv4_cache& C, int layer,
 // Cosines and sines for the eight values [8 c, 8 c + 8) of a head at a row's positions.
 template <int D>
 __device__ __forceinline__ void turn_of(const Kv4AppendArgs& a, int c, int row, int place, float (&cs)[8], float (&sn)[8]) {
-  const larosa_rotary& r = a.r;
+  const Kv4AppendArgs& r = a;
   const int half = r.rot_dim / 2;
   const int f0 = r.interleaved ? 4 * c : (8 * c >= half ? 8 * c - half : 8 * c), nf = r.interleaved ? 4 : 8;
   auto axis_of = [&](int f) {
     int axis = 0;
-    for (int end = r.axis_pairs[0]; axis + 1 < r.n_axes && f >= end; end += r.axis_pairs[axis]) ++axis;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) axis += f >= static_cast<int>(r.axis_ends >> 8 * i & 255);
     return axis;
   };
   const int axis = r.n_axes > 1 ? axis_of(f0) : 0;
   const bool one = r.n_axes == 1 || axis_of(f0 + nf - 1) == axis;
-  auto position = [&](int ax) { return r.positions ? r.positions[static_cast<size_t>(ax) * a.b.n_rows + row] : place; };
+  auto position = [&](int ax) { return r.positions ? r.positions[static_cast<size_t>(ax) * a.n_rows + row] : place; };
 #pragma unroll
   for (int i = 0; i < 8; ++i) cs[i] = sn[i] = __uint_as_float(0x7FC00000u);       // outside the table
   if (one) {
     const int p = position(axis);
     if (p < 0 || p >= r.n_positions) return;
-    const float4* t = reinterpret_cast<const float4*>(r.table + static_cast<size_t>(p) * r.rot_dim + f0);
-    const float4* u = reinterpret_cast<const float4*>(r.table + static_cast<size_t>(p) * r.rot_dim + half + f0);
+    const float4* t = reinterpret_cast<const float4*>(r.turns + static_cast<size_t>(p) * r.rot_dim + f0);
+    const float4* u = reinterpret_cast<const float4*>(r.turns + static_cast<size_t>(p) * r.rot_dim + half + f0);
     const float4 c0 = t[0], s0 = u[0];
     if (r.interleaved) {
       cs[0] = cs[1] = c0.x; cs[2] = cs[3] = c0.y; cs[4] = cs[5] = c0.z; cs[6] = cs[7] = c0.w;
@@ -161,17 +150,17 @@ __device__ __forceinline__ void turn_of(const Kv4AppendArgs& a, int c, int row, 
     const int f = f0 + (r.interleaved ? i / 2 : i);
     const int p = position(axis_of(f));
     if (p < 0 || p >= r.n_positions) continue;
-    cs[i] = r.table[static_cast<size_t>(p) * r.rot_dim + f];
-    sn[i] = r.table[static_cast<size_t>(p) * r.rot_dim + half + f];
+    cs[i] = r.turns[static_cast<size_t>(p) * r.rot_dim + f];
+    sn[i] = r.turns[static_cast<size_t>(p) * r.rot_dim + half + f];
   }
 }
 
 // y = v turned; w: the partners (the other half's values), or v itself where they are neighbours.  Products and sums are rounded one by
 // one, so that k is quantised from values that any fp32 program gets.
-__device__ __forceinline__ void turn(const larosa_rotary& r, int c, const float (&cs)[8], const float (&sn)[8], const float (&w)[8],
+__device__ __forceinline__ void turn(const Kv4AppendArgs& r, int c, const float (&cs)[8], const float (&sn)[8], const float (&w)[8],
                                      float (&v)[8]) {
 #pragma clang fp contract(off)
-  const bool upper = 8 * c >= r.rot_dim / 2;
+  const bool upper = 8 * c >= static_cast<int>(r.rot_dim / 2);
   float y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -229,42 +218,45 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
   constexpr int HS = 256 / LP / TW;                           // heads at a time
   const int c = threadIdx.x % LP;                             // values [8 c, 8 c + 8)
   const int hs = threadIdx.x / LP % HS, tok = threadIdx.x / LP / HS;
-  const int H = a.C.n_kv_heads, heads = a.n_heads + 2 * H;
-  const Sequence q = sequence(a.C, a.b, blockIdx.y);
+  const int H = a.n_kv_heads, n_heads = a.n_heads, heads = n_heads + 2 * H;
+  const Sequence q = sequence(a, blockIdx.y);
   const int base = q.len - q.n_new;
   // j: the token among the sequence's new ones
   const int j = TW == 1 ? static_cast<int>(blockIdx.z) : static_cast<int>(blockIdx.z) * TW + tok - (base & (TW - 1));
   const int row = q.row0 + j;
-  if (!q.real || j < 0 || j >= q.n_new || j >= a.b.max_new || row < 0 || row >= a.b.n_rows) return;
+  if (!q.real || j < 0 || j >= q.n_new || j >= static_cast<int>(a.max_new) || row < 0 || row >= a.n_rows) return;
   const int place = base + j;
 
   const uint16_t* x = a.qkv + static_cast<size_t>(row) * a.ld_qkv;
-  const int half = a.r.rot_dim / 2;
-  const bool turned = a.r.table && 8 * c < a.r.rot_dim;
-  const int partner = a.r.interleaved ? 0 : (8 * c >= half ? -half : half);
+  const int half = a.rot_dim / 2;
+  const bool turned = a.turns && 8 * c < static_cast<int>(a.rot_dim);
+  const int partner = a.interleaved ? 0 : (8 * c >= half ? -half : half);
   uint4 raw[HPL], other[HPL];
 #pragma unroll
   for (int k = 0; k < HPL; ++k) {
     const int head = (blockIdx.x * HPL + k) * HS + hs;
     if (head < heads) raw[k] = *reinterpret_cast<const uint4*>(x + static_cast<size_t>(head) * D + 8 * c);
-    if (turned && !a.r.interleaved && head < a.n_heads + H)
+    if (turned && !a.interleaved && head < n_heads + H)
       other[k] = *reinterpret_cast<const uint4*>(x + static_cast<size_t>(head) * D + 8 * c + partner);
   }
   float cs[8], sn[8];
   if (turned) turn_of<D>(a, c, row, place, cs, sn);
-  const int page = place >= 0 ? page_of(a.C, q.slot, place / a.C.page_tokens) : -1;
+  const int page_index = place >> a.page_shift;               // (of no use for a place below zero)
+  int page = place >= 0 && page_index < a.max_pages ? a.table[static_cast<size_t>(q.slot) * a.max_pages + page_index] : -1;
+  if (page >= a.n_pages) page = -1;
+  const unsigned part = (34u * D / kBlockTokens) << a.page_shift;       // bytes of a head's part of a page
 #pragma unroll
   for (int k = 0; k < HPL; ++k) {
     const int head = (blockIdx.x * HPL + k) * HS + hs;
     if (head >= heads) break;
     float v[8], w[8];
     unpack8<T>(raw[k], v);
-    if (turned && head < a.n_heads + H) {
-      if (!a.r.interleaved) unpack8<T>(other[k], w);
-      turn(a.r, c, cs, sn, w, v);
+    if (turned && head < n_heads + H) {
+      if (!a.interleaved) unpack8<T>(other[k], w);
+      turn(a, c, cs, sn, w, v);
     }
     uint4 result;
-    if (head < a.n_heads) {
+    if (head < n_heads) {
       result = uint4{Mat<T>::round2(v[0], v[1]), Mat<T>::round2(v[2], v[3]), Mat<T>::round2(v[4], v[5]), Mat<T>::round2(v[6], v[7])};
     } else {
       uint32_t scale;
@@ -280,10 +272,10 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4AppendArgs a) {
       if (page >= 0) {
         constexpr int LB = D / 8, W = LB < 16 ? LB : 16;      // a lane's bytes of a tile in the attention, and those of one load
         const int t = place % kBlockTokens, u = t / 16, m = t % 16;
-        const bool is_v = head >= a.n_heads + H;
-        const int kv = head - a.n_heads - (is_v ? H : 0);
-        uint8_t* block = static_cast<uint8_t*>(a.C.data) +
-                         block_at(a.C, a.layer, page, kv, place % a.C.page_tokens / kBlockTokens, D);
+        const bool is_v = head >= n_heads + H;
+        const int kv = head - n_heads - (is_v ? H : 0);
+        uint8_t* block = a.data + (static_cast<size_t>(page) * H + kv) * part +
+                         ((place & ((1 << a.page_shift) - 1)) / kBlockTokens) * (34 * D);
         auto at = [&](int lane, int byte) { return u * 8 * D + byte / W * 64 * W + lane * W + byte % W; };
         const int g = c / 4;
         if (!is_v) {
@@ -569,13 +561,14 @@ __device__ __forceinline__ Tile find_tile(const Kv4AttentionArgs& a, const Seque
   t.see.all_from = a.window > 0 ? t.base + last_j + 1 - a.window : 0;
   t.b_lo = t.see.lo / kBlockTokens;
   t.b_hi = (t.see.hi + kBlockTokens - 1) / kBlockTokens;
-  t.splits = max(1, min(a.splits, (t.b_hi - t.b_lo + a.chunk - 1) / a.chunk));
+  t.splits = max(1, min(static_cast<int>(a.splits), (t.b_hi - t.b_lo + a.chunk - 1) / a.chunk));
   return t;
 }
 
 // Floats of a split's sums: [rows][D], then the rows' references and totals.
 __device__ __forceinline__ float* split_sums(const Kv4AttentionArgs& a, int s, int unit_in_seq, int split, int D) {
-  const size_t unit = static_cast<size_t>(s) * a.row_tiles * a.C.n_kv_heads + unit_in_seq;
+  const unsigned row_tiles = (a.max_new * a.group + a.tile_rows - 1) / a.tile_rows;
+  const size_t unit = static_cast<size_t>(s) * row_tiles * a.n_kv_heads + unit_in_seq;
   return a.partial + (unit * a.splits + split) * (static_cast<size_t>(a.partial_rows) * (D + 2));
 }
 
@@ -590,20 +583,21 @@ template <typename T, int D, int NT, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_attention_kernel(Kv4AttentionArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, kq = lane >> 4;
-  const int head = blockIdx.x % a.C.n_kv_heads;
-  const int tile = blockIdx.x / a.C.n_kv_heads;
+  const int n_kv = a.n_kv_heads;
+  const int head = blockIdx.x % n_kv;
+  const int tile = blockIdx.x / n_kv;
   const int split = blockIdx.z;
   // Until the first keys are asked for, time goes into loads that wait for one another.  So what depends on the slot (length, pages) and the
   // queries are asked for before any of them is looked at, from addresses that are made valid instead of branches.
-  Sequence sq = sequence_rows(a.C, a.b, blockIdx.y);
-  const int news = min(sq.n_new, a.b.max_new);
+  Sequence sq = sequence_rows(a, blockIdx.y);
+  const int news = min(sq.n_new, static_cast<int>(a.max_new));
   if (tile * 16 * NT >= news * a.group) return;
   const int slot = sq.real ? sq.slot : 0;
-  const int length = a.C.length[slot];
+  const int length = a.length[slot];
   // 64 blocks' pages at a time, one to a lane; without a window the first of them do not have to wait for the length
-  const int page_shift = __builtin_ctz(a.C.page_tokens / kBlockTokens);
-  const int32_t* table = a.C.table + static_cast<size_t>(slot) * a.C.max_pages;
-  auto pages_from = [&](int c0) { return table[min((c0 + lane * kWaves) >> page_shift, a.C.max_pages - 1)]; };
+  const int page_shift = a.page_shift - 5;                     // of blocks
+  const int32_t* table = a.table + static_cast<size_t>(slot) * a.max_pages;
+  auto pages_from = [&](int c0) { return table[min((c0 + lane * kWaves) >> page_shift, a.max_pages - 1)]; };
   int my_page = 0;
   if (a.window == 0) my_page = pages_from(split * a.chunk + wave);
   // this lane's rows: the z-th is row 16 z + n of the tile
@@ -614,7 +608,7 @@ __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_atten
     const int r = tile * 16 * NT + 16 * z + n, j = r / a.group;
     hq[z] = head * a.group + r - j * a.group;
     row[z] = sq.row0 + j;
-    if (j >= news || row[z] >= a.b.n_rows) row[z] = -1;
+    if (j >= news || row[z] >= a.n_rows) row[z] = -1;
     rows[z].to = j + 1;       // (from the place of the first new token on, until the length is known)
     const uint16_t* q = a.q + static_cast<size_t>(max(0, row[z])) * a.ld_q + static_cast<size_t>(hq[z]) * D + kq * (D / 4);
 #pragma unroll
@@ -640,14 +634,14 @@ __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_atten
   }
 
   // the head's part of page 0 and the distance to the next page's
-  const unsigned part = (34u * D) << page_shift, page_bytes = part * static_cast<unsigned>(a.C.n_kv_heads);
-  const uint8_t* first_page = static_cast<const uint8_t*>(a.C.data) + static_cast<size_t>(a.layer) * a.C.n_pages * page_bytes + static_cast<size_t>(head) * part;
+  const unsigned part = (34u * D) << page_shift, page_bytes = part * static_cast<unsigned>(n_kv);
+  const uint8_t* first_page = a.data + static_cast<size_t>(head) * part;
   for (int c0 = b0 + wave; c0 < b1; c0 += 64 * kWaves) {
     const int mine = min(64, (b1 - c0 + kWaves - 1) / kWaves);
     if (c0 != b0 + wave) my_page = pages_from(c0);
     auto page_at = [&](int i) {                               // -1: a block without a page, which nobody sees
       const int page = __builtin_amdgcn_readlane(my_page, i);
-      return page < a.C.n_pages && (c0 + i * kWaves) >> page_shift < a.C.max_pages ? page : -1;
+      return page < a.n_pages && (c0 + i * kWaves) >> page_shift < a.max_pages ? page : -1;
     };
     auto address = [&](int i) {                               // (without a page any will do)
       return first_page + static_cast<size_t>(static_cast<unsigned>(max(0, page_at(i)))) * page_bytes +
@@ -681,7 +675,7 @@ __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_atten
     join_waves<D>(r, sh, lane, wave);
     if (wave > 0) continue;
     if (t.splits > 1) {
-      if (16 * z + n >= a.partial_rows) continue;
+      if (16 * z + n >= static_cast<int>(a.partial_rows)) continue;
       float* sums = split_sums(a, blockIdx.y, blockIdx.x, split, D);
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
@@ -722,14 +716,14 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
   constexpr int PL = D / 4 < 64 ? D / 4 : 64, GL = 64 / PL;   // lanes to a split's sums, splits at a time
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int unit = blockIdx.x;                                // as in kv4_attention_kernel
-  const int head = unit % a.C.n_kv_heads, tile = unit / a.C.n_kv_heads;
+  const int n_kv = a.n_kv_heads, head = unit % n_kv, tile = unit / n_kv;
   const int n = blockIdx.z * (4 / WR) + wave / WR;            // row of the tile
   const int first = wave % WR;
   // what a split of the plan may have left is read before it is known whether it did: the length takes as long to come
   const size_t stride = static_cast<size_t>(a.partial_rows) * (D + 2) * WR;
   const float* sums = split_sums(a, blockIdx.y, unit, first, D);
   float ref = -INFINITY, total = 0.f;
-  const int most = n < a.partial_rows ? (a.splits - first + WR - 1) / WR : 0;
+  const int most = n < static_cast<int>(a.partial_rows) ? (a.splits - first + WR - 1) / WR : 0;
   if (lane < most) {
     ref = sums[lane * stride + a.partial_rows * D + n];
     total = sums[lane * stride + a.partial_rows * (D + 1) + n];
@@ -743,13 +737,13 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
     early[e] = floatx4{0, 0, 0, 0};
     if (k < most) early[e] = *reinterpret_cast<const floatx4*>(sums + k * stride + n * D + 4 * c);
   }
-  const Sequence sq = sequence(a.C, a.b, blockIdx.y);
-  const int news = min(sq.n_new, a.b.max_new);
-  if (tile * a.tile_rows >= news * a.group) return;           // (uniform over the workgroup, as is the next)
+  const Sequence sq = sequence(a, blockIdx.y);
+  const int news = min(sq.n_new, static_cast<int>(a.max_new));
+  if (tile * static_cast<int>(a.tile_rows) >= news * a.group) return;           // (uniform over the workgroup, as is the next)
   const Tile t = find_tile(a, sq, news, tile, a.tile_rows);
   if (t.splits == 1) return;
-  const int r = tile * a.tile_rows + n, j = r / a.group, row = sq.row0 + j;
-  const bool has_row = n < a.partial_rows && j < news && row >= 0 && row < a.b.n_rows;
+  const int r = tile * static_cast<int>(a.tile_rows) + n, j = r / a.group, row = sq.row0 + j;
+  const bool has_row = n < static_cast<int>(a.partial_rows) && j < news && row >= 0 && row < a.n_rows;
   const int mine = has_row ? (t.splits - first + WR - 1) / WR : 0;
   if (lane >= mine) {
     ref = -INFINITY;
@@ -822,63 +816,52 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
 }
 
 template <typename F>
-hipError_t by_type(const larosa_kv4_cache& C, F&& f) {
-  const bool bf = C.dtype == LAROSA_BF16;
-  switch (C.head_dim) {
-    case 64: return bf ? f.template operator()<BF16, 64>() : f.template operator()<F16, 64>();
-    case 128: return bf ? f.template operator()<BF16, 128>() : f.template operator()<F16, 128>();
-    default: return bf ? f.template operator()<BF16, 256>() : f.template operator()<F16, 256>();
+hipError_t by_kind(Kv4Kind kind, F&& f) {
+  switch (kind.head_dim) {
+    case 64: return kind.bf16 ? f.template operator()<BF16, 64>() : f.template operator()<F16, 64>();
+    case 128: return kind.bf16 ? f.template operator()<BF16, 128>() : f.template operator()<F16, 128>();
+    default: return kind.bf16 ? f.template operator()<BF16, 256>() : f.template operator()<F16, 256>();
   }
 }
 
 struct AppendLaunch {
   const Kv4AppendArgs& a;
+  int n_seq;
   hipStream_t s;
   template <typename T, int D> hipError_t operator()() const {
-    const int heads = a.n_heads + 2 * a.C.n_kv_heads;
+    const int heads = a.n_heads + 2 * a.n_kv_heads, max_new = a.max_new;
     constexpr int kSlots = 256 / (D / 8), TW = kSlots < 16 ? kSlots : 16, HPL = 4;
-    if (a.b.max_new < TW) {
-      const dim3 grid((heads + kSlots - 1) / kSlots, a.b.n_seq, a.b.max_new);
-      hipLaunchKernelGGL((kv4_append_kernel<T, D, 1, 1>), grid, dim3(256), 0, s, a);
-    } else {
-      constexpr int kHeads = HPL * (kSlots / TW);
-      const dim3 grid((heads + kHeads - 1) / kHeads, a.b.n_seq, (a.b.max_new + TW - 1 + TW - 1) / TW);
-      hipLaunchKernelGGL((kv4_append_kernel<T, D, TW, HPL>), grid, dim3(256), 0, s, a);
-    }
-    return hipGetLastError();
+    if (max_new < TW) return kv4_launch(kv4_append_kernel<T, D, 1, 1>, dim3((heads + kSlots - 1) / kSlots, n_seq, max_new), dim3(256), s, a);
+    constexpr int kHeads = HPL * (kSlots / TW);
+    return kv4_launch(kv4_append_kernel<T, D, TW, HPL>, dim3((heads + kHeads - 1) / kHeads, n_seq, (max_new + TW - 1 + TW - 1) / TW), dim3(256), s, a);
   }
 };
 
 struct AttentionLaunch {
   const Kv4AttentionArgs& a;
+  int n_seq, row_tiles;
   hipStream_t s;
   template <typename T, int D> hipError_t operator()() const {
-    const dim3 grid(static_cast<unsigned>(a.row_tiles * a.C.n_kv_heads), static_cast<unsigned>(a.b.n_seq), static_cast<unsigned>(a.splits));
-    const dim3 block(64 * kWaves);
+    const dim3 grid(static_cast<unsigned>(row_tiles) * a.n_kv_heads, n_seq, a.splits), block(64 * kWaves);
+    const bool once = row_tiles == 1;
+    void (*kernel)(Kv4AttentionArgs) = once ? kv4_attention_kernel<T, D, 1, true> : kv4_attention_kernel<T, D, 1, false>;
     if constexpr (D <= 128) {
-      if (a.tile_rows == 32 && a.row_tiles == 1)
-        hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, true>), grid, block, 0, s, a);
-      else if (a.tile_rows == 32)
-        hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, false>), grid, block, 0, s, a);
+      if (a.tile_rows == 32) kernel = once ? kv4_attention_kernel<T, D, 2, true> : kv4_attention_kernel<T, D, 2, false>;
     }
-    if (a.tile_rows == 16 && a.row_tiles == 1)
-      hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, true>), grid, block, 0, s, a);
-    else if (a.tile_rows == 16)
-      hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, false>), grid, block, 0, s, a);
-    if (a.splits == 1) return hipGetLastError();
-    if (hipError_t e = hipGetLastError()) return e;
-    const unsigned rows = static_cast<unsigned>(a.partial_rows);
-    if (a.splits <= 16)
-      hipLaunchKernelGGL((kv4_combine_kernel<T, D, 1>), dim3(grid.x, grid.y, (rows + 3) / 4), dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((kv4_combine_kernel<T, D, 4>), dim3(grid.x, grid.y, rows), dim3(256), 0, s, a);
-    return hipGetLastError();
+    if (hipError_t e = kv4_launch(kernel, grid, block, s, a)) return e;
+    if (a.splits == 1) return hipSuccess;
+    if (a.splits <= 16) return kv4_launch(kv4_combine_kernel<T, D, 1>, dim3(grid.x, grid.y, (a.partial_rows + 3) / 4), dim3(256), s, a);
+    return kv4_launch(kv4_combine_kernel<T, D, 4>, dim3(grid.x, grid.y, a.partial_rows), dim3(256), s, a);
   }
 };
 
 }  // namespace
 
-hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s) { return by_type(a.C, AppendLaunch{a, s}); }
-hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, hipStream_t s) { return by_type(a.C, AttentionLaunch{a, s}); }
+hipError_t launch_kv4_append(const Kv4AppendArgs& a, Kv4Kind kind, int n_seq, hipStream_t s) {
+  return by_kind(kind, AppendLaunch{a, n_seq, s});
+}
+hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, Kv4Kind kind, int n_seq, int row_tiles, hipStream_t s) {
+  return by_kind(kind, AttentionLaunch{a, n_seq, row_tiles, s});
+}
 
 }  // namespace larosa

@@ -23,7 +23,7 @@ int check_sizes(const larosa_kv4_cache* C) {
   if (C->page_tokens != 32 && C->page_tokens != 64 && C->page_tokens != 128 && C->page_tokens != 256) return LAROSA_EINVAL;
   if (C->head_dim != 64 && C->head_dim != 128 && C->head_dim != 256) return LAROSA_EUNSUPPORTED;
   // places in a sequence and numbers of pages are 32-bit
-  if (static_cast<long>(C->max_pages) * C->page_tokens >= (1L << 30) || C->n_kv_heads > 4096) return LAROSA_EUNSUPPORTED;
+  if (static_cast<long>(C->max_pages) * C->page_tokens >= (1L << 30) || C->n_kv_heads > kKv4HeadsMax) return LAROSA_EUNSUPPORTED;
   if (C->n_pages > (1 << 28) || C->n_slots > kKv4SlotsMax || C->n_layers > 65535) return LAROSA_EUNSUPPORTED;
   if (static_cast<long>(C->n_slots) * C->max_pages >= (1L << 31)) return LAROSA_EUNSUPPORTED;   // (counts of pages are 32-bit)
   return LAROSA_OK;
@@ -40,7 +40,7 @@ int check_batch(const larosa_kv4_batch* b) {
   if (!b || !b->slots || b->n_seq < 1 || b->n_rows < 1 || b->max_new < 1) return LAROSA_EINVAL;
   if (!aligned(b->slots, 4) || !aligned(b->starts, 4)) return LAROSA_EINVAL;
   if (!b->starts && (b->max_new != 1 || b->n_rows < b->n_seq)) return LAROSA_EINVAL;
-  if (b->n_seq > 65535 || b->max_new > (1 << 18)) return LAROSA_EUNSUPPORTED;      // (sides of a launch)
+  if (b->n_seq > 65535 || b->max_new > kKv4NewMax) return LAROSA_EUNSUPPORTED;      // (sides of a launch)
   return LAROSA_OK;
 }
 
@@ -116,28 +116,24 @@ AttentionPlan plan_attention(const larosa_kv4_cache* C, const larosa_kv4_batch* 
   return p;
 }
 
-size_t scratch_bytes(const larosa_kv4_cache* C) {
-  return 512 + 5 * round_up(static_cast<size_t>(C->n_pages) * 4, 256) + 2 * round_up(static_cast<size_t>(C->n_slots) * 4, 256);
+Kv4Scratch scratch_of(void* ws) { return Kv4Scratch{reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kCounterBytes)}; }
+
+Kv4Kind kind_of(const larosa_kv4_cache* C) { return Kv4Kind{C->head_dim, C->dtype == LAROSA_BF16}; }
+
+uint8_t* layer_data(const larosa_kv4_cache* C, int layer) {
+  return static_cast<uint8_t*>(C->data) +
+         static_cast<size_t>(layer) * C->n_pages * larosa_kv4_page_bytes(C->page_tokens, C->n_kv_heads, C->head_dim);
 }
 
-Kv4Scratch scratch_of(const larosa_kv4_cache* C, void* ws) {
-  char* p = static_cast<char*>(ws) + kCounterBytes;
-  auto take = [&](size_t words) {
-    int32_t* r = reinterpret_cast<int32_t*>(p);
-    p += round_up(words * 4, 256);
-    return r;
-  };
-  Kv4Scratch x;
-  x.n_pairs = take(1);
-  x.pair_src = take(C->n_pages);
-  x.pair_dst = take(C->n_pages);
-  x.free_ids = take(C->n_pages);
-  x.growing = take(C->n_pages);
-  x.last = take(C->n_pages);
-  x.offset = take(C->n_slots);
-  x.pair = take(C->n_slots);
-  x.n_live = take(1);
-  return x;
+// What append and attention have in common.
+template <typename Args>
+void fill_common(Args& a, const larosa_kv4_cache* C, const larosa_kv4_batch* b, int layer) {
+  a.data = layer_data(C, layer);
+  a.table = C->table; a.length = C->length;
+  a.slots = b->slots; a.starts = b->starts;
+  a.n_pages = C->n_pages; a.max_pages = C->max_pages; a.n_slots = C->n_slots; a.n_kv_heads = C->n_kv_heads;
+  a.n_rows = b->n_rows; a.max_new = b->max_new;
+  a.page_shift = __builtin_ctz(C->page_tokens);
 }
 
 // A list of slots and the status it reports to.
@@ -185,11 +181,20 @@ int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_bat
     if (!out) return LAROSA_EINVAL;
   }
   Kv4AppendArgs a{};
-  a.C = *C; a.b = *b; a.layer = layer; a.n_heads = n_heads;
-  if (rotary) a.r = *rotary;
+  fill_common(a, C, b, layer);
+  a.n_heads = n_heads;
+  if (rotary) {
+    a.turns = rotary->table; a.positions = rotary->positions;
+    a.n_positions = rotary->n_positions; a.rot_dim = rotary->rot_dim;
+    a.interleaved = rotary->interleaved != 0; a.n_axes = rotary->n_axes;
+    for (int i = 0, end = 0; i < 3; ++i) {
+      if (i + 1 < rotary->n_axes) end += rotary->axis_pairs[i];
+      a.axis_ends |= static_cast<uint32_t>(i + 1 < rotary->n_axes ? end : 255) << 8 * i;
+    }
+  }
   a.qkv = static_cast<const uint16_t*>(qkv); a.ld_qkv = ld_qkv;
   a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
-  return status_of(launch_kv4_append(a, stream_of(stream)));
+  return status_of(launch_kv4_append(a, kind_of(C), b->n_seq, stream_of(stream)));
 }
 
 size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int max_len) {
@@ -208,7 +213,8 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   if (!std::isfinite(scale) || window < 0 || max_len < 0) return LAROSA_EINVAL;
   if (!ws || !aligned(ws, 256) || ws_bytes < larosa_kv4_attention_workspace_bytes(C, b, n_heads, max_len)) return LAROSA_EWORKSPACE;
   Kv4AttentionArgs a{};
-  a.C = *C; a.b = *b; a.layer = layer; a.n_heads = n_heads; a.group = n_heads / C->n_kv_heads;
+  fill_common(a, C, b, layer);
+  a.group = n_heads / C->n_kv_heads;
   a.q = static_cast<const uint16_t*>(q); a.ld_q = ld_q;
   a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
   a.scale_log2 = scale * 1.4426950408889634f;
@@ -218,16 +224,15 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   if (p.partial_bytes > all.partial_bytes) p = all;
   if (p.row_tiles * C->n_kv_heads >= (1L << 23)) return LAROSA_EUNSUPPORTED;      // workgroups along one side of a launch
   a.tile_rows = p.tile_rows;
-  a.row_tiles = static_cast<int>(p.row_tiles);
   a.chunk = p.chunk; a.splits = p.splits; a.partial_rows = p.partial_rows;
   a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
-  return status_of(launch_kv4_attention(a, stream_of(stream)));
+  return status_of(launch_kv4_attention(a, kind_of(C), b->n_seq, static_cast<int>(p.row_tiles), stream_of(stream)));
 }
 
 // ---- pages ---------------------------------------------------------------------------------------
 
 size_t larosa_kv4_pages_workspace_bytes(const larosa_kv4_cache* C) {
-  return check_sizes(C) == LAROSA_OK ? kCounterBytes + scratch_bytes(C) : 0;
+  return check_sizes(C) == LAROSA_OK ? kCounterBytes + kv4_scratch_bytes(*C) : 0;
 }
 
 int larosa_kv4_grow(const larosa_kv4_cache* C, const int32_t* slots, const int32_t* counts, int n, int32_t* status, void* ws,
@@ -236,7 +241,7 @@ int larosa_kv4_grow(const larosa_kv4_cache* C, const int32_t* slots, const int32
   if (int rc = check_list(C, slots, n)) return rc;
   if (!aligned(counts, 4) || !status || !aligned(status, 4)) return LAROSA_EINVAL;
   if (!ws || !aligned(ws, 256) || ws_bytes < larosa_kv4_pages_workspace_bytes(C)) return LAROSA_EWORKSPACE;
-  return status_of(launch_kv4_grow(*C, slots, counts, n, status, scratch_of(C, ws), stream_of(stream)));
+  return status_of(launch_kv4_grow(*C, slots, counts, n, status, scratch_of(ws), stream_of(stream)));
 }
 
 int larosa_kv4_fork(const larosa_kv4_cache* C, const int32_t* src, const int32_t* dst, int n, int32_t* status, void* stream) {
@@ -258,7 +263,7 @@ int larosa_kv4_compact(const larosa_kv4_cache* C, int32_t* live, void* ws, size_
   if (int rc = check_cache(C)) return rc;
   if (!aligned(live, 4)) return LAROSA_EINVAL;
   if (!ws || !aligned(ws, 256) || ws_bytes < larosa_kv4_pages_workspace_bytes(C)) return LAROSA_EWORKSPACE;
-  return status_of(launch_kv4_compact(*C, live, scratch_of(C, ws), stream_of(stream)));
+  return status_of(launch_kv4_compact(*C, live, scratch_of(ws), stream_of(stream)));
 }
 
 int larosa_kv4_copy_pages(const larosa_kv4_cache* C, const int32_t* src, const int32_t* dst, int n, void* stream) {

@@ -153,8 +153,8 @@ __device__ __forceinline__ uint32_t free_bits(const larosa_kv4_cache& C, int p0)
 
 // Latency-bound: a chain of loads (slot, length, table, references), the free pages looked for beside it.  A lane keeps what it found out
 // about its slot; lists longer than the workgroup look again.
-__global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, const int32_t* slots, const int32_t* counts, int n,
-                                                         int32_t* status, Kv4Scratch x) {
+__global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, const int32_t* slots, const int32_t* counts,
+                                                         int32_t* status, Kv4Scratch x, int n) {
   __shared__ int bad, shared_pages, many;
   __shared__ uint32_t listed[kKv4SlotsMax / 32];
   __shared__ int s_ids[2 * kBook], s_offset[kBook], s_pair[kBook];
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, con
   for (int k = tid; k < (C.n_slots + 31) / 32; k += kBook) listed[k] = 0;
   if (tid == 0) {
     bad = shared_pages = many = 0;
-    *x.n_pairs = 0;
+    *x.n_pairs() = 0;
   }
   __syncthreads();
   for (int i = tid; i < n; i += kBook) {
@@ -178,8 +178,8 @@ __global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, con
     }
     if (w.page >= 0) {
       shared_pages = 1;
-      atomicExch(&x.growing[w.page], 0);
-      atomicExch(&x.last[w.page], 0);
+      atomicExch(&x.growing(C)[w.page], 0);
+      atomicExch(&x.last(C)[w.page], 0);
     }
   }
   __syncthreads();
@@ -191,15 +191,15 @@ __global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, con
     for (int i = tid; i < n; i += kBook) {
       const Want w = want(i);
       if (w.page >= 0) {
-        atomicAdd(&x.growing[w.page], 1);
-        atomicMax(&x.last[w.page], i + 1);
+        atomicAdd(&x.growing(C)[w.page], 1);
+        atomicMax(&x.last(C)[w.page], i + 1);
       }
     }
     __syncthreads();
   }
   // pages for each slot of the list, in its order: a copy of the shared page first, then the new ones
-  int* const offset = n <= kBook ? s_offset : x.offset;
-  int* const pair = n <= kBook ? s_pair : x.pair;
+  int* const offset = n <= kBook ? s_offset : x.offset(C);
+  int* const pair = n <= kBook ? s_pair : x.pair(C);
   unsigned wanted = 0, copies = 0;
   for (int i0 = 0; i0 < n; i0 += kBook) {
     const int i = i0 + tid;
@@ -207,20 +207,20 @@ __global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, con
     bool copy = false;
     if (i < n) {
       w = want(i);
-      copy = w.page >= 0 && !(atomicAdd(&x.growing[w.page], 0) == C.refs[w.page] && atomicAdd(&x.last[w.page], 0) == i + 1);
+      copy = w.page >= 0 && !(atomicAdd(&x.growing(C)[w.page], 0) == C.refs[w.page] && atomicAdd(&x.last(C)[w.page], 0) == i + 1);
     }
     const Sums s = book_scan(w.new_pages - w.old_pages + copy, copy);
     if (i < n) {
       offset[i] = static_cast<int>(wanted + s.a);
       pair[i] = copy ? static_cast<int>(copies + s.b) : -1;
       // (more copies than pages: the call is refused below)
-      if (copy && copies + s.b < static_cast<unsigned>(C.n_pages)) x.pair_src[copies + s.b] = w.page;
+      if (copy && copies + s.b < static_cast<unsigned>(C.n_pages)) x.pair_src(C)[copies + s.b] = w.page;
     }
     wanted += s.all_a;
     copies += s.all_b;
   }
   // the lowest free pages, eight to a lane at a time
-  int* const ids = wanted <= 2 * kBook ? s_ids : x.free_ids;
+  int* const ids = wanted <= 2 * kBook ? s_ids : x.ids(C);
   unsigned found = 0;
   for (int p0 = 0; p0 < C.n_pages && found < wanted; p0 += kBook * 8) {
     const uint32_t free8 = p0 == 0 ? first_free : free_bits(C, p0);
@@ -243,8 +243,8 @@ __global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, con
     C.table[static_cast<size_t>(w.slot) * C.max_pages + w.old_pages - copied + r] = page;
     C.refs[page] = 1;
     if (copied && r == 0) {
-      x.pair_dst[pair[i]] = page;
-      atomicSub(&C.refs[x.pair_src[pair[i]]], 1);
+      x.pair_dst(C)[pair[i]] = page;
+      atomicSub(&C.refs[x.pair_src(C)[pair[i]]], 1);
     }
   };
   constexpr int kFew = 4;     // a lane gives its slot so many; slots that get more are a wave's work each
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kBook) void kv4_grow_kernel(larosa_kv4_cache C, con
     C.length[w.slot] = w.had + w.count;
   }
   if (tid == 0) {
-    *x.n_pairs = static_cast<int>(copies);
+    *x.n_pairs() = static_cast<int>(copies);
     *status = 0;
   }
 }
@@ -292,22 +292,22 @@ __global__ __launch_bounds__(kBook) void kv4_compact_kernel(larosa_kv4_cache C, 
     const Sums s = book_scan(__popc(hole8), __popc(mover8));
     unsigned a = holes + s.a, b = movers + s.b;
     for (int k = 0; k < 8; ++k) {
-      if (hole8 >> k & 1) x.pair_dst[a++] = p + k;
-      if (mover8 >> k & 1) x.pair_src[b++] = p + k;
+      if (hole8 >> k & 1) x.pair_dst(C)[a++] = p + k;
+      if (mover8 >> k & 1) x.pair_src(C)[b++] = p + k;
     }
     holes += s.all_a;
     movers += s.all_b;
   }
   __syncthreads();
   for (unsigned k = tid; k < movers; k += kBook) {
-    const int from = x.pair_src[k], to = x.pair_dst[k];
-    x.free_ids[from] = to;
+    const int from = x.pair_src(C)[k], to = x.pair_dst(C)[k];
+    x.ids(C)[from] = to;
     C.refs[to] = C.refs[from];
     C.refs[from] = 0;
   }
   if (tid == 0) {
-    *x.n_pairs = static_cast<int>(movers);
-    *x.n_live = n_live;
+    *x.n_pairs() = static_cast<int>(movers);
+    *x.n_live() = n_live;
     if (live) *live = n_live;
   }
 }
@@ -335,25 +335,26 @@ __device__ __forceinline__ void copy_step(const piece_t* a, piece_t* b, unsigned
   }
 }
 
-// Pages src[i] into dst[i], all layers; the pairs' number comes from n_pairs or, where that is null, from n.  Where `to` is given, ids
-// from *n_live on in the tables become to[id] as well.  Layer by layer, so that neighbouring pages move at the same time (packing
+// Pages src[i] into dst[i], all layers; the pairs' number comes from n_pairs or, where that is null, from n.  With `remap`, ids
+// that a packing has moved change in the tables as well.  Layer by layer, so that neighbouring pages move at the same time (packing
 // 102 pages of 2.2 MB: 145 us pair by pair, 120 so, 98 at the rate of a large copy); what the 256 MB cache behind the L2s does
 // not hold passes them by (128 us without; but 23 MB take 6.4 us through them, 7.4 past them).
 __global__ __launch_bounds__(256) void kv4_copy_kernel(larosa_kv4_cache C, const int32_t* src, const int32_t* dst, const int32_t* n_pairs,
-                                                       int n, unsigned page_pieces, const int32_t* to, const int32_t* n_live) {
+                                                       Kv4Scratch remap, int n, unsigned page_pieces, unsigned grid) {
   if (n_pairs) n = *n_pairs;
-  if (to) {
+  if (remap.base) {
+    const int32_t* to = remap.ids(C);
     const unsigned entries = static_cast<unsigned>(C.n_slots) * C.max_pages;
-    for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < entries; e += gridDim.x * 256) {
+    for (unsigned e = blockIdx.x * 256 + threadIdx.x; e < entries; e += grid * 256) {
       const int page = C.table[e];
-      if (page >= *n_live && page < C.n_pages) C.table[e] = to[page];
+      if (page >= *remap.n_live() && page < C.n_pages) C.table[e] = to[page];
     }
   }
   const unsigned steps = (page_pieces + kCopyPieces - 1) / kCopyPieces;
   const unsigned items = static_cast<unsigned>(n) * C.n_layers * steps;        // (16 KiB each: far below 2^32 in any memory)
   const bool stream = static_cast<size_t>(n) * C.n_layers * page_pieces * 32 > (static_cast<size_t>(256) << 20);
   piece_t* data = static_cast<piece_t*>(C.data);
-  for (unsigned it = blockIdx.x; it < items; it += gridDim.x) {
+  for (unsigned it = blockIdx.x; it < items; it += grid) {
     const unsigned rest = it / steps, first = (it - rest * steps) * kCopyPieces;
     const unsigned layer = rest / n, i = rest - layer * n;
     const int from = src[i], into = dst[i];
@@ -368,51 +369,45 @@ __global__ __launch_bounds__(256) void kv4_copy_kernel(larosa_kv4_cache C, const
   }
 }
 
-hipError_t launch_copy(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, const int32_t* n_pairs, int n,
-                       const int32_t* to, const int32_t* n_live, hipStream_t s) {
+hipError_t launch_copy(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, const int32_t* n_pairs, Kv4Scratch remap, int n,
+                       hipStream_t s) {
   const unsigned page_pieces = static_cast<unsigned>(C.n_kv_heads) * (C.page_tokens / 32) * 34 * C.head_dim / 16;
   const size_t items = static_cast<size_t>(n) * C.n_layers * ((page_pieces + kCopyPieces - 1) / kCopyPieces);
   const unsigned grid = static_cast<unsigned>(items < 16384 ? items : 16384);
-  hipLaunchKernelGGL(kv4_copy_kernel, dim3(grid), dim3(256), 0, s, C, src, dst, n_pairs, n, page_pieces, to, n_live);
-  return hipGetLastError();
+  return kv4_launch(kv4_copy_kernel, dim3(grid), dim3(256), s, C, src, dst, n_pairs, remap, n, page_pieces, grid);
 }
 
 }  // namespace
 
 hipError_t launch_kv4_trim(const larosa_kv4_cache& C, const int32_t* slots, const int32_t* keep, int n, hipStream_t s) {
-  hipLaunchKernelGGL(kv4_trim_kernel, dim3((n + 3) / 4), dim3(256), 0, s, C, slots, keep, n);
-  return hipGetLastError();
+  return kv4_launch(kv4_trim_kernel, dim3((n + 3) / 4), dim3(256), s, C, slots, keep, n);
 }
 
 hipError_t launch_kv4_fork(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, int n, int32_t* status, hipStream_t s) {
   // up to eight entries a lane: 2 us less than with a launch for the tables
   const bool whole = static_cast<long>(n) * C.max_pages <= 8 * kBook;
-  hipLaunchKernelGGL(kv4_fork_check_kernel, dim3(1), dim3(kBook), 0, s, C, src, dst, n, status, whole);
-  if (hipError_t e = hipGetLastError()) return e;
+  if (hipError_t e = kv4_launch(kv4_fork_check_kernel, dim3(1), dim3(kBook), s, C, src, dst, n, status, whole)) return e;
   if (whole) return hipSuccess;
   for (int at = 0; at < n; at += 65535) {
     const dim3 grid((C.max_pages + 255) / 256, n - at < 65535 ? n - at : 65535);
-    hipLaunchKernelGGL(kv4_fork_kernel, grid, dim3(256), 0, s, C, src + at, dst + at, status);
-    if (hipError_t e = hipGetLastError()) return e;
+    if (hipError_t e = kv4_launch(kv4_fork_kernel, grid, dim3(256), s, C, src + at, dst + at, static_cast<const int32_t*>(status))) return e;
   }
   return hipSuccess;
 }
 
-hipError_t launch_kv4_grow(const larosa_kv4_cache& C, const int32_t* slots, const int32_t* counts, int n, int32_t* status,
-                           const Kv4Scratch& x, hipStream_t s) {
-  hipLaunchKernelGGL(kv4_grow_kernel, dim3(1), dim3(kBook), 0, s, C, slots, counts, n, status, x);
-  if (hipError_t e = hipGetLastError()) return e;
-  return launch_copy(C, x.pair_src, x.pair_dst, x.n_pairs, n < C.n_pages ? n : C.n_pages, nullptr, nullptr, s);
+hipError_t launch_kv4_grow(const larosa_kv4_cache& C, const int32_t* slots, const int32_t* counts, int n, int32_t* status, Kv4Scratch x,
+                           hipStream_t s) {
+  if (hipError_t e = kv4_launch(kv4_grow_kernel, dim3(1), dim3(kBook), s, C, slots, counts, status, x, n)) return e;
+  return launch_copy(C, x.pair_src(C), x.pair_dst(C), x.n_pairs(), Kv4Scratch{nullptr}, n < C.n_pages ? n : C.n_pages, s);
 }
 
-hipError_t launch_kv4_compact(const larosa_kv4_cache& C, int32_t* live, const Kv4Scratch& x, hipStream_t s) {
-  hipLaunchKernelGGL(kv4_compact_kernel, dim3(1), dim3(kBook), 0, s, C, live, x);
-  if (hipError_t e = hipGetLastError()) return e;
-  return launch_copy(C, x.pair_src, x.pair_dst, x.n_pairs, C.n_pages, x.free_ids, x.n_live, s);
+hipError_t launch_kv4_compact(const larosa_kv4_cache& C, int32_t* live, Kv4Scratch x, hipStream_t s) {
+  if (hipError_t e = kv4_launch(kv4_compact_kernel, dim3(1), dim3(kBook), s, C, live, x)) return e;
+  return launch_copy(C, x.pair_src(C), x.pair_dst(C), x.n_pairs(), x, C.n_pages, s);
 }
 
 hipError_t launch_kv4_copy_pages(const larosa_kv4_cache& C, const int32_t* src, const int32_t* dst, int n, hipStream_t s) {
-  return launch_copy(C, src, dst, nullptr, n, nullptr, nullptr, s);
+  return launch_copy(C, src, dst, nullptr, Kv4Scratch{nullptr}, n, s);
 }
 
 }  // namespace larosa
