@@ -11,7 +11,10 @@ namespace {
 
 constexpr int kBook = 1024;   // lanes of a bookkeeping workgroup
 
-__device__ __forceinline__ int pages_for(int tokens, int page_tokens) { return (tokens + page_tokens - 1) / page_tokens; }
+// (unsigned: a number of tokens may be up to 2^31 - 1)
+__device__ __forceinline__ int pages_for(int tokens, int page_tokens) {
+  return static_cast<int>((static_cast<unsigned>(tokens) + page_tokens - 1) / page_tokens);
+}
 
 // Exclusive prefix sums of two counts over the workgroup's lanes, and their totals.
 struct Sums { unsigned a, b, all_a, all_b; };
@@ -50,8 +53,9 @@ __global__ __launch_bounds__(256) void kv4_trim_kernel(larosa_kv4_cache C, const
   int had = 0;
   if (lane == 0) had = atomicMin(&C.length[slot], kept);
   had = __shfl(had, 0);
-  const int to = min(pages_for(had, C.page_tokens), C.max_pages);
-  for (int p = pages_for(kept, C.page_tokens) + lane; p < to; p += 64) {
+  // keep may exceed what the sequence has, by anything: its pages then all stay
+  const int from = pages_for(max(0, min(kept, had)), C.page_tokens), to = min(pages_for(max(0, had), C.page_tokens), C.max_pages);
+  for (int p = from + lane; p < to; p += 64) {
     const int page = atomicExch(&C.table[static_cast<size_t>(slot) * C.max_pages + p], -1);
     if (page >= 0 && page < C.n_pages) atomicSub(&C.refs[page], 1);
   }

@@ -282,3 +282,14 @@ def test_two_streams_with_a_cache_and_workspace_each(gpu_device):
     torch.cuda.synchronize()
     for j in jobs:
         assert torch.equal(j["out"].view(torch.int16), j["alone"].view(torch.int16))
+
+
+def test_trim_that_keeps_more_than_there_is(gpu_device):
+    """keep up to the largest int32, for used and free slots, beside a smaller keep of the same slot: nothing else may change."""
+    t = Twin(K.Cache(1, 12, 32, 6, 4, 1, 64, "f16"))
+    assert t.grow([0, 1, 2], [70, 128, 32]) == 0
+    for keep in (71, 129, 2 ** 31 - 33, 2 ** 31 - 32, 2 ** 31 - 31, 2 ** 31 - 1):
+        t.trim([0, 1, 2, 3, 5], [keep] * 5)
+    t.trim([1, 1, 4, 2], [2 ** 31 - 1, 40, 2 ** 31 - 1, 2 ** 31 - 2])
+    t.trim([0, 3], [2 ** 31 - 32, -2 ** 31])
+    assert t.cache.length.tolist() == [70, 40, 32, 0, 0, 0]
