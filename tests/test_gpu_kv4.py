@@ -210,6 +210,36 @@ def test_attention_extreme_logits(gpu_device):
     check_attention(C, slots, None, q, 1, scale=-1.0)
 
 
+def chosen_tokens(rng, dtype, keys, values, page=64):
+    """One sequence whose keys are keys[t] in their first value and zero elsewhere, whose values are values[t]: a logit is
+    then the query's first value times keys[t] times the scale."""
+    n, D = values.shape
+    C, slots = U.random_cache(rng, [n], page, 1, D, dtype)
+    for t in range(n):
+        block = C.block(0, slots[0], t, 0)
+        k = np.zeros(D)
+        k[0] = keys[t]
+        K.write_token(block, D, t % 32, 0, *K.quantise(k, dtype))
+        K.write_token(block, D, t % 32, 1, *K.quantise(values[t], dtype))
+    return C, slots
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,gap", [(700, 8.1), (700, 11.2), (700, 13.3), (700, 14.2), (3000, 12.4), (3000, 14.0), (3000, 14.5)])
+def test_attention_many_small_weights_behind_a_large_one(gpu_device, dtype, n, gap):
+    """The first token's logit lies `gap` above all others' (weights down to 2^-20.9 of its own), and its value is zero: the output
+    is made of the small weights alone, each of which keeps its half step (the tolerance knows no floor of the weights)."""
+    rng = np.random.default_rng(18)
+    D = 64
+    keys, values = np.zeros(n), np.tile(rng.choice(K.LEVELS[1:], D) * 64.0, (n, 1))
+    keys[0], values[0] = 4.0, 0.0
+    C, slots = chosen_tokens(rng, dtype, keys, values)
+    q = rng.standard_normal((1, 2 * D))
+    q[0, 0] = q[0, D] = 1.0
+    got = check_attention(C, slots, None, O.encode16(q, dtype), 2, scale=gap / 4)
+    assert got.any()
+
+
 # ---- append ---------------------------------------------------------------------------------------------------
 
 def make_table(rng, n, rot):
