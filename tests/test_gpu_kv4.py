@@ -240,6 +240,25 @@ def test_attention_many_small_weights_behind_a_large_one(gpu_device, dtype, n, g
     assert got.any()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [700, 4000])
+def test_attention_weights_that_round_alike(gpu_device, dtype, n):
+    """The first 128 tokens' logits are zero (every wave's reference), all others' weights just below the middle between two
+    neighbouring 16-bit numbers, and all values equal: their average is that value again, to the bit."""
+    rng = np.random.default_rng(19)
+    D = 64
+    step = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -10
+    keys = np.where(np.arange(n) < 128, 0.0, 1.0)
+    values = np.tile(rng.choice(K.LEVELS[1:], D), (n, 1))
+    C, slots = chosen_tokens(rng, dtype, keys, values)
+    q = np.zeros((1, D))
+    q[0, 0] = 1.0
+    for octaves in (0, 2):
+        scale = np.log(2.0 ** octaves * (1 + 0.495 * step))
+        got = check_attention(C, slots, None, O.encode16(q, dtype), 1, scale=scale)
+        assert np.array_equal(got[0, 0], values[0])
+
+
 # ---- append ---------------------------------------------------------------------------------------------------
 
 def make_table(rng, n, rot):
