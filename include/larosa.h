@@ -170,7 +170,9 @@ size_t larosa_layer_workspace_bytes(const larosa_layer* L, int B);
  *   h4 = R(SiLU(gate) * up); down = R(S_K4(h4) Wdown); x2 = R(s2 + down);
  *   x_out = R(x2 adapter) or x2;  s1 = R(x shortcut_attn) or x;  s2 = R(x1 shortcut_mlp) or x1.
  *   R = one rounding to the layer dtype.
- * trace may be NULL.  x_out must not alias x. */
+ * trace may be NULL.  x_out must not alias x.  Rows: the projections of several rows take a counter of the workspace for each
+ * group of 32 rows and 128 output columns (those of a shortcut adapter beside its projection's included), and there are
+ * 4096: with gate|up 28672 wide up to 576 rows.  More are LAROSA_EUNSUPPORTED. */
 int larosa_layer_forward(const larosa_layer* L, const void* x, void* x_out, int B,
                          const larosa_trace* trace, void* ws, size_t ws_bytes, void* stream);
 
@@ -374,7 +376,8 @@ int larosa_kv4_copy_pages(const larosa_kv4_cache* C, const int32_t* src, const i
 /* One decoder layer with this cache as its attention core: larosa_layer_qkv, larosa_kv4_append, larosa_kv4_attention and
  * larosa_layer_after_attention over batch->n_rows rows, x [n_rows, d] -> x_out [n_rows, d].  The lengths count the rows'
  * tokens already (larosa_kv4_grow once for all layers).  L's head_dim, d_kv and dtype are the cache's.  trace as in the split calls.
- * Rows of no sequence come out unspecified.  Workspace: larosa_layer_kv4_workspace_bytes, initialised as ever. */
+ * Rows of no sequence come out unspecified.  Rows up to what larosa_layer_forward takes: longer prompts go through in pieces, the cache
+ * holds what came before.  Workspace: larosa_layer_kv4_workspace_bytes (0 for a call that would be refused), initialised as ever. */
 size_t larosa_layer_kv4_workspace_bytes(const larosa_layer* L, const larosa_kv4_cache* C, const larosa_kv4_batch* batch, int max_len);
 int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* batch,
                              const larosa_rotary* rotary, float scale, int window, int max_len, const void* x, void* x_out,

@@ -46,6 +46,9 @@ size_t batched_partial_bytes(const GemvPlan& p, int B, bool coef_scale, int d_in
   return groups * tpg * p.partial_floats * sizeof(float);
 }
 
+// Arrival counters of a batched product: one for each group of tokens and strip.
+size_t batched_slots(size_t groups, int d_out) { return groups * ((d_out + kBatchStrip - 1) / kBatchStrip); }
+
 // One launch of the batched kernels (B > 1): C holds the tokens' coefficients over all rows.  An
 // optional side product (side.W != nullptr: same token count, no coefficient scale) shares the launch.
 // Counters and partial sums are laid out, and refused, by strips of 128 columns, whatever the launch takes (plan_batched).
@@ -77,7 +80,7 @@ int run_batched(BatchArgs a, bool bf16, void* ws, size_t ws_bytes, hipStream_t s
     x.strip_cols = p.strip_cols;
     x.counters = counters + slots * kCounterStride;
     x.partial = reinterpret_cast<float*>(partial + pbytes);
-    slots += groups * ((x.d_out + kBatchStrip - 1) / kBatchStrip);
+    slots += batched_slots(groups, x.d_out);
     pbytes += groups * tpg * p.partial_floats * sizeof(float);
   };
   BatchPair pr{};
@@ -315,6 +318,31 @@ static int check_layer(const larosa_layer* L, int B) {
   return LAROSA_OK;
 }
 
+// Whether the counters of a workspace suffice for every batched launch of a layer (what run_batched would refuse, with some of the
+// launches already enqueued).  L and B have passed check_layer.
+static int check_layer_counters(const larosa_layer* L, int B, bool until_qkv, bool after_attention) {
+  if (B == 1) return LAROSA_OK;
+  const bool norm = L->rms_eps >= 0.f;
+  auto fits = [&](int d_in, int d_out, const void* scale, const void* side) {
+    const bool cs = norm && scale;
+    const size_t tpg = batched_tokens_per_group(B, cs, d_in, d_out), groups = (B + tpg - 1) / tpg;
+    return batched_slots(groups, d_out) + (side ? batched_slots(groups, L->d) : 0) <= kCounterSlots;
+  };
+  bool ok = true;
+  if (until_qkv) {
+    if (L->Q_attn) ok = ok && fits(L->d, L->d, L->rms_attn, nullptr);
+    // (after the attention the shortcut's value is there already)
+    ok = ok && fits(L->d, L->d_q + 2 * L->d_kv, nullptr, L->shortcut_attn);
+  }
+  if (after_attention) {
+    ok = ok && fits(L->d_q, L->d, nullptr, nullptr);
+    if (L->Q_mlp) ok = ok && fits(L->d, L->d, L->rms_mlp, nullptr);
+    ok = ok && fits(L->d, 2 * L->d_ff, nullptr, L->shortcut_mlp) && fits(L->d_ff, L->d, nullptr, nullptr);
+    if (L->adapter) ok = ok && fits(L->d, L->d, nullptr, nullptr);
+  }
+  return ok ? LAROSA_OK : LAROSA_EUNSUPPORTED;
+}
+
 static int max3(int a, int b, int c) { return a > b ? (a > c ? a : c) : (b > c ? b : c); }
 
 static size_t layer_gemv_ws(const larosa_layer* L, int B) {
@@ -392,6 +420,7 @@ int layer_run(const larosa_layer* L, const void* x_in, void* x_out, int B, const
     if (part == kAfterAttention && (!attn_ext || !aligned(attn_ext, 16))) return LAROSA_EINVAL;
   }
   if (!ws || !aligned(ws, 256) || ws_bytes < larosa_layer_workspace_bytes(L, B)) return LAROSA_EWORKSPACE;
+  if (int rc = check_layer_counters(L, B, part != kAfterAttention, part != kUntilQkv)) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf = L->dtype == LAROSA_BF16;
   const size_t Bz = static_cast<size_t>(B);
@@ -966,3 +995,8 @@ int larosa_set_tuning(int key, int value) {
 }
 
 }  // extern "C"
+
+int larosa::check_layer_rows(const larosa_layer* L, int B) {
+  if (int rc = check_layer(L, B)) return rc;
+  return check_layer_counters(L, B, true, true);
+}

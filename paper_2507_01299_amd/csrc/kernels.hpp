@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/larosa.h"
+
 namespace larosa {
 
 // Row-streaming mat-vec  y[b,:] = epilogue( sum_t c[b,t] * W[row(b,t), :] ).
@@ -213,5 +215,9 @@ hipError_t launch_contraction(ContractionArgs a, bool a_kmajor, bool bf16, hipSt
 int contraction_terms(bool bf16);
 // dst[t][i] for t < terms: src[i] * pre_scale = sum_t dst[t][i] up to the last term's rounding
 hipError_t launch_split_terms(const float* src, uint16_t* dst, long n, float pre_scale, bool bf16, hipStream_t s);
+
+// api.hip: whether a decoder layer and B rows are a call that larosa_layer_qkv and larosa_layer_after_attention both take (sizes and
+// pointers of the layer alone).
+int check_layer_rows(const larosa_layer* L, int B);
 
 }  // namespace larosa

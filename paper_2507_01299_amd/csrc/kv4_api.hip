@@ -49,6 +49,13 @@ int check_heads(const larosa_kv4_cache* C, int n_heads) {
   return n_heads > 65536 ? LAROSA_EUNSUPPORTED : LAROSA_OK;
 }
 
+// Attention of so many heads: its tiles of 16 rows lie along one side of a launch (of 256 lanes each, below 2^32).
+int check_attention(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads) {
+  if (int rc = check_heads(C, n_heads)) return rc;
+  const long rows = static_cast<long>(b->max_new) * (n_heads / C->n_kv_heads);
+  return (rows + 15) / 16 * C->n_kv_heads >= (1L << 24) ? LAROSA_EUNSUPPORTED : LAROSA_OK;
+}
+
 int check_rotary(const larosa_rotary* r, const larosa_kv4_cache* C) {
   if (!r->table || !aligned(r->table, 16) || !aligned(r->positions, 4) || r->n_positions < 1) return LAROSA_EINVAL;
   if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > C->head_dim) return LAROSA_EINVAL;
@@ -198,7 +205,7 @@ int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_bat
 }
 
 size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int max_len) {
-  if (check_sizes(C) != LAROSA_OK || check_batch(b) != LAROSA_OK || check_heads(C, n_heads) != LAROSA_OK || max_len < 0) return 0;
+  if (check_sizes(C) != LAROSA_OK || check_batch(b) != LAROSA_OK || check_attention(C, b, n_heads) != LAROSA_OK || max_len < 0) return 0;
   return kCounterBytes + round_up(plan_attention(C, b, n_heads, 0, max_len).partial_bytes, 256);
 }
 
@@ -206,7 +213,7 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
                          float scale, int window, int max_len, void* out, int ld_out, void* ws, size_t ws_bytes, void* stream) {
   if (int rc = check_cache(C)) return rc;
   if (int rc = check_batch(b)) return rc;
-  if (int rc = check_heads(C, n_heads)) return rc;
+  if (int rc = check_attention(C, b, n_heads)) return rc;
   if (layer < 0 || layer >= C->n_layers || !q || !out || !aligned(q, 16) || !aligned(out, 16)) return LAROSA_EINVAL;
   const long width = static_cast<long>(n_heads) * C->head_dim;
   if (ld_q < width || ld_q % 8 || ld_out < width || ld_out % 8 || q == out) return LAROSA_EINVAL;
@@ -222,7 +229,6 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   AttentionPlan p = plan_attention(C, b, n_heads, window, max_len);
   const AttentionPlan all = plan_attention(C, b, n_heads, 0, max_len);      // what the workspace is sized for
   if (p.partial_bytes > all.partial_bytes) p = all;
-  if (p.row_tiles * C->n_kv_heads >= (1L << 23)) return LAROSA_EUNSUPPORTED;      // workgroups along one side of a launch
   a.tile_rows = p.tile_rows;
   a.chunk = p.chunk; a.splits = p.splits; a.partial_rows = p.partial_rows;
   a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
@@ -276,14 +282,15 @@ int larosa_kv4_copy_pages(const larosa_kv4_cache* C, const int32_t* src, const i
 
 namespace {
 
-// Whether a layer, a cache and a batch fit together (the layer's own checks are its calls').
+// Whether a layer, a cache and a batch fit together, for all four steps.
 int check_layer_cache(const larosa_layer* L, const larosa_kv4_cache* C, const larosa_kv4_batch* b) {
   if (!L) return LAROSA_EINVAL;
   if (int rc = check_sizes(C)) return rc;
   if (int rc = check_batch(b)) return rc;
   if (L->head_dim != C->head_dim || L->dtype != C->dtype || L->d_kv != C->n_kv_heads * C->head_dim || L->d_q % C->head_dim)
     return LAROSA_EINVAL;
-  return check_heads(C, L->d_q / C->head_dim);
+  if (int rc = check_attention(C, b, L->d_q / C->head_dim)) return rc;
+  return check_layer_rows(L, b->n_rows);
 }
 
 // What the three steps use one after the other; q|k|v, the shortcut and the attention's output lie behind it.
@@ -316,10 +323,6 @@ int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, i
   if (rotary)
     if (int rc = check_rotary(rotary, C)) return rc;
   const size_t need = larosa_layer_kv4_workspace_bytes(L, C, b, max_len);
-  if (!need) {                // the layer is at fault: its own call says how, before it looks at a workspace
-    const int rc = larosa_layer_qkv(L, x, x_out, x_out, b->n_rows, nullptr, nullptr, 0, stream);
-    return rc == LAROSA_OK || rc == LAROSA_EWORKSPACE ? LAROSA_EINVAL : rc;
-  }
   if (!ws || !aligned(ws, 256) || ws_bytes < need) return LAROSA_EWORKSPACE;
   const size_t head = shared_scratch(L, C, b, max_len), rows = b->n_rows;
   const int d_qkv = L->d_q + 2 * L->d_kv, heads = L->d_q / C->head_dim;

@@ -170,6 +170,40 @@ def test_layer_with_cache_refuses(lib):
     assert call(L=layer(attn_mode=1)) == api.EUNSUPPORTED
 
 
+def test_layer_with_cache_refuses_rows_before_anything_is_enqueued(lib):
+    """More rows than the layer's projections have counters for (4096, one for each 32 rows and 128 columns), and more attention
+    tiles than a launch has workgroups: refused by the size query and by the call, which with these addresses could enqueue nothing."""
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+    big = dict(d=4096, d_q=4096, d_kv=1024, d_ff=14336, head_dim=128, K1=2000, K2=2000, K3=2000, K4=7000, Wqkv=FAKE, Wo=FAKE, Wgu=FAKE,
+               Wdown=FAKE, rms_eps=1e-5, dtype=1)
+    small = dict(big, d=256, d_q=512, d_kv=256, d_ff=704, K1=100, K2=100, K3=100, K4=300)
+    C8, C2 = cache(n_kv_heads=8), cache()
+
+    def both(L, C, n):
+        L, b = api._Layer(**L), batch(starts=FAKE, n_seq=1, n_rows=n, max_new=n)
+        size = lib.larosa_layer_kv4_workspace_bytes(ref(L), ref(C), ref(b), 0)
+        rc = [lib.larosa_layer_forward_kv4(ref(L), ref(C), 0, ref(b), None, 1.0, 0, 0, FAKE, OTHER, None, FAKE, BIG, None)] if not size else []
+        if rc:                        # and the layer's own calls that reach the projection at fault
+            rc += [lib.larosa_layer_forward(ref(L), FAKE, OTHER, n, None, FAKE, BIG, None),
+                   lib.larosa_layer_after_attention(ref(L), FAKE, FAKE, OTHER, n, None, FAKE, BIG, None)]
+        return size, rc
+
+    # gate|up: 224 strips of 128 columns, 18 groups of 32 rows; with a shortcut adapter 256 strips, 16 groups
+    for L, C, most in ((big, C8, 576), (dict(big, shortcut_mlp=FAKE), C8, 512), (small, C2, 32 * (4096 // 11))):
+        assert both(L, C, most)[0] > 0 and both(L, C, 1)[0] > 0
+        for n in (most + 1, most + 40, 16384):
+            assert both(L, C, n) == (0, [api.EUNSUPPORTED] * 3), n
+    assert both(small, C2, 65536) == (0, [api.EINVAL] * 3)
+    # tiles of 16 rows times key/value heads: below 2^24
+    wide, C1 = dict(small, d_q=16384, d_kv=64, head_dim=64), cache(n_kv_heads=1, head_dim=64)
+    b = lambda most: batch(starts=FAKE, n_seq=1, n_rows=8, max_new=most)                  # noqa: E731
+    assert lib.larosa_layer_kv4_workspace_bytes(ref(api._Layer(**wide)), ref(C1), ref(b(1 << 18)), 0) > 0
+    wide["d_q"] = 32768
+    assert lib.larosa_kv4_attention_workspace_bytes(ref(C1), ref(b(1 << 18)), 1024, 0) == 0
+    assert lib.larosa_kv4_attention(ref(C1), 0, ref(b(1 << 18)), FAKE, 65536, 1024, 1.0, 0, 0, OTHER, 65536, FAKE, BIG, None) == api.EUNSUPPORTED
+
+
 def test_binding_refuses():
     import torch
     from paper_2507_01299_amd import api
