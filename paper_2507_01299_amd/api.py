@@ -380,6 +380,24 @@ def layer_after_attention(layer: Layer, residual, attn, x_out, ws: Workspace, tr
     return x_out
 
 
+def _list(t, n, device):
+    """Address of a list for the 4-bit cache (None: none): anything but n int32 in a row on the cache's device would be misread there."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"a list of {n} contiguous int32 on the cache's device")
+    return t.data_ptr()
+
+
+def _word(t, device):
+    """Address of the one int32 that a call reports to."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < 1 or t.get_device() != device:
+        raise ValueError("an int32 on the cache's device")
+    return t.data_ptr()
+
+
 class KvCache:
     """Device tensors of a 4-bit key/value cache and the matching C struct.  Tensors that are not given are allocated, and the
     cache is then made empty; given ones are taken as they are (all of refs, table and length, or none)."""
@@ -406,6 +424,9 @@ class KvCache:
             raise ValueError("refs [n_pages], table [n_slots, max_pages], length [n_slots], data of larosa_kv4_data_bytes")
         if any(t.dtype != torch.int32 for t in (refs, table, length)) or not all(t.is_contiguous() for t in (data, refs, table, length)):
             raise ValueError("refs, table and length are contiguous int32 tensors, data is contiguous")
+        self.device = refs.get_device()      # (as a number: all of a call's tensors are compared with it)
+        if any(t.get_device() != self.device for t in (data, table, length)):
+            raise ValueError("refs, table, length and data lie on one device")
         self.data, self.refs, self.table, self.length = data, refs, table, length
         self.c.data, self.c.refs, self.c.table, self.c.length = (t.data_ptr() for t in (data, refs, table, length))
         self.ref = ctypes.byref(self.c)
@@ -418,11 +439,10 @@ class KvBatch:
     row for each sequence), max_new the most of one sequence."""
 
     def __init__(self, slots, n_rows: int, starts=None, max_new: int = 1):
-        if slots.dtype != torch.int32 or (starts is not None and (starts.dtype != torch.int32 or starts.numel() != slots.numel() + 1)):
-            raise ValueError("slots [n_seq] and starts [n_seq + 1] are int32")
+        self.device, n_seq = slots.get_device(), slots.numel()
         self.tensors = (slots, starts)       # keep alive
         self.n_rows = n_rows
-        self.c = _KvBatch(_ptr(slots), _ptr(starts), slots.numel(), n_rows, max_new)
+        self.c = _KvBatch(_list(slots, n_seq, self.device), _list(starts, n_seq + 1, self.device), n_seq, n_rows, max_new)
         self.ref = ctypes.byref(self.c)
 
 
@@ -494,32 +514,36 @@ def kv4_pages_workspace(cache: KvCache, device="cuda:0") -> Workspace:
 
 def kv4_grow(cache: KvCache, slots, status, ws: Workspace, counts=None):
     """Room for counts (default one) more tokens in every listed slot; status [1] int32: 0, pages missing, or -1."""
-    _check(lib().larosa_kv4_grow(cache.ref, _ptr(slots), _ptr(counts), slots.numel(), _ptr(status), ws.ptr, ws.nbytes,
+    n, dev = slots.numel(), cache.device
+    _check(lib().larosa_kv4_grow(cache.ref, _list(slots, n, dev), _list(counts, n, dev), n, _word(status, dev), ws.ptr, ws.nbytes,
                                  _stream()), "larosa_kv4_grow")
     return status
 
 
 def kv4_fork(cache: KvCache, src, dst, status):
     """The sequences of src into the free slots dst, all pages shared; status [1] int32: 0 or -1."""
-    _check(lib().larosa_kv4_fork(cache.ref, _ptr(src), _ptr(dst), src.numel(), _ptr(status), _stream()),
+    n, dev = src.numel(), cache.device
+    _check(lib().larosa_kv4_fork(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _word(status, dev), _stream()),
            "larosa_kv4_fork")
     return status
 
 
 def kv4_trim(cache: KvCache, slots, keep=None):
     """Listed slots keep their first keep tokens (default none)."""
-    _check(lib().larosa_kv4_trim(cache.ref, _ptr(slots), _ptr(keep), slots.numel(), _stream()), "larosa_kv4_trim")
+    n, dev = slots.numel(), cache.device
+    _check(lib().larosa_kv4_trim(cache.ref, _list(slots, n, dev), _list(keep, n, dev), n, _stream()), "larosa_kv4_trim")
 
 
 def kv4_compact(cache: KvCache, live, ws: Workspace):
     """Pages in use to the lowest ids; live [1] int32 (or None) receives their number."""
-    _check(lib().larosa_kv4_compact(cache.ref, _ptr(live), ws.ptr, ws.nbytes, _stream()), "larosa_kv4_compact")
+    _check(lib().larosa_kv4_compact(cache.ref, _word(live, cache.device), ws.ptr, ws.nbytes, _stream()), "larosa_kv4_compact")
     return live
 
 
 def kv4_copy_pages(cache: KvCache, src, dst):
     """Pages src of every layer into pages dst."""
-    _check(lib().larosa_kv4_copy_pages(cache.ref, _ptr(src), _ptr(dst), src.numel(), _stream()), "larosa_kv4_copy_pages")
+    n, dev = src.numel(), cache.device
+    _check(lib().larosa_kv4_copy_pages(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _stream()), "larosa_kv4_copy_pages")
 
 
 def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: int = 0, device="cuda:0") -> Workspace:

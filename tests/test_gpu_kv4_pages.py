@@ -293,3 +293,18 @@ def test_trim_that_keeps_more_than_there_is(gpu_device):
     t.trim([1, 1, 4, 2], [2 ** 31 - 1, 40, 2 ** 31 - 1, 2 ** 31 - 2])
     t.trim([0, 3], [2 ** 31 - 32, -2 ** 31])
     assert t.cache.length.tolist() == [70, 40, 32, 0, 0, 0]
+
+
+def test_binding_refuses_lists_on_another_device(gpu_device):
+    from paper_2507_01299_amd import api
+    c = api.KvCache(1, 4, 32, 4, 1, 1, 64, "f16")
+    here, status = torch.tensor([0], dtype=torch.int32), torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    ws = api.kv4_pages_workspace(c)
+    for call in (lambda: api.kv4_trim(c, here), lambda: api.kv4_trim(c, here.cuda(), here), lambda: api.kv4_grow(c, here, status, ws),
+                 lambda: api.kv4_grow(c, here.cuda(), status.cpu(), ws), lambda: api.kv4_fork(c, here, here.cuda() + 1, status),
+                 lambda: api.kv4_copy_pages(c, here.cuda(), here), lambda: api.kv4_compact(c, status.cpu(), ws),
+                 lambda: api.KvBatch(here.cuda(), 2, starts=here.new_zeros(2))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        api.KvCache(1, 4, 32, 4, 1, 1, 64, "f16", data=c.data, refs=c.refs, table=c.table.cpu(), length=c.length)

@@ -230,3 +230,35 @@ def test_binding_refuses():
                  lambda: api.kv4_attention(c, 0, b, enough, 2, turned, None), lambda: api.layer_forward_kv4(None, c, 0, b, few, enough, None)):
         with pytest.raises(ValueError):
             call()
+
+
+def cpu_cache(api):
+    import torch
+    z = torch.zeros(4, dtype=torch.int32)
+    return api.KvCache(1, 4, 32, 4, 1, 1, 64, "f16", data=torch.zeros(4 * 32 * 68, dtype=torch.uint8), refs=z, table=z.clone(), length=z.clone())
+
+
+def test_binding_refuses_lists_that_the_device_would_misread(lib):
+    """64-bit, floating or strided lists, partners of another length, a status that is no int32."""
+    import torch
+    from paper_2507_01299_amd import api
+    c = cpu_cache(api)
+    ws = type("Ws", (), dict(ptr=FAKE, nbytes=BIG))
+    good, status = torch.tensor([0, 1], dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    lists = [good.long(), good.short(), good.float(), torch.zeros(4, dtype=torch.int32)[::2]]
+    partners = lists + [good[:1], torch.zeros(3, dtype=torch.int32)]
+    calls = []
+    for bad in lists:
+        calls += [lambda t=bad: api.kv4_trim(c, t), lambda t=bad: api.kv4_grow(c, t, status, ws), lambda t=bad: api.kv4_fork(c, t, good, status),
+                  lambda t=bad: api.kv4_copy_pages(c, t, good), lambda t=bad: api.KvBatch(t, 2)]
+    for bad in partners:
+        calls += [lambda t=bad: api.kv4_trim(c, good, t), lambda t=bad: api.kv4_grow(c, good, status, ws, t),
+                  lambda t=bad: api.kv4_fork(c, good, t, status), lambda t=bad: api.kv4_copy_pages(c, good, t)]
+    for bad in (torch.zeros(4, dtype=torch.int32)[::2], torch.zeros(4, dtype=torch.int32), torch.zeros(3)):
+        calls.append(lambda t=bad: api.KvBatch(good, 2, starts=t))
+    for bad in (status.long(), status[:0], status.float()):
+        calls += [lambda t=bad: api.kv4_grow(c, good, t, ws), lambda t=bad: api.kv4_fork(c, good, good, t), lambda t=bad: api.kv4_compact(c, t, ws)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    api.KvBatch(good, 2, starts=torch.zeros(3, dtype=torch.int32))
