@@ -404,7 +404,7 @@ class KvCache:
 
     def __init__(self, n_layers, n_pages, page_tokens, n_slots, max_pages, n_kv_heads, head_dim, dtype, data=None, refs=None,
                  table=None, length=None, device="cuda:0"):
-        self.dtype = dtype_code(dtype)
+        self.dtype, self.torch_dtype = dtype_code(dtype), torch_dtype(dtype)
         self.c = _KvCache(n_layers, n_pages, page_tokens, n_slots, max_pages, n_kv_heads, head_dim, self.dtype)
         nbytes = lib().larosa_kv4_data_bytes(ctypes.byref(self.c))
         if nbytes == 0:
@@ -458,18 +458,30 @@ class Rotary:
         if table.dtype != torch.float32 or not table.is_contiguous() or (
                 positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous())):
             raise ValueError("table [n_positions, rot_dim] is contiguous float32, positions [n_axes, n_rows] contiguous int32")
-        self.n_rows = None if positions is None else positions.shape[1]
+        self.device, self.n_rows = table.get_device(), None if positions is None else positions.shape[1]
+        if positions is not None and positions.get_device() != self.device:
+            raise ValueError("table and positions lie on one device")
         self.c = _Rotary(_ptr(table), table.shape[0], table.shape[1], int(interleaved), _ptr(positions), n_axes)
         for k, n in enumerate(axis_pairs or ()):
             self.c.axis_pairs[k] = n
         self.ref = ctypes.byref(self.c)
 
 
-def _row_stride(t, n_rows: int) -> int:
+def _rows(t, n_rows: int, cache) -> int:
+    """Distance between the rows of a tensor of the cache's type; anything else would be misread on the device."""
+    if t.dtype is not cache.torch_dtype or t.get_device() != cache.device:
+        raise ValueError("rows are of the cache's type and on its device")
     ld, one = t.stride()
     if one != 1 or t.shape[0] < n_rows:
         raise ValueError(f"a tensor of at least {n_rows} rows, whose values lie next to one another")
     return ld
+
+
+def _check_batch(cache, batch, rotary=None):
+    if batch.device != cache.device or (rotary is not None and rotary.device != cache.device):
+        raise ValueError("batch and rotary positions lie on the cache's device")
+    if rotary is not None and rotary.n_rows is not None and rotary.n_rows != batch.n_rows:
+        raise ValueError("positions have a column for every row of the batch")
 
 
 def kv4_clear(cache: KvCache):
@@ -478,10 +490,9 @@ def kv4_clear(cache: KvCache):
 
 def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, out=None, rotary: Rotary | None = None):
     """The rows' new keys and values into the cache; out (may be qkv) receives q as turned and k, v as stored."""
-    if rotary is not None and rotary.n_rows is not None and rotary.n_rows != batch.n_rows:
-        raise ValueError("positions have a column for every row of the batch")
-    ld_qkv = _row_stride(qkv, batch.n_rows)
-    ld_out = 0 if out is None else _row_stride(out, batch.n_rows)
+    _check_batch(cache, batch, rotary)
+    ld_qkv = _rows(qkv, batch.n_rows, cache)
+    ld_out = 0 if out is None else _rows(out, batch.n_rows, cache)
     _check(lib().larosa_kv4_append(cache.ref, layer, batch.ref, _ptr(qkv), ld_qkv, n_heads,
                                    rotary.ref if rotary is not None else None, _ptr(out), ld_out,
                                    _stream()), "larosa_kv4_append")
@@ -501,7 +512,8 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
     1 / sqrt(head_dim)."""
     if scale is None:
         scale = cache.c.head_dim ** -0.5
-    ld_q, ld_out = _row_stride(q, batch.n_rows), _row_stride(out, batch.n_rows)
+    _check_batch(cache, batch)
+    ld_q, ld_out = _rows(q, batch.n_rows, cache), _rows(out, batch.n_rows, cache)
     _check(lib().larosa_kv4_attention(cache.ref, layer, batch.ref, _ptr(q), ld_q, n_heads, scale,
                                       window, max_len, _ptr(out), ld_out, ws.ptr, ws.nbytes, _stream()),
            "larosa_kv4_attention")
@@ -556,10 +568,11 @@ def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: i
 def layer_forward_kv4(layer: Layer, cache: KvCache, index: int, batch: KvBatch, x, x_out, ws: Workspace, rotary: Rotary | None = None,
                       scale: float | None = None, window: int = 0, max_len: int = 0, trace: dict | None = None):
     """A decoder layer whose attention runs over layer `index` of the cache; the rows' tokens are counted in the lengths."""
-    if rotary is not None and rotary.n_rows is not None and rotary.n_rows != batch.n_rows:
-        raise ValueError("positions have a column for every row of the batch")
-    if x.shape[0] != batch.n_rows or x_out.shape[0] != batch.n_rows:
-        raise ValueError("x and x_out have the batch's rows")
+    _check_batch(cache, batch, rotary)
+    for t in (x, x_out):
+        _rows(t, batch.n_rows, cache)
+        if tuple(t.shape) != (batch.n_rows, layer.c.d) or not t.is_contiguous():
+            raise ValueError("x and x_out [n_rows of the batch, d of the layer] are contiguous")
     if scale is None:
         scale = cache.c.head_dim ** -0.5
     tr = _trace_struct(trace)

@@ -308,3 +308,20 @@ def test_binding_refuses_lists_on_another_device(gpu_device):
             call()
     with pytest.raises(ValueError):
         api.KvCache(1, 4, 32, 4, 1, 1, 64, "f16", data=c.data, refs=c.refs, table=c.table.cpu(), length=c.length)
+
+
+def test_binding_refuses_rows_on_another_device(gpu_device):
+    from paper_2507_01299_amd import api
+    c = api.KvCache(1, 4, 32, 4, 1, 1, 64, "f16")
+    slots = torch.tensor([0], dtype=torch.int32)
+    batch, away = api.KvBatch(slots.cuda(), 1), api.KvBatch(slots, 1)
+    rows, table = torch.zeros(1, 192, dtype=torch.float16), torch.zeros(8, 64)
+    ws = api.kv4_attention_workspace(c, batch, 1)
+    for call in (lambda: api.kv4_append(c, 0, batch, rows, 1), lambda: api.kv4_append(c, 0, batch, rows.cuda(), 1, out=rows),
+                 lambda: api.kv4_append(c, 0, away, rows.cuda(), 1),
+                 lambda: api.kv4_append(c, 0, batch, rows.cuda(), 1, out=rows.cuda(), rotary=api.Rotary(table)),
+                 lambda: api.Rotary(table.cuda(), positions=slots[None]),
+                 lambda: api.kv4_attention(c, 0, batch, rows, 1, rows.cuda(), ws), lambda: api.kv4_attention(c, 0, batch, rows.cuda(), 1, rows, ws),
+                 lambda: api.kv4_attention(c, 0, away, rows.cuda(), 1, rows.cuda(), ws)):
+        with pytest.raises(ValueError):
+            call()

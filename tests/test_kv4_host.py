@@ -262,3 +262,23 @@ def test_binding_refuses_lists_that_the_device_would_misread(lib):
         with pytest.raises(ValueError):
             call()
     api.KvBatch(good, 2, starts=torch.zeros(3, dtype=torch.int32))
+
+
+def test_binding_refuses_rows_of_another_type(lib):
+    """Rows of another 16-bit type than the cache's, or of 32 bits; a layer's rows that are not dense."""
+    import torch
+    from paper_2507_01299_amd import api
+    c = cpu_cache(api)
+    b = api.KvBatch(torch.tensor([0, 1, 2], dtype=torch.int32), 3)
+    good = torch.zeros(3, 256, dtype=torch.float16)
+    layer = type("L", (), dict(c=api._Layer(d=256)))
+    for bad in (good.bfloat16(), good.float(), good.view(torch.int16)):
+        for call in (lambda: api.kv4_append(c, 0, b, bad, 2), lambda: api.kv4_append(c, 0, b, good, 2, out=bad),
+                     lambda: api.kv4_attention(c, 0, b, bad, 2, good, None), lambda: api.kv4_attention(c, 0, b, good, 2, bad, None),
+                     lambda: api.layer_forward_kv4(layer, c, 0, b, bad, good, None), lambda: api.layer_forward_kv4(layer, c, 0, b, good, bad, None)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (torch.zeros(3, 512, dtype=torch.float16)[:, :256], torch.zeros(3, 264, dtype=torch.float16), good.T.contiguous().T):
+        for call in (lambda: api.layer_forward_kv4(layer, c, 0, b, bad, good, None), lambda: api.layer_forward_kv4(layer, c, 0, b, good, bad, None)):
+            with pytest.raises(ValueError):
+                call()
