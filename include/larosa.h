@@ -402,6 +402,12 @@ int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, i
  * Returns LAROSA_EINVAL for an unknown key or a value out of range. */
 int larosa_set_tuning(int key, int value);
 
+/* How larosa_kv4_attention would divide a call (host only): plan[0] = rows of a tile (16 or 32), [1] = tiles of a key/value head's
+ * rows, [2] = blocks of 32 tokens that a workgroup takes at most, unless it is a tile's last, [3] = most workgroups of a tile, [4] = floats that
+ * each of them leaves where there are several.  Pointers of the cache and the batch's starts are not followed. */
+int larosa_kv4_attention_plan(const larosa_kv4_cache* C, const larosa_kv4_batch* batch, int n_heads, int window, int max_len,
+                              int* plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -110,6 +110,7 @@ def lib() -> ctypes.CDLL:
         L.larosa_kv4_attention_workspace_bytes.restype = sz
         L.larosa_kv4_attention_workspace_bytes.argtypes = [cache, batch, i, i]
         L.larosa_kv4_attention.argtypes = [cache, i, batch, vp, i, i, ctypes.c_float, i, i, vp, i, vp, sz, vp]
+        L.larosa_kv4_attention_plan.argtypes = [cache, batch, i, i, i, ctypes.POINTER(i)]
         L.larosa_kv4_pages_workspace_bytes.restype = sz
         L.larosa_kv4_pages_workspace_bytes.argtypes = [cache]
         L.larosa_kv4_grow.argtypes = [cache, vp, vp, i, vp, vp, sz, vp]
@@ -518,6 +519,13 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
                                       window, max_len, _ptr(out), ld_out, ws.ptr, ws.nbytes, _stream()),
            "larosa_kv4_attention")
     return out
+
+
+def kv4_attention_plan(cache: KvCache, batch: KvBatch, n_heads: int, window: int = 0, max_len: int = 0) -> dict:
+    """How kv4_attention would divide the call (for tests and experiments; not part of the stable interface)."""
+    plan = (ctypes.c_int * 5)()
+    _check(lib().larosa_kv4_attention_plan(cache.ref, batch.ref, n_heads, window, max_len, plan), "larosa_kv4_attention_plan")
+    return dict(zip(("tile_rows", "row_tiles", "chunk", "splits", "sums"), plan))
 
 
 def kv4_pages_workspace(cache: KvCache, device="cuda:0") -> Workspace:

@@ -581,7 +581,7 @@ __device__ __forceinline__ Tile find_tile(const Kv4AttentionArgs& a, const Seque
 __device__ __forceinline__ float* split_sums(const Kv4AttentionArgs& a, int s, int unit_in_seq, int split, int D) {
   const unsigned row_tiles = (a.max_new * a.group + a.tile_rows - 1) / a.tile_rows;
   const size_t unit = static_cast<size_t>(s) * row_tiles * a.n_kv_heads + unit_in_seq;
-  return a.partial + (unit * a.splits + split) * (static_cast<size_t>(a.partial_rows) * (D + 2));
+  return a.partial + (unit * a.splits + split) * kv4_sums_floats(a.partial_rows, D);
 }
 
 // Waves of each SIMD that the registers are shared out for.
@@ -732,7 +732,7 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttentionArgs a) {
   const int n = blockIdx.z * (4 / WR) + wave / WR;            // row of the tile
   const int first = wave % WR;
   // what a split of the plan may have left is read before it is known whether it did: the length takes as long to come
-  const size_t stride = static_cast<size_t>(a.partial_rows) * (D + 2) * WR;
+  const size_t stride = static_cast<size_t>(kv4_sums_floats(a.partial_rows, D)) * WR;
   const float* sums = split_sums(a, blockIdx.y, unit, first, D);
   float ref = -INFINITY, total = 0.f;
   const int most = n < static_cast<int>(a.partial_rows) ? (a.splits - first + WR - 1) / WR : 0;

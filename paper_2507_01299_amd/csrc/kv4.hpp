@@ -47,7 +47,7 @@ struct Kv4AttentionArgs {
   const int32_t *table, *length, *slots, *starts;
   const uint16_t* q;
   uint16_t* out;
-  float* partial;             // [n_seq][row tiles * n_kv_heads][splits][partial_rows * (head_dim + 2)] fp32
+  float* partial;             // [n_seq][row tiles * n_kv_heads][splits][kv4_sums_floats] fp32
   int n_pages, max_pages, n_rows, ld_q, ld_out;
   int group;                  // query heads of a key/value head
   int window;                 // 0: none
@@ -57,6 +57,8 @@ struct Kv4AttentionArgs {
   uint32_t max_new : 19, page_shift : 4, tile_rows : 6;       // tile: 16 or 32 (new token, query head of the group) pairs
   uint32_t splits : 10, partial_rows : 6;      // partial_rows: rows that a tile can have
 };
+// Floats of one split's sums: rows of head_dim, the rows' references and totals; whole 16-byte pieces, which is how they are moved.
+__host__ __device__ constexpr int kv4_sums_floats(int partial_rows, int head_dim) { return (partial_rows * (head_dim + 2) + 3) / 4 * 4; }
 hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, Kv4Kind kind, int n_seq, int row_tiles, hipStream_t s);
 constexpr int kKv4SplitsMax = 256;            // that one row's sums are joined from
 

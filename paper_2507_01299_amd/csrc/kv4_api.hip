@@ -119,8 +119,14 @@ AttentionPlan plan_attention(const larosa_kv4_cache* C, const larosa_kv4_batch* 
   const long splits = (blocks + chunk - 1) / chunk;
   p.chunk = static_cast<int>(chunk);
   p.splits = static_cast<int>(splits);
-  p.partial_bytes = splits > 1 ? static_cast<size_t>(p.units) * splits * p.partial_rows * (C->head_dim + 2) * 4 : 0;
+  p.partial_bytes = splits > 1 ? static_cast<size_t>(p.units) * splits * kv4_sums_floats(p.partial_rows, C->head_dim) * 4 : 0;
   return p;
+}
+
+// The plan of a call: a window's own only where the workspace, which is sized without it, suffices.
+AttentionPlan plan_call(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int window, int max_len) {
+  const AttentionPlan p = plan_attention(C, b, n_heads, window, max_len), all = plan_attention(C, b, n_heads, 0, max_len);
+  return p.partial_bytes > all.partial_bytes ? all : p;
 }
 
 Kv4Scratch scratch_of(void* ws) { return Kv4Scratch{reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kCounterBytes)}; }
@@ -226,13 +232,25 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.window = window;
-  AttentionPlan p = plan_attention(C, b, n_heads, window, max_len);
-  const AttentionPlan all = plan_attention(C, b, n_heads, 0, max_len);      // what the workspace is sized for
-  if (p.partial_bytes > all.partial_bytes) p = all;
+  const AttentionPlan p = plan_call(C, b, n_heads, window, max_len);
   a.tile_rows = p.tile_rows;
   a.chunk = p.chunk; a.splits = p.splits; a.partial_rows = p.partial_rows;
   a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes);
   return status_of(launch_kv4_attention(a, kind_of(C), b->n_seq, static_cast<int>(p.row_tiles), stream_of(stream)));
+}
+
+int larosa_kv4_attention_plan(const larosa_kv4_cache* C, const larosa_kv4_batch* b, int n_heads, int window, int max_len, int* plan) {
+  if (int rc = check_sizes(C)) return rc;
+  if (int rc = check_batch(b)) return rc;
+  if (int rc = check_attention(C, b, n_heads)) return rc;
+  if (window < 0 || max_len < 0 || !plan) return LAROSA_EINVAL;
+  const AttentionPlan p = plan_call(C, b, n_heads, window, max_len);
+  plan[0] = p.tile_rows;
+  plan[1] = static_cast<int>(p.row_tiles);
+  plan[2] = p.chunk;
+  plan[3] = p.splits;
+  plan[4] = kv4_sums_floats(p.partial_rows, C->head_dim);
+  return LAROSA_OK;
 }
 
 // ---- pages ---------------------------------------------------------------------------------------

@@ -282,3 +282,30 @@ def test_binding_refuses_rows_of_another_type(lib):
         for call in (lambda: api.layer_forward_kv4(layer, c, 0, b, bad, good, None), lambda: api.layer_forward_kv4(layer, c, 0, b, good, bad, None)):
             with pytest.raises(ValueError):
                 call()
+
+
+def plan_of(lib, C, b, heads, window=0, max_len=0):
+    plan = (ctypes.c_int * 5)()
+    assert lib.larosa_kv4_attention_plan(ctypes.byref(C), ctypes.byref(b), heads, window, max_len, plan) == 0
+    return dict(zip(("tile_rows", "row_tiles", "chunk", "splits", "sums"), plan))
+
+
+def test_sums_of_splits_start_at_16_bytes(lib):
+    """Each split's sums are moved 16 bytes at a time: whole pieces for any number of rows, and the workspace holds all of them."""
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+    for D in (64, 128, 256):
+        for kv, group, new in ((1, 1, 1), (4, 7, 1), (2, 1, 3), (1, 3, 5), (8, 4, 1), (1, 5, 3), (2, 3, 9), (1, 1, 31), (1, 4, 100)):
+            for seqs, most in ((1, 2000), (3, 900), (40, 300)):
+                C = cache(n_kv_heads=kv, head_dim=D, max_pages=most, n_pages=1 << 20, n_slots=64)
+                b = batch(starts=FAKE, n_seq=seqs, n_rows=seqs * new, max_new=new)
+                p = plan_of(lib, C, b, kv * group)
+                rows = min(new * group, p["tile_rows"])
+                assert p["row_tiles"] == -(-new * group // p["tile_rows"])
+                assert p["sums"] % 4 == 0 and rows * (D + 2) <= p["sums"] < rows * (D + 2) + 4
+                left = p["row_tiles"] * kv * seqs * p["splits"] * p["sums"] * 4 if p["splits"] > 1 else 0
+                assert lib.larosa_kv4_attention_workspace_bytes(ref(C), ref(b), kv * group, 0) >= (1 << 20) + left
+    bad = (ctypes.c_int * 5)()
+    for args in ((None, ref(batch()), 8, 0, 0, bad), (ref(cache()), ref(batch(n_seq=0)), 8, 0, 0, bad), (ref(cache()), ref(batch()), 7, 0, 0, bad),
+                 (ref(cache()), ref(batch()), 8, -1, 0, bad), (ref(cache()), ref(batch()), 8, 0, -1, bad), (ref(cache()), ref(batch()), 8, 0, 0, None)):
+        assert lib.larosa_kv4_attention_plan(*args) == api.EINVAL
