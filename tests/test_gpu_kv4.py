@@ -215,12 +215,18 @@ def chosen_tokens(rng, dtype, keys, values, page=64):
     then the query's first value times keys[t] times the scale."""
     n, D = values.shape
     C, slots = U.random_cache(rng, [n], page, 1, D, dtype)
+    quantised = {}
     for t in range(n):
         block = C.block(0, slots[0], t, 0)
         k = np.zeros(D)
         k[0] = keys[t]
-        K.write_token(block, D, t % 32, 0, *K.quantise(k, dtype))
-        K.write_token(block, D, t % 32, 1, *K.quantise(values[t], dtype))
+        for which, x in ((0, k), (1, values[t])):
+            if x.tobytes() not in quantised:
+                quantised[x.tobytes()] = K.quantise(x, dtype)
+            codes, scales = quantised[x.tobytes()]
+            at, _, sc = K._places(D, which)           # two neighbouring values to a byte
+            block[at[t % 32, ::2]] = codes[::2] | codes[1::2] << 4
+            block[sc[t % 32]] = scales
     return C, slots
 
 
@@ -257,6 +263,100 @@ def test_attention_weights_that_round_alike(gpu_device, dtype, n):
         scale = np.log(2.0 ** octaves * (1 + 0.495 * step))
         got = check_attention(C, slots, None, O.encode16(q, dtype), 1, scale=scale)
         assert np.array_equal(got[0, 0], values[0])
+
+
+# ---- every way in which a call is divided: tiles of 16 and 32 rows, alone and several, whole and split, with and without a window ----
+
+def plan_of(C, slots, starts, n_rows, n_heads, max_new=1, window=0, max_len=0):
+    from paper_2507_01299_amd import api
+    batch = api.KvBatch(U.int32(slots), n_rows, starts=U.int32(starts), max_new=max_new)
+    return api.kv4_attention_plan(U.device_cache(C), batch, n_heads, window, max_len)
+
+
+def real_splits(C, slots, plan, window=0):
+    """Workgroups that the longest sequence's last tile is divided among (at least: a window may begin inside a block)."""
+    longest = max(int(C.length[s]) for s in slots)
+    return min(plan["splits"], -(-(-(-(min(longest, window) if window else longest) // 32)) // plan["chunk"]))
+
+
+@pytest.mark.parametrize("dtype,D,heads,kv,news,window,row_tiles", [
+    ("bf16", 128, 16, 4, [7, 1, 5, 7, 2, 7, 3, 7], 0, 1),             # 28 rows: one tile, 28 rows of sums
+    ("f16", 64, 4, 4, [17, 16, 3, 17, 9, 17, 1, 17], 0, 1),           # 17: one row in the tile's second half
+    ("f16", 128, 8, 4, [16, 16, 15, 16, 1, 16, 8, 16], 0, 1),         # 32: a full tile
+    ("bf16", 64, 24, 4, [7, 6, 7, 5, 1, 7, 7, 3], 0, 2),              # 42: two tiles
+    ("f16", 128, 16, 4, [9, 9, 1, 9, 4, 9, 9, 9], 0, 2),              # 36
+])
+def test_attention_split_tiles_of_32_rows(gpu_device, dtype, D, heads, kv, news, window, row_tiles):
+    rng = np.random.default_rng(D + heads + len(news))
+    lengths = [3000, 2047, 40, 1025, 9, 2600, 700, 1500]
+    lengths = [max(n, k) for n, k in zip(lengths, news)]
+    C, slots = U.random_cache(rng, lengths, 256, kv, D, dtype, headroom=33000)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    plan = plan_of(C, slots, starts, int(starts[-1]), heads, max(news), max_len=33000)
+    assert (plan["tile_rows"], plan["row_tiles"]) == (32, row_tiles) and real_splits(C, slots, plan) >= 2, plan
+    q = U.random_rows(rng, int(starts[-1]), heads * D, dtype)
+    check_attention(C, slots, starts, q, heads, max_new=max(news), max_len=33000)
+
+
+@pytest.mark.parametrize("dtype,heads,kv,new,row_tiles", [("bf16", 64, 16, 5, 1), ("f16", 32, 8, 9, 2)])
+def test_attention_split_tiles_of_32_rows_with_a_window(gpu_device, dtype, heads, kv, new, row_tiles):
+    rng = np.random.default_rng(heads + new)
+    lengths = [2500, 2100, 2040] + rng.integers(new, 300, 29).tolist()
+    C, slots = U.random_cache(rng, lengths, 256, kv, 64, dtype)
+    starts = np.arange(33) * new
+    plan = plan_of(C, slots, starts, 32 * new, heads, new, window=2000)
+    assert (plan["tile_rows"], plan["row_tiles"]) == (32, row_tiles) and real_splits(C, slots, plan, 2000) >= 2, plan
+    check_attention(C, slots, starts, U.random_rows(rng, 32 * new, heads * 64, dtype), heads, window=2000, max_new=new)
+
+
+@pytest.mark.parametrize("dtype,D,heads,n,least", [("bf16", 64, 3, 66001, 200), ("f16", 128, 1, 66001, 200), ("f16", 256, 5, 25000, 90)])
+def test_attention_many_splits(gpu_device, dtype, D, heads, n, least):
+    """One sequence among up to 256 workgroups: the joining launch takes its sums in several rounds."""
+    rng = np.random.default_rng(D)
+    C, slots = U.random_cache(rng, [n], 256, 1, D, dtype)
+    plan = plan_of(C, slots, None, 1, heads)
+    assert real_splits(C, slots, plan) >= least, plan
+    check_attention(C, slots, None, U.random_rows(rng, 1, heads * D, dtype), heads)
+
+
+@pytest.mark.parametrize("window", [0, 700])
+@pytest.mark.parametrize("max_len", [1, 700, 800, 1500, 100000])
+def test_attention_longer_and_shorter_than_announced(gpu_device, window, max_len):
+    """max_len only divides the work: the last workgroup of a tile takes what is left, those past the end nothing."""
+    rng = np.random.default_rng(27)
+    C, slots = U.random_cache(rng, [3000, 801, 5, 0], 64, 2, 64, "f16")
+    check_attention(C, slots, None, U.random_rows(rng, 4, 6 * 64, "f16"), 6, window=window, max_len=max_len)
+
+
+@pytest.mark.parametrize("dtype,D,heads,kv,n,new,window,tile_rows", [
+    ("bf16", 128, 8, 2, 2300, 1400, 0, 16), ("f16", 64, 6, 2, 2999, 1100, 0, 16), ("bf16", 64, 8, 2, 2500, 2500, 900, 32),
+    ("bf16", 128, 8, 2, 2300, 1900, 0, 32), ("f16", 64, 6, 2, 2999, 1900, 0, 32), ("f16", 256, 2, 1, 700, 450, 0, 16)])
+def test_attention_long_prompts(gpu_device, dtype, D, heads, kv, n, new, window, tile_rows):
+    """Prompts, the longer ones in tiles of 32 rows by their own length, against fp64 in whole matrices."""
+    rng = np.random.default_rng(D + n)
+    C, slots = U.random_cache(rng, [n], 64, kv, D, dtype)
+    q_bits = U.random_rows(rng, new, heads * D, dtype)
+    assert plan_of(C, slots, [0, new], new, heads, new, window)["tile_rows"] == tile_rows
+    got, _ = run_attention(C, slots, [0, new], q_bits, heads, window=window, scale=D ** -0.5, max_new=new)
+    q, group = O.decode16(q_bits, dtype).reshape(new, heads, D), heads // kv
+    place, t = np.arange(n - new, n)[:, None], np.arange(n)[None, :]
+    seen = (t <= place) & ((t > place - window) if window else True)
+    for h in range(heads):
+        k, v, have = K.keys_values(C, 0, slots[0], n, h // group)
+        assert have.all()
+        s = np.where(seen, q[:, h] @ k.T * D ** -0.5, -np.inf)
+        size = np.where(seen, np.abs(q[:, h]) @ np.abs(k).T * D ** -0.5, 0).max(1, keepdims=True)
+        top = s.max(1, keepdims=True)
+        spread = np.where(seen, top - s, 0).max(1, keepdims=True)
+        w = np.exp(s - top)
+        w /= w.sum(1, keepdims=True)
+        out, mag = w @ v, w @ np.abs(v)
+        # the terms of attention_want: a weight's and the store's half step, the logit's and the sums' fp32
+        u = U.HALF_STEP[dtype]
+        logit = (D * size + 3 * (size + spread)) * 2.0 ** -24 + 2.0 ** -22
+        tol = u * np.abs(out) * 1.01 + mag * (u + 2 * (logit + 2 * (n + 8) * 2.0 ** -24)) + 2.0 ** -25
+        err = np.abs(got[:, h] - out)
+        assert (err <= tol).all(), f"head {h}: {(err / tol).max():.2f} of the tolerance"
 
 
 # ---- append ---------------------------------------------------------------------------------------------------

@@ -325,3 +325,53 @@ def test_binding_refuses_rows_on_another_device(gpu_device):
                  lambda: api.kv4_attention(c, 0, away, rows.cuda(), 1, rows.cuda(), ws)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype,shortcut,n", [("f16", True, 2900), ("bf16", False, 2900), ("f16", False, 70)])
+def test_layer_with_one_row(gpu_device, dtype, shortcut, n):
+    """One token at a time, the kernels of a single row: their key histograms and the attention's partial sums lie in one workspace, one
+    after the other.  Three steps through two layers and that workspace, against the split calls with workspaces of their own."""
+    from paper_2507_01299_amd import api
+    rng = np.random.default_rng(51)
+    heads, kv, D = 4, 2, 64
+    built = [small_layer(dtype, 81 + i, shortcut) for i in range(2)]
+    C, slots = U.random_cache(rng, [n], 64, kv, D, dtype, n_layers=2, headroom=8, spare_pages=4)
+    cache = U.device_cache(C)
+    ws, status = api.kv4_pages_workspace(cache), new_status()
+    sl = U.int32(slots)
+    batch = api.KvBatch(sl, 1)
+    angles = np.outer(np.arange(n + 8), 0.9 ** np.arange(32))
+    rotary = api.Rotary(torch.from_numpy(np.concatenate([np.cos(angles), np.sin(angles)], 1).astype(np.float32)).to("cuda:0"))
+    assert (api.kv4_attention_plan(cache, batch, heads)["splits"] > 1) == (n > 1000)
+    whole = api.layer_kv4_workspace(built[0][1], cache, batch)
+    for _ in range(3):
+        api.kv4_grow(cache, sl, status, ws)
+        assert int(status) == 0
+        x = to_dev(U.random_rows(rng, 1, 256, dtype), dtype)
+        for i, (case, layer) in enumerate(built):
+            before = cache.data.clone()
+            x_all = torch.zeros_like(x)
+            api.layer_forward_kv4(layer, cache, i, batch, x, x_all, whole, rotary=rotary)
+            after = cache.data.clone()
+            cache.data.copy_(before)
+            lw, tr = api.Workspace(layer.workspace_bytes(1)), layer.trace_buffers(1)
+            qkv = torch.zeros(1, (heads + 2 * kv) * D, dtype=x.dtype, device="cuda:0")
+            s1 = torch.zeros_like(x) if shortcut else None
+            attn, x_out = torch.zeros(1, heads * D, dtype=x.dtype, device="cuda:0"), torch.zeros_like(x)
+            api.layer_qkv(layer, x, qkv, s1, lw, tr)
+            turned = torch.zeros_like(qkv)
+            api.kv4_append(cache, i, batch, qkv, heads, out=turned, rotary=rotary)
+            api.kv4_attention(cache, i, batch, turned, heads, attn, api.kv4_attention_workspace(cache, batch, heads))
+            api.layer_after_attention(layer, s1 if shortcut else x, attn, x_out, lw, tr)
+            torch.cuda.synchronize()
+            assert torch.equal(x_all.view(torch.int16), x_out.view(torch.int16)) and torch.equal(cache.data, after)
+            tr["qkv"] = qkv
+            if shortcut:
+                tr["s1"] = s1
+            check_layer_trace(case.layer, to_bits(x), tr, x_out, attn_bits=to_bits(attn))
+            C.data = cache.data.cpu().numpy().reshape(C.data.shape)
+            C.table, C.length, C.refs = (t.cpu().numpy() for t in (cache.table, cache.length, cache.refs))
+            q = O.decode16(to_bits(turned[:, :heads * D].contiguous()), dtype).reshape(1, heads, D)
+            o, tol = U.attention_want(C, i, slots, None, q, heads, D ** -0.5, 0, 1)[0]
+            assert (np.abs(O.decode16(to_bits(attn), dtype).reshape(heads, D) - o) <= tol).all()
+            x = x_out
