@@ -83,6 +83,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 //    8191 tokens, 7 new each: 22.9 us; pieces of 24 25.5, of 40 24.6, of 64 27.7), longer ones past 4096 of them (64 sequences of up
 //    to 16384 tokens: 75.5 us; past 2048 80.1).
 constexpr long kWholeBlocks = 24, kLeastBlocks = 8, kPieceBlocks = 32, kResident = 512, kMostWorkgroups = 4096;
+constexpr int kWindowMost = 0x7FFFFFFF - 2 * kKv4NewMax;      // (places with a page are below 2^30)
 struct AttentionPlan {
   int tile_rows;
   long row_tiles, units;      // tiles of a key/value head's rows; such tiles of all sequences
@@ -231,7 +232,8 @@ int larosa_kv4_attention(const larosa_kv4_cache* C, int layer, const larosa_kv4_
   a.q = static_cast<const uint16_t*>(q); a.ld_q = ld_q;
   a.out = static_cast<uint16_t*>(out); a.ld_out = ld_out;
   a.scale_log2 = scale * 1.4426950408889634f;
-  a.window = window;
+  // the kernels take it from the places of a tile's rows, which may lie up to max_new before a sequence's first token
+  a.window = window < kWindowMost ? window : kWindowMost;
   const AttentionPlan p = plan_call(C, b, n_heads, window, max_len);
   a.tile_rows = p.tile_rows;
   a.chunk = p.chunk; a.splits = p.splits; a.partial_rows = p.partial_rows;

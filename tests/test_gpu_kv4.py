@@ -319,6 +319,18 @@ def test_attention_many_splits(gpu_device, dtype, D, heads, n, least):
     check_attention(C, slots, None, U.random_rows(rng, 1, heads * D, dtype), heads)
 
 
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 12, 2 ** 30])
+def test_attention_largest_windows_with_rows_before_the_first_token(gpu_device, window):
+    """More new rows than tokens: the first ones see nothing, the others in the same tile everything, however large the window."""
+    rng = np.random.default_rng(28)
+    C, slots = U.random_cache(rng, [10, 0, 40, 700], 32, 1, 64, "f16")
+    q = U.random_rows(rng, 14 + 5 + 60 + 3, 2 * 64, "f16")
+    starts = [0, 14, 19, 79, 82]
+    got = check_attention(C, slots, starts, q, 2, window=window, max_new=60)
+    assert not got[:4].any() and got[4:14].any((1, 2)).all()
+    assert np.array_equal(got, check_attention(C, slots, starts, q, 2, max_new=60))
+
+
 @pytest.mark.parametrize("window", [0, 700])
 @pytest.mark.parametrize("max_len", [1, 700, 800, 1500, 100000])
 def test_attention_longer_and_shorter_than_announced(gpu_device, window, max_len):
