@@ -478,6 +478,14 @@ def _rows(t, n_rows: int, cache) -> int:
     return ld
 
 
+def _cache_stream(cache):
+    """The current stream; its device has to be the cache's."""
+    device = torch.cuda.current_device()
+    if device != cache.device:
+        raise ValueError("the cache's device is not the current one")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _check_batch(cache, batch, rotary=None):
     if batch.device != cache.device or (rotary is not None and rotary.device != cache.device):
         raise ValueError("batch and rotary positions lie on the cache's device")
@@ -486,7 +494,7 @@ def _check_batch(cache, batch, rotary=None):
 
 
 def kv4_clear(cache: KvCache):
-    _check(lib().larosa_kv4_clear(cache.ref, _stream()), "larosa_kv4_clear")
+    _check(lib().larosa_kv4_clear(cache.ref, _cache_stream(cache)), "larosa_kv4_clear")
 
 
 def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, out=None, rotary: Rotary | None = None):
@@ -496,7 +504,7 @@ def kv4_append(cache: KvCache, layer: int, batch: KvBatch, qkv, n_heads: int, ou
     ld_out = 0 if out is None else _rows(out, batch.n_rows, cache)
     _check(lib().larosa_kv4_append(cache.ref, layer, batch.ref, _ptr(qkv), ld_qkv, n_heads,
                                    rotary.ref if rotary is not None else None, _ptr(out), ld_out,
-                                   _stream()), "larosa_kv4_append")
+                                   _cache_stream(cache)), "larosa_kv4_append")
     return out
 
 
@@ -516,7 +524,7 @@ def kv4_attention(cache: KvCache, layer: int, batch: KvBatch, q, n_heads: int, o
     _check_batch(cache, batch)
     ld_q, ld_out = _rows(q, batch.n_rows, cache), _rows(out, batch.n_rows, cache)
     _check(lib().larosa_kv4_attention(cache.ref, layer, batch.ref, _ptr(q), ld_q, n_heads, scale,
-                                      window, max_len, _ptr(out), ld_out, ws.ptr, ws.nbytes, _stream()),
+                                      window, max_len, _ptr(out), ld_out, ws.ptr, ws.nbytes, _cache_stream(cache)),
            "larosa_kv4_attention")
     return out
 
@@ -536,14 +544,14 @@ def kv4_grow(cache: KvCache, slots, status, ws: Workspace, counts=None):
     """Room for counts (default one) more tokens in every listed slot; status [1] int32: 0, pages missing, or -1."""
     n, dev = slots.numel(), cache.device
     _check(lib().larosa_kv4_grow(cache.ref, _list(slots, n, dev), _list(counts, n, dev), n, _word(status, dev), ws.ptr, ws.nbytes,
-                                 _stream()), "larosa_kv4_grow")
+                                 _cache_stream(cache)), "larosa_kv4_grow")
     return status
 
 
 def kv4_fork(cache: KvCache, src, dst, status):
     """The sequences of src into the free slots dst, all pages shared; status [1] int32: 0 or -1."""
     n, dev = src.numel(), cache.device
-    _check(lib().larosa_kv4_fork(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _word(status, dev), _stream()),
+    _check(lib().larosa_kv4_fork(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _word(status, dev), _cache_stream(cache)),
            "larosa_kv4_fork")
     return status
 
@@ -551,19 +559,19 @@ def kv4_fork(cache: KvCache, src, dst, status):
 def kv4_trim(cache: KvCache, slots, keep=None):
     """Listed slots keep their first keep tokens (default none)."""
     n, dev = slots.numel(), cache.device
-    _check(lib().larosa_kv4_trim(cache.ref, _list(slots, n, dev), _list(keep, n, dev), n, _stream()), "larosa_kv4_trim")
+    _check(lib().larosa_kv4_trim(cache.ref, _list(slots, n, dev), _list(keep, n, dev), n, _cache_stream(cache)), "larosa_kv4_trim")
 
 
 def kv4_compact(cache: KvCache, live, ws: Workspace):
     """Pages in use to the lowest ids; live [1] int32 (or None) receives their number."""
-    _check(lib().larosa_kv4_compact(cache.ref, _word(live, cache.device), ws.ptr, ws.nbytes, _stream()), "larosa_kv4_compact")
+    _check(lib().larosa_kv4_compact(cache.ref, _word(live, cache.device), ws.ptr, ws.nbytes, _cache_stream(cache)), "larosa_kv4_compact")
     return live
 
 
 def kv4_copy_pages(cache: KvCache, src, dst):
     """Pages src of every layer into pages dst."""
     n, dev = src.numel(), cache.device
-    _check(lib().larosa_kv4_copy_pages(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _stream()), "larosa_kv4_copy_pages")
+    _check(lib().larosa_kv4_copy_pages(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _cache_stream(cache)), "larosa_kv4_copy_pages")
 
 
 def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: int = 0, device="cuda:0") -> Workspace:
@@ -586,6 +594,6 @@ def layer_forward_kv4(layer: Layer, cache: KvCache, index: int, batch: KvBatch, 
     tr = _trace_struct(trace)
     _check(lib().larosa_layer_forward_kv4(ctypes.byref(layer.c), cache.ref, index, batch.ref,
                                           rotary.ref if rotary is not None else None, scale, window, max_len, _ptr(x),
-                                          _ptr(x_out), ctypes.byref(tr) if tr is not None else None, ws.ptr, ws.nbytes, _stream()),
+                                          _ptr(x_out), ctypes.byref(tr) if tr is not None else None, ws.ptr, ws.nbytes, _cache_stream(cache)),
            "larosa_layer_forward_kv4")
     return x_out

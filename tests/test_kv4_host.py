@@ -309,3 +309,21 @@ def test_sums_of_splits_start_at_16_bytes(lib):
     for args in ((None, ref(batch()), 8, 0, 0, bad), (ref(cache()), ref(batch(n_seq=0)), 8, 0, 0, bad), (ref(cache()), ref(batch()), 7, 0, 0, bad),
                  (ref(cache()), ref(batch()), 8, -1, 0, bad), (ref(cache()), ref(batch()), 8, 0, -1, bad), (ref(cache()), ref(batch()), 8, 0, 0, None)):
         assert lib.larosa_kv4_attention_plan(*args) == api.EINVAL
+
+
+def test_binding_refuses_a_cache_of_another_than_the_current_device(lib, monkeypatch):
+    import torch
+    from paper_2507_01299_amd import api
+    c = cpu_cache(api)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: c.device + 1)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    ws = type("Ws", (), dict(ptr=FAKE, nbytes=BIG))
+    one, status = torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    b, rows, q = api.KvBatch(one, 1), torch.zeros(1, 192, dtype=torch.float16), torch.zeros(1, 64, dtype=torch.float16)
+    layer = type("L", (), dict(c=api._Layer(d=64)))
+    for call in (lambda: api.kv4_clear(c), lambda: api.kv4_trim(c, one), lambda: api.kv4_grow(c, one, status, ws),
+                 lambda: api.kv4_fork(c, one, one + 1, status), lambda: api.kv4_compact(c, None, ws), lambda: api.kv4_copy_pages(c, one, one + 1),
+                 lambda: api.kv4_append(c, 0, b, rows, 1), lambda: api.kv4_attention(c, 0, b, rows, 1, q, ws),
+                 lambda: api.layer_forward_kv4(layer, c, 0, b, q, q.clone(), ws)):
+        with pytest.raises(ValueError, match="current"):
+            call()
