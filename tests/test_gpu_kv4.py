@@ -265,6 +265,37 @@ def test_attention_weights_that_round_alike(gpu_device, dtype, n):
         assert np.array_equal(got[0, 0], values[0])
 
 
+def test_attention_extreme_logits_f16(gpu_device):
+    """As for bf16: differences that underflow, the whole range of f16's weights."""
+    rng = np.random.default_rng(26)
+    C, slots = U.random_cache(rng, [700, 700], 64, 1, 64, "f16")
+    q = U.random_rows(rng, 2, 64, "f16", size=30.0)
+    for scale in (1.0, 0.0, -1.0):
+        check_attention(C, slots, None, q, 1, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 30.0, 700.0, 2.0e4, 1.0e6])
+def test_attention_logits_beyond_what_fp32_tells_apart(gpu_device, dtype, scale):
+    """Logits up to 10^11, where fp32's neighbours lie further apart than any weight reaches: the keys that lead share the output, and no
+    weight leaves its type's range."""
+    rng = np.random.default_rng(29)
+    n, D = 700, 64
+    keys = rng.choice([0.5, 1.0, 2.0, 3.0], n)
+    leads = [5, 40, 41, 300, 699]
+    keys[leads] = 4.0
+    values = rng.choice(K.LEVELS[1:], (n, D))
+    C, slots = chosen_tokens(rng, dtype, keys, values)
+    for q0 in (1000.0, 1001.0, 30016.0, 60000.0):
+        q = np.zeros((1, D))
+        q[0, 0] = q0
+        got, _ = run_attention(C, slots, None, O.encode16(q, dtype), 1, scale=scale)
+        # (q0 scale is at least 1000 between the leading keys and the next: weights of zero)
+        k, v, have = K.keys_values(C, 0, slots[0], n, 0)
+        want = v[leads].mean(0)
+        assert have.all() and (np.abs(got[0, 0] - want) <= U.HALF_STEP[dtype] * np.abs(want) * 1.01).all()
+
+
 # ---- every way in which a call is divided: tiles of 16 and 32 rows, alone and several, whole and split, with and without a window ----
 
 def plan_of(C, slots, starts, n_rows, n_heads, max_new=1, window=0, max_len=0):
