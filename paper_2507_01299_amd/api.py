@@ -381,20 +381,30 @@ def layer_after_attention(layer: Layer, residual, attn, x_out, ws: Workspace, tr
     return x_out
 
 
+_INT32 = torch.int32        # (a name of this module: each look into torch's costs a call 40 ns, and a list is checked by four)
+
+
 def _list(t, n, device):
     """Address of a list for the 4-bit cache (None: none): anything but n int32 in a row on the cache's device would be misread there."""
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+    if t.dtype is not _INT32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
         raise ValueError(f"a list of {n} contiguous int32 on the cache's device")
     return t.data_ptr()
+
+
+def _first_list(t, device):
+    """A call's first list, which says how long the others are: its length and address."""
+    if t.dtype is not _INT32 or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError("a list of contiguous int32 on the cache's device")
+    return t.numel(), t.data_ptr()
 
 
 def _word(t, device):
     """Address of the one int32 that a call reports to."""
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.numel() < 1 or t.get_device() != device:
+    if t.dtype is not _INT32 or t.numel() < 1 or t.get_device() != device:
         raise ValueError("an int32 on the cache's device")
     return t.data_ptr()
 
@@ -440,10 +450,11 @@ class KvBatch:
     row for each sequence), max_new the most of one sequence."""
 
     def __init__(self, slots, n_rows: int, starts=None, max_new: int = 1):
-        self.device, n_seq = slots.get_device(), slots.numel()
+        self.device = slots.get_device()
+        n_seq, listed = _first_list(slots, self.device)
         self.tensors = (slots, starts)       # keep alive
         self.n_rows = n_rows
-        self.c = _KvBatch(_list(slots, n_seq, self.device), _list(starts, n_seq + 1, self.device), n_seq, n_rows, max_new)
+        self.c = _KvBatch(listed, _list(starts, n_seq + 1, self.device), n_seq, n_rows, max_new)
         self.ref = ctypes.byref(self.c)
 
 
@@ -480,7 +491,7 @@ def _rows(t, n_rows: int, cache) -> int:
 
 def _cache_stream(cache):
     """The current stream; its device has to be the cache's."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()      # (the cache's tensors are there, so the runtime is up)
     if device != cache.device:
         raise ValueError("the cache's device is not the current one")
     return torch._C._cuda_getCurrentRawStream(device)
@@ -542,24 +553,27 @@ def kv4_pages_workspace(cache: KvCache, device="cuda:0") -> Workspace:
 
 def kv4_grow(cache: KvCache, slots, status, ws: Workspace, counts=None):
     """Room for counts (default one) more tokens in every listed slot; status [1] int32: 0, pages missing, or -1."""
-    n, dev = slots.numel(), cache.device
-    _check(lib().larosa_kv4_grow(cache.ref, _list(slots, n, dev), _list(counts, n, dev), n, _word(status, dev), ws.ptr, ws.nbytes,
+    dev = cache.device
+    n, listed = _first_list(slots, dev)
+    _check(lib().larosa_kv4_grow(cache.ref, listed, _list(counts, n, dev), n, _word(status, dev), ws.ptr, ws.nbytes,
                                  _cache_stream(cache)), "larosa_kv4_grow")
     return status
 
 
 def kv4_fork(cache: KvCache, src, dst, status):
     """The sequences of src into the free slots dst, all pages shared; status [1] int32: 0 or -1."""
-    n, dev = src.numel(), cache.device
-    _check(lib().larosa_kv4_fork(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _word(status, dev), _cache_stream(cache)),
+    dev = cache.device
+    n, listed = _first_list(src, dev)
+    _check(lib().larosa_kv4_fork(cache.ref, listed, _list(dst, n, dev), n, _word(status, dev), _cache_stream(cache)),
            "larosa_kv4_fork")
     return status
 
 
 def kv4_trim(cache: KvCache, slots, keep=None):
     """Listed slots keep their first keep tokens (default none)."""
-    n, dev = slots.numel(), cache.device
-    _check(lib().larosa_kv4_trim(cache.ref, _list(slots, n, dev), _list(keep, n, dev), n, _cache_stream(cache)), "larosa_kv4_trim")
+    dev = cache.device
+    n, listed = _first_list(slots, dev)
+    _check(lib().larosa_kv4_trim(cache.ref, listed, _list(keep, n, dev), n, _cache_stream(cache)), "larosa_kv4_trim")
 
 
 def kv4_compact(cache: KvCache, live, ws: Workspace):
@@ -570,8 +584,9 @@ def kv4_compact(cache: KvCache, live, ws: Workspace):
 
 def kv4_copy_pages(cache: KvCache, src, dst):
     """Pages src of every layer into pages dst."""
-    n, dev = src.numel(), cache.device
-    _check(lib().larosa_kv4_copy_pages(cache.ref, _list(src, n, dev), _list(dst, n, dev), n, _cache_stream(cache)), "larosa_kv4_copy_pages")
+    dev = cache.device
+    n, listed = _first_list(src, dev)
+    _check(lib().larosa_kv4_copy_pages(cache.ref, listed, _list(dst, n, dev), n, _cache_stream(cache)), "larosa_kv4_copy_pages")
 
 
 def layer_kv4_workspace(layer: Layer, cache: KvCache, batch: KvBatch, max_len: int = 0, device="cuda:0") -> Workspace:

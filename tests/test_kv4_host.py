@@ -315,7 +315,7 @@ def test_binding_refuses_a_cache_of_another_than_the_current_device(lib, monkeyp
     import torch
     from paper_2507_01299_amd import api
     c = cpu_cache(api)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: c.device + 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: c.device + 1, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
     ws = type("Ws", (), dict(ptr=FAKE, nbytes=BIG))
     one, status = torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
