@@ -334,8 +334,9 @@ int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_bat
  * key/value head h / (n_heads / n_kv_heads)):
  *   out[row, h, :] = sum_t w_t v_t / sum_t w_t,   w_t = exp(scale (q[row, h, :] . k_t) - max)
  * over the tokens t <= place of the row in its sequence and, with window > 0, t > place - window.  A row that sees no token (an
- * empty sequence, padding of a batch with starts, pages missing) gets zeros.  The 16-bit weights w_t and exact values multiply on the
- * matrix cores, sums and the maximum are fp32.  q [n_rows, ld_q], out [n_rows, ld_out]: multiples of 8 apart, out rounded once.
+ * empty sequence, padding of a batch with starts, pages missing) gets zeros, and so does one whose logits are all -infinity.  Sums and the
+ * maximum are fp32; the weights w_t are rounded to 16 bits, above and below alike (f16: those below 2^-21 of a row's largest may
+ * lose more), the values are exact.  Sums of bf16 values are fp32's too: many of more than 2^110 overflow.  q [n_rows, ld_q], out [n_rows, ld_out]: multiples of 8 apart, out rounded once.
  * max_len: about the longest sequence, by which the work is divided over the chip (0: max_pages * page_tokens); longer ones are
  * right too.  Workspace: larosa_kv4_attention_workspace_bytes of the same arguments, initialised by larosa_workspace_init. */
 size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* batch, int n_heads, int max_len);

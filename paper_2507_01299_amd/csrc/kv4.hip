@@ -472,7 +472,8 @@ __device__ __forceinline__ void attend_block(Block<D>& x, const uint8_t* block, 
     const float ref = r.ref == -INFINITY ? 0.f : r.ref;
 #pragma unroll
     for (int i = 0; i < 8; ++i) p[z][i] = __builtin_amdgcn_exp2f(p[z][i] - ref);
-    // weights to 16 bits: half a step on each, 2^-8 (bf16) or 2^-11 (f16, from 2^-14 on) relative
+    // weights to 16 bits, as the values are that they meet on the matrix cores: half a step on each, 2^-8 (bf16) or 2^-11 (f16, from 2^-14
+    // on) relative.  Outputs are 2.2e-3 (bf16) or 2.5e-4 (f16) from fp64 so, and 1.7e-3 or 2.0e-4 by the store alone
     pf[z] = u32x4_t{Mat<T>::round2(p[z][0], p[z][1]), Mat<T>::round2(p[z][2], p[z][3]), Mat<T>::round2(p[z][4], p[z][5]),
                     Mat<T>::round2(p[z][6], p[z][7])};
     // summed as rounded, so that what all weights have lost or gained in common cancels
@@ -589,8 +590,8 @@ constexpr int attention_waves(int D, int NT) { return D == 64 ? (NT == 1 ? 4 : 3
 
 // One workgroup: a tile of 16 NT rows and one split of the tokens that they see; its four waves take every fourth block of 32 tokens
 // each.  Where a tile has several splits, each leaves its sums for kv4_combine_kernel.  Bound by HBM where there is work for all
-// compute units (about 230 vector instructions for a block of 4352 bytes at head_dim 128: 1000 cycles of a SIMD, and 2300 at the rate
-// of a large copy); a short call is a chain of loads: slot, length and page, keys, output.
+// compute units (about 214 vector instructions for a block of 4352 bytes at head_dim 128: 860 cycles of a SIMD, and 1720 at the rate
+// of a large read, 6.2 TB/s); a short call is a chain of loads: slot, length and page, keys, output.
 template <typename T, int D, int NT, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, attention_waves(D, NT)) void kv4_attention_kernel(Kv4AttentionArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -341,8 +341,8 @@ __device__ __forceinline__ void copy_step(const piece_t* a, piece_t* b, unsigned
 
 // Pages src[i] into dst[i], all layers; the pairs' number comes from n_pairs or, where that is null, from n.  With `remap`, ids
 // that a packing has moved change in the tables as well.  Layer by layer, so that neighbouring pages move at the same time (packing
-// 102 pages of 2.2 MB: 145 us pair by pair, 120 so, 98 at the rate of a large copy); what the 256 MB cache behind the L2s does
-// not hold passes them by (128 us without; but 23 MB take 6.4 us through them, 7.4 past them).
+// 170 pages of 2.2 MB: 145 us pair by pair, 120 so; a copy of 4 GiB would take 164 for as much, but part of this stays in the 256 MB cache
+// behind the L2s); what that cache does not hold passes them by (128 us without; but 23 MB take 6.4 us through them, 7.4 past them).
 __global__ __launch_bounds__(256) void kv4_copy_kernel(larosa_kv4_cache C, const int32_t* src, const int32_t* dst, const int32_t* n_pairs,
                                                        Kv4Scratch remap, int n, unsigned page_pieces, unsigned grid) {
   if (n_pairs) n = *n_pairs;

@@ -296,6 +296,23 @@ def test_attention_logits_beyond_what_fp32_tells_apart(gpu_device, dtype, scale)
         assert have.all() and (np.abs(got[0, 0] - want) <= U.HALF_STEP[dtype] * np.abs(want) * 1.01).all()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_infinite_queries(gpu_device, dtype):
+    """Logits of -infinity alone: zeros, whole and split; +infinity among them: NaN; a finite query beside them stays finite."""
+    rng = np.random.default_rng(30)
+    for n in (20, 1500):
+        keys, values = np.ones(n), rng.choice(K.LEVELS[1:], (n, 64))
+        C, slots = chosen_tokens(rng, dtype, keys, values)
+        q = np.zeros((1, 3, 64))
+        q[0, :, 0] = -np.inf, np.inf, 0.5
+        got, _ = run_attention(C, slots, None, O.encode16(q.reshape(1, -1), dtype), 3)
+        assert not got[0, 0].any() and np.isnan(got[0, 1]).all() and np.isfinite(got[0, 2]).all()
+        keys[3:] = -1.0                               # logits of +infinity behind the first three's -infinity, and the reverse
+        C, slots = chosen_tokens(rng, dtype, keys, values)
+        got, _ = run_attention(C, slots, None, O.encode16(q.reshape(1, -1), dtype), 3)
+        assert np.isnan(got[0, :2]).all() and np.isfinite(got[0, 2]).all()
+
+
 # ---- every way in which a call is divided: tiles of 16 and 32 rows, alone and several, whole and split, with and without a window ----
 
 def plan_of(C, slots, starts, n_rows, n_heads, max_new=1, window=0, max_len=0):
