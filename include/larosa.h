@@ -171,8 +171,8 @@ size_t larosa_layer_workspace_bytes(const larosa_layer* L, int B);
  *   x_out = R(x2 adapter) or x2;  s1 = R(x shortcut_attn) or x;  s2 = R(x1 shortcut_mlp) or x1.
  *   R = one rounding to the layer dtype.
  * trace may be NULL.  x_out must not alias x.  Rows: the projections of several rows take a counter of the workspace for each
- * group of 32 rows and 128 output columns (those of a shortcut adapter beside its projection's included), and there are
- * 4096: with gate|up 28672 wide up to 576 rows.  More are LAROSA_EUNSUPPORTED. */
+ * group of 32 rows (an explicit rotation behind a learned pre-norm scale: of 4) and 128 output columns (those of a shortcut adapter
+ * beside its projection's included), and there are 4096: with gate|up 28672 wide up to 576 rows.  More are LAROSA_EUNSUPPORTED. */
 int larosa_layer_forward(const larosa_layer* L, const void* x, void* x_out, int B,
                          const larosa_trace* trace, void* ws, size_t ws_bytes, void* stream);
 
@@ -336,7 +336,8 @@ int larosa_kv4_append(const larosa_kv4_cache* C, int layer, const larosa_kv4_bat
  * over the tokens t <= place of the row in its sequence and, with window > 0, t > place - window.  A row that sees no token (an
  * empty sequence, padding of a batch with starts, pages missing) gets zeros, and so does one whose logits are all -infinity.  Sums and the
  * maximum are fp32; the weights w_t are rounded to 16 bits, above and below alike (f16: those below 2^-21 of a row's largest may
- * lose more), the values are exact.  Sums of bf16 values are fp32's too: many of more than 2^110 overflow.  q [n_rows, ld_q], out [n_rows, ld_out]: multiples of 8 apart, out rounded once.
+ * lose more), the values are exact.  Sums of bf16 values are fp32's too: many of more than 2^110 overflow.
+ * q [n_rows, ld_q], out [n_rows, ld_out]: multiples of 8 apart, out rounded once.
  * max_len: about the longest sequence, by which the work is divided over the chip (0: max_pages * page_tokens); longer ones are
  * right too.  Workspace: larosa_kv4_attention_workspace_bytes of the same arguments, initialised by larosa_workspace_init. */
 size_t larosa_kv4_attention_workspace_bytes(const larosa_kv4_cache* C, const larosa_kv4_batch* batch, int n_heads, int max_len);

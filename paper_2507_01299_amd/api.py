@@ -411,7 +411,8 @@ def _word(t, device):
 
 class KvCache:
     """Device tensors of a 4-bit key/value cache and the matching C struct.  Tensors that are not given are allocated, and the
-    cache is then made empty; given ones are taken as they are (all of refs, table and length, or none)."""
+    cache is then made empty; given ones are taken as they are (all of refs, table and length, or none).  Calls on a cache are made with
+    its device as the current one, and with lists and rows on it."""
 
     def __init__(self, n_layers, n_pages, page_tokens, n_slots, max_pages, n_kv_heads, head_dim, dtype, data=None, refs=None,
                  table=None, length=None, device="cuda:0"):

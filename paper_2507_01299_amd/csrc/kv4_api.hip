@@ -98,7 +98,8 @@ AttentionPlan plan_attention(const larosa_kv4_cache* C, const larosa_kv4_batch* 
   if (window > 0 && window < span) span = window + b->max_new < span ? window + b->max_new : span;
   const long blocks = (span + 31) / 32 + (window > 0 ? 1 : 0);
   // 32 rows to a tile convert the codes half as often, but leave fewer waves and workgroups: from a thousand pieces of 32 blocks on
-  // (a prompt of 4096 tokens, 8B heads: 306 -> 268 us, 32 sequences of 8000 tokens with eight new: 98 -> 91; eight such: 31 -> 34)
+  // (a prompt of 4096 tokens, 8B heads: 278 -> 233 us, 32 sequences of 8000 tokens with eight new: 95 -> 80; with less work it goes
+  // either way: eight such sequences 27 -> 24, one of 20000 tokens 14.7 -> 16.5).  At head_dim 256 the 16 rows take all registers.
   const long tiles32 = (rows + 31) / 32;
   p.tile_rows = rows > 16 && C->head_dim <= 128 && tiles32 * C->n_kv_heads * b->n_seq * blocks >= 1000 * kPieceBlocks ? 32 : 16;
   p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;

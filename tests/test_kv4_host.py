@@ -189,8 +189,10 @@ def test_layer_with_cache_refuses_rows_before_anything_is_enqueued(lib):
                    lib.larosa_layer_after_attention(ref(L), FAKE, FAKE, OTHER, n, None, FAKE, BIG, None)]
         return size, rc
 
-    # gate|up: 224 strips of 128 columns, 18 groups of 32 rows; with a shortcut adapter 256 strips, 16 groups
-    for L, C, most in ((big, C8, 576), (dict(big, shortcut_mlp=FAKE), C8, 512), (small, C2, 32 * (4096 // 11))):
+    # gate|up: 224 strips of 128 columns, 18 groups of 32 rows; with a shortcut adapter 256 strips, 16 groups; a rotation behind a
+    # learned scale: 32 strips, 128 groups of 4 rows
+    for L, C, most in ((big, C8, 576), (dict(big, shortcut_mlp=FAKE), C8, 512), (small, C2, 32 * (4096 // 11)),
+                       (dict(big, Q_mlp=FAKE, rms_mlp=FAKE), C8, 512)):
         assert both(L, C, most)[0] > 0 and both(L, C, 1)[0] > 0
         for n in (most + 1, most + 40, 16384):
             assert both(L, C, n) == (0, [api.EUNSUPPORTED] * 3), n
