@@ -277,7 +277,8 @@ int larosa_threshold_select(const void* h, int B, int d, float eps, larosa_dtype
  *   table   [n_slots, max_pages]: page of tokens [p page_tokens, (p + 1) page_tokens) of the sequence in a slot, -1 = none
  *   length  [n_slots]: tokens of the sequence in a slot (0: the slot is free)
  *   refs    [n_pages]: table entries that name the page (0: the page is free)
- * head_dim is 64, 128 or 256; page_tokens 32, 64, 128 or 256; at most 2^18 slots and 2^28 pages; data 16-byte aligned.  A page id outside [0, n_pages) is
+ * head_dim is 64, 128 or 256; page_tokens 32, 64, 128 or 256; at most 2^18 slots, 2^28 pages and 2^43 bytes of data,
+ * which is 16-byte aligned.  A page id outside [0, n_pages) is
  * never followed: tokens on it are not stored and not seen.  Two calls that use one cache are ordered on one stream. */
 typedef struct {
   int n_layers, n_pages, page_tokens, n_slots, max_pages;

@@ -16,6 +16,10 @@ inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 inline hipStream_t stream_of(void* s) { return static_cast<hipStream_t>(s); }
 inline int status_of(hipError_t e) { return e == hipSuccess ? LAROSA_OK : LAROSA_EHIP; }
 
+size_t page_bytes_of(const larosa_kv4_cache* C) {
+  return static_cast<size_t>(C->n_kv_heads) * (C->page_tokens / 32) * 34 * C->head_dim;
+}
+
 // Sizes of a cache; nothing of it is read.
 int check_sizes(const larosa_kv4_cache* C) {
   if (!C || C->n_layers < 1 || C->n_pages < 1 || C->n_slots < 1 || C->max_pages < 1 || C->n_kv_heads < 1) return LAROSA_EINVAL;
@@ -26,6 +30,8 @@ int check_sizes(const larosa_kv4_cache* C) {
   if (static_cast<long>(C->max_pages) * C->page_tokens >= (1L << 30) || C->n_kv_heads > kKv4HeadsMax) return LAROSA_EUNSUPPORTED;
   if (C->n_pages > (1 << 28) || C->n_slots > kKv4SlotsMax || C->n_layers > 65535) return LAROSA_EUNSUPPORTED;
   if (static_cast<long>(C->n_slots) * C->max_pages >= (1L << 31)) return LAROSA_EUNSUPPORTED;   // (counts of pages are 32-bit)
+  // 8 TiB: pages of all layers, of 2176 bytes at least, are counted in 32 bits; bytes of one layer stay below 2^57
+  if (page_bytes_of(C) * C->n_pages > ((size_t{1} << 43) - 1) / C->n_layers) return LAROSA_EUNSUPPORTED;
   return LAROSA_OK;
 }
 
@@ -136,8 +142,7 @@ Kv4Scratch scratch_of(void* ws) { return Kv4Scratch{reinterpret_cast<int32_t*>(s
 Kv4Kind kind_of(const larosa_kv4_cache* C) { return Kv4Kind{C->head_dim, C->dtype == LAROSA_BF16}; }
 
 uint8_t* layer_data(const larosa_kv4_cache* C, int layer) {
-  return static_cast<uint8_t*>(C->data) +
-         static_cast<size_t>(layer) * C->n_pages * larosa_kv4_page_bytes(C->page_tokens, C->n_kv_heads, C->head_dim);
+  return static_cast<uint8_t*>(C->data) + static_cast<size_t>(layer) * C->n_pages * page_bytes_of(C);
 }
 
 // What append and attention have in common.
@@ -166,12 +171,12 @@ size_t larosa_kv4_page_bytes(int page_tokens, int n_kv_heads, int head_dim) {
   C.n_layers = C.n_pages = C.n_slots = C.max_pages = 1;
   C.page_tokens = page_tokens; C.n_kv_heads = n_kv_heads; C.head_dim = head_dim;
   if (check_sizes(&C) != LAROSA_OK) return 0;
-  return static_cast<size_t>(n_kv_heads) * (page_tokens / 32) * 34 * head_dim;
+  return page_bytes_of(&C);
 }
 
 size_t larosa_kv4_data_bytes(const larosa_kv4_cache* C) {
   if (check_sizes(C) != LAROSA_OK) return 0;
-  return static_cast<size_t>(C->n_layers) * C->n_pages * larosa_kv4_page_bytes(C->page_tokens, C->n_kv_heads, C->head_dim);
+  return static_cast<size_t>(C->n_layers) * C->n_pages * page_bytes_of(C);
 }
 
 int larosa_kv4_clear(const larosa_kv4_cache* C, void* stream) {

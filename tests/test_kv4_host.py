@@ -329,3 +329,24 @@ def test_binding_refuses_a_cache_of_another_than_the_current_device(lib, monkeyp
                  lambda: api.layer_forward_kv4(layer, c, 0, b, q, q.clone(), ws)):
         with pytest.raises(ValueError, match="current"):
             call()
+
+
+def test_data_of_2_to_the_43_bytes_is_refused(lib):
+    """Bytes are counted in 64 bits and pieces of pages in 32: a product of sizes that are fine one by one may pass both."""
+    from paper_2507_01299_amd import api
+    ref = ctypes.byref
+    page = lib.larosa_kv4_page_bytes(64, 2, 128)
+    most = ((1 << 43) - 1) // page
+    for layers in (1, 2, 1000, 65535):
+        n = min(most // layers, 1 << 28)
+        assert lib.larosa_kv4_data_bytes(ref(cache(n_layers=layers, n_pages=n))) == layers * n * page
+    for sizes in (dict(n_layers=2, n_pages=1 << 28), dict(n_layers=1000, n_pages=most // 1000 + 1),
+                  dict(n_layers=65535, n_pages=1 << 28, n_kv_heads=4096, head_dim=256, page_tokens=256),
+                  # 2^64 + 2^54 bytes and the like: what is left of them in 64 bits would look modest
+                  dict(n_layers=4096, n_pages=(1 << 28) - 1, n_kv_heads=4096, head_dim=256, page_tokens=256),
+                  dict(n_layers=61681, n_pages=17 * (1 << 22), n_kv_heads=1 << 12, head_dim=256, page_tokens=32)):
+        C = cache(**sizes)
+        assert lib.larosa_kv4_data_bytes(ref(C)) == 0, sizes
+        assert lib.larosa_kv4_clear(ref(C), None) == api.EUNSUPPORTED
+        assert lib.larosa_kv4_pages_workspace_bytes(ref(C)) == 0
+        assert lib.larosa_kv4_copy_pages(ref(C), FAKE, OTHER, 1, None) == api.EUNSUPPORTED
