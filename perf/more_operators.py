@@ -6,11 +6,11 @@ and all of it in one call, from hidden rows to log probabilities.
 plain torch where `own` is false and calls `paper_2507_01299_amd.api` where it is true; `exact` states them in 64 bits;
 `work` gives the bytes and operations of one pass.
 
-The format.  A code is an e4m3 number (4 exponent bits, 3 of mantissa, at most 448).  A block of values v (128 x 128 of a weight,
-128 neighbours of a row) with m = max(max |v|, 2^-54) has the scale m / 448, rounded to 32 bits, and the codes nearest to
-v * (448 / m), quotient and product rounded to 32 bits; a value is its code times its block's scale.  Codes of a weight
-[d_in, d_out] are stored [d_out, d_in], d_in rounded up to 16 (zeros), its scales by block [d_out / 128, d_in / 128]; codes of rows
-[n, d] the same way, their scales [d / 128, n].
+The format.  A code is an e4m3 number (4 exponent bits, 3 of mantissa, at most 448).  A block of values (128 x 128 of a weight,
+128 neighbours of a row) has the scale 2^e with the least e >= -64 for which its largest magnitude is at most 448 * 2^e, held as the
+byte e + 127; its codes are the numbers nearest to value / 2^e, ties to the even one.  Codes of a weight [d_in, d_out] are stored [d_out, d_in],
+d_in rounded up to 16 (zeros), its scales by block [d_out / 128, d_in / 128], the latter rounded up to 4 (127); codes of rows [n, d] and
+their scales [n, d / 128] the same way.
 """
 import math
 
@@ -22,7 +22,7 @@ own = False
 DEV = "cuda:0"
 TYPE = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
 E4M3 = torch.float8_e4m3fn
-TINY = 2.0 ** -54
+LEAST = -64          # exponent of a scale
 
 
 # ---- the cases ------------------------------------------------------------------------------------------
@@ -30,11 +30,11 @@ TINY = 2.0 ** -54
 def listed():
     return [
         # the attention output projection of a 7B or 8B model, one token: latency
-        dict(name="dense_7b_o_1", op="dense", rows=1, d_in=4096, d_out=4096, dtype="bf16", out="bf16"),
+        dict(name="dense_7b_o_1", op="dense", rows=1, d_in=4096, d_out=4096, dtype="bf16"),
         # the down projection of a 7B model over a short prompt: rows that fill no tile, few output columns, a long sum
-        dict(name="dense_7b_down_333", op="dense", rows=333, d_in=11008, d_out=4096, dtype="f16", out="f16"),
+        dict(name="dense_7b_down_333", op="dense", rows=333, d_in=11008, d_out=4096, dtype="f16"),
         # gate|up of a 70B model over a long prompt: the largest product
-        dict(name="dense_70b_gate_up_4096", op="dense", rows=4096, d_in=8192, d_out=57344, dtype="bf16", out="bf16"),
+        dict(name="dense_70b_gate_up_4096", op="dense", rows=4096, d_in=8192, d_out=57344, dtype="bf16"),
         # a decode batch's rows to 8 bits, once for several products
         dict(name="rows_5x4096", op="rows", rows=5, d=4096, dtype="f16"),
         # the same for the MLP's inner rows of a 70B model's prompt
@@ -67,7 +67,7 @@ def draw(rng):
     if op == "dense":
         d_in, d_out = eight(512, 28672), eight(512, 57344)
         rows = _log_int(rng, 1, min(8192, int(4096 * 8192 * 57344 / (d_in * d_out))))
-        return dict(op=op, rows=rows, d_in=d_in, d_out=d_out, dtype=dtype, out=rng.choice([dtype, dtype, "f32"]))
+        return dict(op=op, rows=rows, d_in=d_in, d_out=d_out, dtype=dtype)
     if op == "rows":
         d = eight(512, 28672)
         return dict(op=op, rows=_log_int(rng, 1, 4096 * 28672 // d), d=d, dtype=dtype)
@@ -90,34 +90,40 @@ def _blocks(n):
     return -(-n // 128)
 
 
+def _exponents(m):
+    """Largest magnitudes of blocks -> the exponents of their scales."""
+    part, power = torch.frexp(m.clamp(min=2.0 ** -70))
+    return (power - 9 + (part > 0.875).to(power.dtype)).clamp(min=LEAST)
+
+
+def _bytes(e):
+    """Exponents [rows, blocks] -> scale bytes, blocks rounded up to 4."""
+    return F.pad(e + 127, (0, -e.shape[1] % 4), value=127).to(torch.uint8)
+
+
 def _codes_of_rows(v):
-    """v [n, d] in 32 bits -> codes [n, d up to 16] and scales [d / 128, n]."""
+    """v [n, d] in 32 bits -> codes [n, d up to 16] and scale bytes [n, d / 128 up to 4]."""
     n, d = v.shape
     v = F.pad(v, (0, 128 * _blocks(d) - d)).unflatten(1, (-1, 128))
-    m = v.abs().amax(-1, keepdim=True).clamp(min=TINY)
-    most = torch.full_like(m, 448.0)      # (a tensor by a number would be multiplied by its rounded inverse)
-    codes = (v * (most / m)).clamp(-448.0, 448.0).to(E4M3).flatten(1)
-    return codes[:, :-(-d // 16) * 16].contiguous(), (m / most)[..., 0].t().contiguous()
+    e = _exponents(v.abs().amax(-1))
+    codes = (v * torch.exp2(-e.float())[..., None]).to(E4M3).flatten(1)
+    return codes[:, :-(-d // 16) * 16].contiguous(), _bytes(e)
 
 
 def _codes_of_weight(W):
-    """W [d_in, d_out] in 32 bits -> codes [d_out, d_in up to 16] and scales [d_out / 128, d_in / 128]."""
+    """W [d_in, d_out] in 32 bits -> codes [d_out, d_in up to 16] and scale bytes [d_out / 128, d_in / 128 up to 4]."""
     d_in, d_out = W.shape
     v = F.pad(W.t(), (0, 128 * _blocks(d_in) - d_in, 0, 128 * _blocks(d_out) - d_out))
     v = v.unflatten(0, (-1, 128)).unflatten(2, (-1, 128))
-    m = v.abs().amax((1, 3), keepdim=True).clamp(min=TINY)
-    most = torch.full_like(m, 448.0)
-    codes = (v * (most / m)).clamp(-448.0, 448.0).to(E4M3).flatten(2).flatten(0, 1)
-    return codes[:d_out, :-(-d_in // 16) * 16].contiguous(), (m / most)[:, 0, :, 0].contiguous()
+    e = _exponents(v.abs().amax((1, 3)))
+    codes = (v * torch.exp2(-e.float())[:, None, :, None]).to(E4M3).flatten(2).flatten(0, 1)
+    return codes[:d_out, :-(-d_in // 16) * 16].contiguous(), _bytes(e)
 
 
-def _row_values(codes, scales, d):
-    return codes[:, :d].to(scales.dtype) * scales.t().repeat_interleave(128, 1)[:, :d]
-
-
-def _weight_values(codes, scales, d_in):
-    v = codes[:, :d_in].to(scales.dtype)
-    return v * scales.repeat_interleave(128, 0)[:v.shape[0]].repeat_interleave(128, 1)[:, :d_in]
+def _values(codes, scales, rows_of_block, d):
+    """What codes stand for, in 32 bits."""
+    unit = torch.exp2(scales[:, :_blocks(d)].float() - 127.0).repeat_interleave(rows_of_block, 0)[:codes.shape[0]]
+    return codes[:, :d].float() * unit.repeat_interleave(128, 1)[:, :d]
 
 
 # ---- what a program has in hand ------------------------------------------------------------------------
@@ -146,7 +152,7 @@ def prepare(case, seed):
         s["x"] = _hidden(g, case["rows"], case["d_in"], case["dtype"])
         W = (torch.randn(case["d_in"], case["d_out"], generator=g, device=DEV) * 0.02).to(TYPE[case["dtype"]])
         s["codes"], s["scales"] = _codes_of_weight(W.float())
-        s["y"] = torch.empty(case["rows"], case["d_out"], dtype=TYPE[case["out"]], device=DEV)
+        s["y"] = torch.empty(case["rows"], case["d_out"], dtype=TYPE[case["dtype"]], device=DEV)
     else:
         rows, V, n = case["rows"], case["vocab"], case["given"]
         s["given"] = _given(g, rows, n, V)
@@ -208,9 +214,9 @@ def run(s):
         ids = _top(z, case["top"])
         return dict(logp=logp, entropy=entropy, top_id=ids.int(), top_logp=z.gather(1, ids) - base)
     d = s["x"].shape[1]
-    y = _row_values(*_codes_of_rows(s["x"].float()), d) @ _weight_values(s["codes"], s["scales"], d).t()
+    y = _values(*_codes_of_rows(s["x"].float()), 1, d) @ _values(s["codes"], s["scales"], 128, d).t()
     if op == "dense":
-        return y.to(TYPE[case["out"]])
+        return y.to(TYPE[case["dtype"]])
     return dict(zip(("logp", "entropy"), _logprobs(y, s["given"])))
 
 
@@ -245,19 +251,19 @@ def work(case):
     op = case["op"]
     if op == "rows":
         n, d = case["rows"], case["d"]
-        return dict(bytes=n * d * 3 + 4 * n * _blocks(d), flops=4 * n * d)
+        return dict(bytes=n * d * 3 + n * _blocks(d), flops=4 * n * d)
     if op == "logprobs":
         n, V = case["rows"], case["vocab"]
         return dict(bytes=n * (V * (4 if case["dtype"] == "f32" else 2) + 8 * case["given"] + 4 + 8 * case["top"]), flops=6 * n * V)
     d_in, d_out = (case["d"], case["vocab"]) if op == "score" else (case["d_in"], case["d_out"])
-    scales = 4 * _blocks(d_in) * _blocks(d_out)
+    scales = _blocks(d_in) * _blocks(d_out)
     if op == "weight":
         return dict(bytes=3 * d_in * d_out + scales, flops=4 * d_in * d_out)
     n = case["rows"]
     held = d_in * d_out + scales + 2 * n * d_in
     if op == "score":
         return dict(bytes=held + n * (8 * case["given"] + 4), flops=2 * n * d_in * d_out + 6 * n * d_out)
-    return dict(bytes=held + n * d_out * (4 if case["out"] == "f32" else 2), flops=2 * n * d_in * d_out)
+    return dict(bytes=held + 2 * n * d_out, flops=2 * n * d_in * d_out)
 
 
 # ---- the definition in 64 bits --------------------------------------------------------------------------
@@ -269,15 +275,20 @@ def _nearest_e4m3(v):
 
 
 def _held(v, rows_of_block):
-    """What blocks of rows_of_block x 128 of v [n, d] (64 bits) hold: codes, scales by block, and the values."""
+    """What blocks of rows_of_block x 128 of v [n, d] (64 bits) hold: codes, scale bytes, and the values."""
     n, d = v.shape
     p = v.new_zeros(-(-n // rows_of_block) * rows_of_block, _blocks(d) * 128)
     p[:n, :d] = v
     p = p.view(-1, rows_of_block, _blocks(d), 128)
-    top = p.abs().amax((1, 3), keepdim=True).clamp(min=TINY)
-    codes = _nearest_e4m3((p * (448.0 / top).float().double()).float().double())   # the format rounds both to 32 bits
-    scales = (top / 448.0).float().double()
-    return codes.flatten(2).flatten(0, 1)[:n], scales[:, 0, :, 0], (codes * scales).flatten(2).flatten(0, 1)[:n, :d]
+    top = p.abs().amax((1, 3))
+    e = torch.full_like(top, LEAST)
+    for k in range(LEAST, 121):
+        e = torch.where(top > 448.0 * 2.0 ** k, k + 1.0, e)
+    unit = torch.exp2(e)[:, None, :, None]
+    codes = _nearest_e4m3(p / unit)
+    scales = torch.full((e.shape[0], -(-e.shape[1] // 4) * 4), 127, dtype=torch.uint8, device=v.device)
+    scales[:, :e.shape[1]] = (e + 127).to(torch.uint8)
+    return codes.flatten(2).flatten(0, 1)[:n], scales, (codes * unit).flatten(2).flatten(0, 1)[:n, :d]
 
 
 def exact(case, seed):
@@ -286,16 +297,16 @@ def exact(case, seed):
     if op in ("rows", "weight"):
         v, high = (s["x"].double(), 1) if op == "rows" else (s["W"].double().t(), 128)
         codes, scales, _ = _held(v, high)
-        return dict(codes=codes[:, :-(-v.shape[1] // 16) * 16].contiguous(), scales=(scales.t() if op == "rows" else scales).contiguous())
+        return dict(codes=codes[:, :-(-v.shape[1] // 16) * 16].contiguous(), scales=scales)
     if op == "logprobs":
         z = s["logits"].double()
     else:
         _, _, x = _held(s["x"].double(), 1)
         W = s["codes"][:, :x.shape[1]].double()
-        scales = s["scales"].double()
+        unit = 2.0 ** (s["scales"].double() - 127.0)
         at_in = torch.arange(W.shape[1], device=DEV) // 128
-        for i in range(scales.shape[0]):
-            W[128 * i:128 * i + 128] *= scales[i][at_in]
+        for i in range(unit.shape[0]):
+            W[128 * i:128 * i + 128] *= unit[i][at_in]
         z = x @ W.t()
         if op == "dense":
             return z
