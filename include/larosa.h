@@ -41,7 +41,11 @@
 extern "C" {
 #endif
 
-typedef enum { LAROSA_F16 = 0, LAROSA_BF16 = 1 } larosa_dtype;
+typedef enum {
+  LAROSA_F16 = 0,
+  LAROSA_BF16 = 1,
+  LAROSA_F32 = 2              /* logits of larosa_logprobs only */
+} larosa_dtype;
 
 typedef enum {
   LAROSA_OK = 0,
@@ -385,6 +389,61 @@ size_t larosa_layer_kv4_workspace_bytes(const larosa_layer* L, const larosa_kv4_
 int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, int layer, const larosa_kv4_batch* batch,
                              const larosa_rotary* rotary, float scale, int window, int max_len, const void* x, void* x_out,
                              const larosa_trace* trace, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Weights in 8-bit floating point: products of any number of rows (prompts, the output head) and what is read off the head's
+ * logits.  The method leaves prompts and the output head dense (Sec. 4.4 is about decoding; perplexity and scored choices are what it is judged
+ * by, Tables 1 and 2); the format is this library's own:
+ *   codes   e4m3 (sign, 4 bits of exponent, 3 of mantissa; at most 448; 0x7F and 0xFF are NaN)
+ *   scales  one byte for each block of 128: 2^(byte - 127), a power of two, which the matrix instructions apply by themselves
+ *   weight  of d_out output and d_in input channels: codes [d_out, P], scales [ceil(d_out / 128), S], a block is 128 x 128
+ *   rows    codes [n_rows, P], scales [n_rows, S], a block is 128 neighbouring values of a row
+ *           P = d_in rounded up to 16 (zeros behind d_in), S = ceil(d_in / 128) rounded up to 4 (127 behind the last block)
+ *   value   = code * 2^(byte - 127), with the byte of the value's block
+ * A block's scale is the least 2^e >= 2^-64 for which its largest magnitude is at most 448 * 2^e, its codes are nearest to value / 2^e, ties
+ * to the even one; a block that holds a NaN or infinity gets scale 1 and NaN codes.  Values below 2^-74 in a block of such values count as 0.
+ * d_in is at most 2^20, d_out and n_rows at most 2^24; codes are 16-byte aligned, scales 4-byte. */
+
+/* W [d_in, d_out] (16-bit, type t, the layout of every weight of this library; d_out a multiple of 8) -> codes, scales. */
+int larosa_quantize_w8(const void* W, int d_in, int d_out, larosa_dtype t, void* codes, void* scales, void* stream);
+
+/* x [n_rows, d] (16-bit, type t, rows ld_x apart, a multiple of 8) -> codes, scales.  rms_eps >= 0: behind a norm,
+ * x / sqrt(mean(x^2) + rms_eps) * rms (rms [d] or NULL = 1), in fp32 and not rounded before the codes; rms_eps < 0: as they are. */
+int larosa_quantize_rows8(const void* x, int ld_x, int n_rows, int d, const void* rms, float rms_eps, larosa_dtype t, void* codes,
+                          void* scales, void* stream);
+
+/* y[m, o] = sum_i x[m, i] W[o, i] over the values that rows and weight stand for; y [n_rows, d_out] (type t, rows ld_y apart, a multiple of
+ * 8), rounded once.  d_out is a multiple of 8.  Sums are fp32; from 17 rows on the products of eight neighbours are added by the 8-bit matrix
+ * instruction, which cuts them 13 bits below the largest one's exponent (about 2^-16 of the result's norm, with a few strong channels 2^-14.5).
+ * Workspace: larosa_product8_workspace_bytes, initialised by larosa_workspace_init.  Up to 2^24 tiles of 128 rows x 128 channels. */
+size_t larosa_product8_workspace_bytes(int n_rows, int d_in, int d_out);
+int larosa_product8(const void* w_codes, const void* w_scales, const void* x_codes, const void* x_scales, void* y, int ld_y,
+                    int n_rows, int d_in, int d_out, larosa_dtype t, void* ws, size_t ws_bytes, void* stream);
+
+/* larosa_quantize_rows8 into the workspace and larosa_product8: x, y and rms in type t. */
+size_t larosa_dense_w8_workspace_bytes(int n_rows, int d_in, int d_out);
+int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, int ld_x, const void* rms, float rms_eps, void* y,
+                    int ld_y, int n_rows, int d_in, int d_out, larosa_dtype t, void* ws, size_t ws_bytes, void* stream);
+
+/* Log probabilities.  For each row of logits [n_rows, n_vocab] (type t, F32 too; rows ld apart, any ld >= n_vocab; aligned to their type), with
+ * z = scale * logit (scale > 0: one over a temperature):
+ *   logp[r, i]  = z[given[r, i]] - ln sum exp z       given, logp [n_rows, n_given]; a negative id is padding: 0; an id >= n_vocab: NaN
+ *   entropy[r]  = - sum p ln p, in nats               [n_rows], nullable
+ *   top_id, top_logp [n_rows, n_top]: the n_top largest logits, ties to the lower id, with their log probabilities (top_logp nullable)
+ * A logit of -infinity has probability 0; a row of nothing else gets logp -infinity and entropy 0.  A row that holds a NaN or +infinity gets
+ * NaN everywhere and top_id -1.  Sums and statistics are fp32.  n_given >= 0, 0 <= n_top <= min(64, n_vocab); outputs that are not asked
+ * for (n_given or n_top 0) may be NULL.
+ * Workspace: larosa_logprobs_workspace_bytes, initialised by larosa_workspace_init; at most 2^24 rows of at most 2^30 logits. */
+size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, larosa_dtype t);
+int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_dtype t, float scale, const int32_t* given,
+                    int n_given, float* logp, float* entropy, int n_top, int32_t* top_id, float* top_logp, void* ws,
+                    size_t ws_bytes, void* stream);
+
+/* From hidden rows to log probabilities: norm (rms, rms_eps as above), rows to 8 bits, the output head (codes, scales of n_vocab output
+ * channels, any number), larosa_logprobs of its fp32 logits.  The logits of a part of the rows at a time lie in the workspace. */
+size_t larosa_score_w8_workspace_bytes(int n_rows, int d_in, int n_vocab, int n_top);
+int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, int ld_x, const void* rms, float rms_eps, int n_rows,
+                    int d_in, int n_vocab, larosa_dtype t, float scale, const int32_t* given, int n_given, float* logp,
+                    float* entropy, int n_top, int32_t* top_id, float* top_logp, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- NOT part of the stable interface: launch tuning for tests and experiments.
  * Process-wide host state read by every call (launch shapes AND workspace sizes depend on it): not

@@ -15,7 +15,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblarosa.so")
 
-F16, BF16 = 0, 1
+F16, BF16, F32 = 0, 1, 2
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, -1, -2, -3, -4
 
 _lib = None
@@ -122,6 +122,16 @@ def lib() -> ctypes.CDLL:
         L.larosa_layer_kv4_workspace_bytes.argtypes = [ctypes.POINTER(_Layer), cache, batch, i]
         L.larosa_layer_forward_kv4.argtypes = [ctypes.POINTER(_Layer), cache, i, batch, rotary, ctypes.c_float, i, i, vp, vp,
                                                ctypes.POINTER(_Trace), vp, sz, vp]
+        f32 = ctypes.c_float
+        L.larosa_quantize_w8.argtypes = [vp, i, i, i, vp, vp, vp]
+        L.larosa_quantize_rows8.argtypes = [vp, i, i, i, vp, f32, i, vp, vp, vp]
+        for name, sizes in (("product8", 3), ("dense_w8", 3), ("logprobs", 4), ("score_w8", 4)):
+            query = getattr(L, f"larosa_{name}_workspace_bytes")
+            query.restype, query.argtypes = sz, [i] * sizes
+        L.larosa_product8.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, sz, vp]
+        L.larosa_dense_w8.argtypes = [vp, vp, vp, i, vp, f32, vp, i, i, i, i, i, vp, sz, vp]
+        L.larosa_logprobs.argtypes = [vp, i, i, i, i, f32, vp, i, vp, vp, i, vp, vp, vp, sz, vp]
+        L.larosa_score_w8.argtypes = [vp, vp, vp, i, vp, f32, i, i, i, i, f32, vp, i, vp, vp, i, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -613,3 +623,182 @@ def layer_forward_kv4(layer: Layer, cache: KvCache, index: int, batch: KvBatch, 
                                           _ptr(x_out), ctypes.byref(tr) if tr is not None else None, ws.ptr, ws.nbytes, _cache_stream(cache)),
            "larosa_layer_forward_kv4")
     return x_out
+
+
+# ---- weights in 8-bit floating point, products over them, log probabilities -------------------------------
+
+def codes_pitch8(d: int) -> int:
+    """Bytes between the rows of the codes of d channels."""
+    return -(-d // 16) * 16
+
+
+def scales_pitch8(d: int) -> int:
+    """Bytes between the rows of their scales."""
+    return -(-d // 512) * 4
+
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _held8(codes, scales, d_in: int, rows_of_block: int, device: int):
+    """Addresses of codes and scales; other shapes or types would be misread on the device."""
+    n = codes.shape[0]
+    if codes.dtype not in _CODES or scales.dtype is not torch.uint8 or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("codes are contiguous float8_e4m3fn (or uint8), scales contiguous uint8")
+    if codes.shape != (n, codes_pitch8(d_in)) or scales.shape != (-(-n // rows_of_block), scales_pitch8(d_in)):
+        raise ValueError(f"codes [n, {codes_pitch8(d_in)}] and scales [n / {rows_of_block} up, {scales_pitch8(d_in)}] of {d_in} channels")
+    if codes.get_device() != device or scales.get_device() != device:
+        raise ValueError("codes and scales lie on the current device")
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def _device_stream(*tensors):
+    """The current device and its stream; every tensor has to lie there."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("every tensor lies on the current device")
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
+def _matrix16(t, code: int) -> int:
+    """Distance between the rows of a matrix of the type `code`."""
+    if t.dtype is not torch_dtype(code) or t.dim() != 2:
+        raise ValueError("rows are a matrix of the call's type")
+    ld, one = t.stride()
+    if one != 1 and t.shape[1] != 1:
+        raise ValueError("the values of a row lie next to one another")
+    return ld if t.shape[0] > 1 else max(ld, -(-t.shape[1] // 8) * 8)
+
+
+def _norm8(rms, d: int, code: int):
+    if rms is not None and (rms.dtype is not torch_dtype(code) or rms.shape != (d,) or not rms.is_contiguous()):
+        raise ValueError("rms is a contiguous vector of the call's type, a value for each channel")
+    return _ptr(rms)
+
+
+def quantize_w8(W, dtype):
+    """e4m3 codes (float8_e4m3fn [d_out, d_in up to 16]) and scale bytes (uint8 [d_out / 128 up, d_in / 128 up, up to 4]) of
+    W [d_in, d_out]."""
+    code = dtype_code(dtype)
+    d_in, d_out = W.shape
+    _, stream = _device_stream(W)
+    if W.dtype is not torch_dtype(code) or not W.is_contiguous():
+        raise ValueError("W is a contiguous matrix of the call's type")
+    codes = torch.empty(d_out, codes_pitch8(d_in), dtype=torch.float8_e4m3fn, device=W.device)
+    scales = torch.empty(-(-d_out // 128), scales_pitch8(d_in), dtype=torch.uint8, device=W.device)
+    _check(lib().larosa_quantize_w8(_ptr(W), d_in, d_out, code, _ptr(codes), _ptr(scales), stream), "larosa_quantize_w8")
+    return codes, scales
+
+
+def quantize_rows8(x, dtype, rms=None, rms_eps: float = -1.0):
+    """Codes [n, d up to 16] and scale bytes [n, d / 128 up, up to 4] of x [n, d]; rms_eps >= 0: behind a norm (rms: its scale)."""
+    code = dtype_code(dtype)
+    n, d = x.shape
+    _, stream = _device_stream(x, rms)
+    ld = _matrix16(x, code)
+    codes = torch.empty(n, codes_pitch8(d), dtype=torch.float8_e4m3fn, device=x.device)
+    scales = torch.empty(n, scales_pitch8(d), dtype=torch.uint8, device=x.device)
+    _check(lib().larosa_quantize_rows8(_ptr(x), ld, n, d, _norm8(rms, d, code), rms_eps, code, _ptr(codes), _ptr(scales), stream),
+           "larosa_quantize_rows8")
+    return codes, scales
+
+
+def _sized(nbytes: int, where: str, device) -> Workspace:
+    if nbytes == 0:
+        raise LarosaError(EINVAL, where)
+    return Workspace(nbytes, device)
+
+
+def product8_workspace(n_rows: int, d_in: int, d_out: int, device="cuda:0") -> Workspace:
+    return _sized(lib().larosa_product8_workspace_bytes(n_rows, d_in, d_out), "larosa_product8_workspace_bytes", device)
+
+
+def product8(w_codes, w_scales, x_codes, x_scales, d_in: int, y, dtype, ws: Workspace):
+    """y [n, d_out] = the product of rows and weight, both in 8 bits."""
+    code = dtype_code(dtype)
+    device, stream = _device_stream(y, ws.buf)
+    wc, wsc = _held8(w_codes, w_scales, d_in, 128, device)
+    xc, xsc = _held8(x_codes, x_scales, d_in, 1, device)
+    ld_y = _matrix16(y, code)
+    n, d_out = y.shape
+    if w_codes.shape[0] != d_out or x_codes.shape[0] != n:
+        raise ValueError("y has a row for each row of x and a column for each output channel")
+    _check(lib().larosa_product8(wc, wsc, xc, xsc, _ptr(y), ld_y, n, d_in, d_out, code, ws.ptr, ws.nbytes, stream), "larosa_product8")
+    return y
+
+
+def dense_w8_workspace(n_rows: int, d_in: int, d_out: int, device="cuda:0") -> Workspace:
+    return _sized(lib().larosa_dense_w8_workspace_bytes(n_rows, d_in, d_out), "larosa_dense_w8_workspace_bytes", device)
+
+
+def dense_w8(w_codes, w_scales, x, y, dtype, ws: Workspace, rms=None, rms_eps: float = -1.0):
+    """y [n, d_out] = x [n, d_in] (behind a norm if rms_eps >= 0), brought to 8 bits, times the weight."""
+    code = dtype_code(dtype)
+    device, stream = _device_stream(x, y, rms, ws.buf)
+    n, d_in = x.shape
+    wc, wsc = _held8(w_codes, w_scales, d_in, 128, device)
+    ld_x, ld_y = _matrix16(x, code), _matrix16(y, code)
+    if y.shape != (n, w_codes.shape[0]):
+        raise ValueError("y has a row for each row of x and a column for each output channel")
+    _check(lib().larosa_dense_w8(wc, wsc, _ptr(x), ld_x, _norm8(rms, d_in, code), rms_eps, _ptr(y), ld_y, n, d_in, y.shape[1], code,
+                                 ws.ptr, ws.nbytes, stream), "larosa_dense_w8")
+    return y
+
+
+_LOGITS = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _outputs8(n: int, given, logp, entropy, top_id, top_logp):
+    """Numbers of given and of top tokens."""
+    n_given = 0 if given is None else given.shape[1]
+    n_top = 0 if top_id is None else top_id.shape[1]
+    for t, width, kind in ((given, n_given, torch.int32), (logp, n_given, torch.float32), (top_id, n_top, torch.int32),
+                           (top_logp, n_top, torch.float32)):
+        if t is not None and (t.dtype is not kind or t.shape != (n, width) or not t.is_contiguous()):
+            raise ValueError("given and top_id are contiguous int32, logp and top_logp contiguous float32 of their shapes")
+    if entropy is not None and (entropy.dtype is not torch.float32 or entropy.shape != (n,) or not entropy.is_contiguous()):
+        raise ValueError("entropy is a contiguous float32 vector, a value for each row")
+    if (logp is None) != (given is None) and n_given:
+        raise ValueError("given tokens and logp come together")
+    return n_given, n_top
+
+
+def logprobs_workspace(n_rows: int, n_vocab: int, n_top: int = 0, dtype="bf16", device="cuda:0") -> Workspace:
+    """For logits of any type: dtype is only asked for because 32-bit logits take more room."""
+    code = F32 if dtype in (F32, "f32", torch.float32) else dtype_code(dtype)
+    return _sized(lib().larosa_logprobs_workspace_bytes(n_rows, n_vocab, n_top, code), "larosa_logprobs_workspace_bytes", device)
+
+
+def logprobs(logits, given, logp, ws: Workspace, entropy=None, top_id=None, top_logp=None, scale: float = 1.0):
+    """Log probabilities of the given tokens [n, n_given] under softmax(scale * logits [n, n_vocab]), the rows' entropy [n] and the most
+    probable tokens top_id [n, n_top] with theirs, top_logp."""
+    device, stream = _device_stream(logits, given, logp, entropy, top_id, top_logp, ws.buf)
+    n, V = logits.shape
+    ld, one = logits.stride()
+    if logits.dtype not in _LOGITS or (one != 1 and V > 1):
+        raise ValueError("logits are float16, bfloat16 or float32, those of a row next to one another")
+    n_given, n_top = _outputs8(n, given, logp, entropy, top_id, top_logp)
+    _check(lib().larosa_logprobs(_ptr(logits), ld if n > 1 else max(ld, V), n, V, _LOGITS[logits.dtype], scale, _ptr(given), n_given,
+                                 _ptr(logp), _ptr(entropy), n_top, _ptr(top_id), _ptr(top_logp), ws.ptr, ws.nbytes, stream),
+           "larosa_logprobs")
+    return logp
+
+
+def score_w8_workspace(n_rows: int, d_in: int, n_vocab: int, n_top: int = 0, device="cuda:0") -> Workspace:
+    return _sized(lib().larosa_score_w8_workspace_bytes(n_rows, d_in, n_vocab, n_top), "larosa_score_w8_workspace_bytes", device)
+
+
+def score_w8(w_codes, w_scales, x, given, logp, dtype, ws: Workspace, entropy=None, top_id=None, top_logp=None, scale: float = 1.0,
+             rms=None, rms_eps: float = -1.0):
+    """logprobs of the output head's logits of x [n, d_in] (behind the final norm if rms_eps >= 0); the head in 8 bits."""
+    code = dtype_code(dtype)
+    device, stream = _device_stream(x, given, logp, entropy, top_id, top_logp, rms, ws.buf)
+    n, d_in = x.shape
+    wc, wsc = _held8(w_codes, w_scales, d_in, 128, device)
+    ld_x = _matrix16(x, code)
+    n_given, n_top = _outputs8(n, given, logp, entropy, top_id, top_logp)
+    _check(lib().larosa_score_w8(wc, wsc, _ptr(x), ld_x, _norm8(rms, d_in, code), rms_eps, n, d_in, w_codes.shape[0], code, scale,
+                                 _ptr(given), n_given, _ptr(logp), _ptr(entropy), n_top, _ptr(top_id), _ptr(top_logp), ws.ptr,
+                                 ws.nbytes, stream), "larosa_score_w8")
+    return logp

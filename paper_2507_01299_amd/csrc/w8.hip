@@ -1,0 +1,635 @@
+// Weights and rows in 8-bit floating point (e4m3) with a power-of-two scale for each block of 128, and their product.
+//
+// A scale that is a power of two is an operand of the matrix instructions (v_mfma_scale_f32_*_f8f6f4 takes a byte for every 32 codes of
+// a row), so a block's scale costs nothing: with scales of 32 bits every 128 products would be followed by a multiply-add per sum
+// outside the matrix cores, and a loop of both reaches 2.9 PFLOP/s here where the scaled instruction alone reaches 4.0 - 4.3.  e4m3 is a
+// floating format: a scale's own fraction bits would only move the border of its subnormal numbers.
+#include <type_traits>
+
+#include "kernels.hpp"
+#include "lds_load.hpp"
+#include "numeric.hpp"
+#include "w8.hpp"
+
+namespace larosa {
+
+namespace {
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bfloat2 __attribute__((ext_vector_type(2)));
+
+// ---- codes -------------------------------------------------------------------------------------------------
+
+constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;
+constexpr uint32_t kScaleOne = 127, kScaleLeast = 63;    // bytes of 2^0 and 2^-64
+
+// Scale byte of a block whose largest magnitude has these bits: the least 2^e >= 2^-64 with m <= 448 2^e.  m = (1 + f) 2^p lies
+// at or below 1.75 2^8 2^e from e = p - 8 on, from p - 7 if f > 0.75.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t magnitude) {
+  const uint32_t p = (magnitude >> 23) + ((magnitude & 0x7FFFFFu) > 0x600000u ? 1u : 0u);
+  return p > kScaleLeast + 8 ? p - 8 : kScaleLeast;
+}
+__device__ __forceinline__ bool finite_bits(uint32_t magnitude) { return magnitude < 0x7F800000u; }
+// 2^-e of a scale byte e + 127 (63 .. 247)
+__device__ __forceinline__ float unscale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// Codes of four values: nearest, ties to even; the instruction rounds so, and no value is above 448.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float unit) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a * unit, b * unit, 0, false);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c * unit, d * unit, lo, true));
+}
+
+__device__ __forceinline__ uint32_t max_u32(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int ROR>
+__device__ __forceinline__ uint32_t row_rotated_u32(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(v), static_cast<int>(v), 0x120 + ROR, 0xF, 0xF, false));
+}
+// largest over each 16 consecutive lanes, in all of them
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max_u32(v, row_rotated_u32<8>(v));
+  v = max_u32(v, row_rotated_u32<4>(v));
+  v = max_u32(v, row_rotated_u32<2>(v));
+  return max_u32(v, row_rotated_u32<1>(v));
+}
+
+__device__ __forceinline__ uint32_t largest8(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) m = max_u32(m, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+  return m;
+}
+
+// Eight values of a row from a lane, 16 lanes to a block: its codes (8 bytes) and the block's scale byte.
+__device__ __forceinline__ uint2 block_codes(const float (&v)[8], uint32_t& byte) {
+  const uint32_t m = row_max(largest8(v));
+  const bool fine = finite_bits(m);
+  byte = fine ? scale_byte(m) : kScaleOne;
+  const float unit = unscale(byte);
+  const uint32_t lo = codes4(v[0], v[1], v[2], v[3], unit), hi = codes4(v[4], v[5], v[6], v[7], unit);
+  return fine ? make_uint2(lo, hi) : make_uint2(kNanCodes, kNanCodes);
+}
+
+// Rows to codes, HBM-bound (2 bytes in, 1 out).  A wave takes 512 columns (16 bytes a lane, four blocks) of four rows at once; a
+// row's four scale bytes are one word.
+constexpr int kRowsAtOnce = 4;
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_rows8_kernel(const uint16_t* __restrict__ x, long ld_x, int n_rows, int d,
+                                                             uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int pitch = (d + 15) / 16 * 16, spitch = ((d + 127) / 128 + 3) / 4 * 4;
+  const int col = blockIdx.x * 512 + lane * 8;
+  const int row0 = (blockIdx.y * 4 + wave) * kRowsAtOnce;
+  uint4 raw[kRowsAtOnce];
+#pragma unroll
+  for (int r = 0; r < kRowsAtOnce; ++r) {
+    raw[r] = make_uint4(0u, 0u, 0u, 0u);
+    if (row0 + r < n_rows && col < d) raw[r] = *reinterpret_cast<const uint4*>(x + (row0 + r) * ld_x + col);
+  }
+#pragma unroll
+  for (int r = 0; r < kRowsAtOnce; ++r) {
+    float v[8];
+    unpack8<T>(raw[r], v);
+    uint32_t byte;
+    uint2 c = block_codes(v, byte);
+    if (col >= d) c = make_uint2(0u, 0u);
+    if (col >= (d + 127) / 128 * 128) byte = kScaleOne;
+    const uint32_t word = __builtin_amdgcn_readlane(byte, 0) | (__builtin_amdgcn_readlane(byte, 16) << 8) |
+                          (__builtin_amdgcn_readlane(byte, 32) << 16) | (__builtin_amdgcn_readlane(byte, 48) << 24);
+    if (row0 + r < n_rows) {
+      if (col < pitch) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(row0 + r) * pitch + col) = c;
+      if (lane == 0) *reinterpret_cast<uint32_t*>(scales + static_cast<size_t>(row0 + r) * spitch + blockIdx.x * 4) = word;
+    }
+  }
+}
+
+// The same behind a norm, v = x / sqrt(mean(x^2) + eps) * g in fp32 and not rounded before the codes: a workgroup per row, which
+// reads it twice (the second time from the caches).
+template <typename T>
+__global__ __launch_bounds__(512) void quantize_normed_rows8_kernel(const uint16_t* __restrict__ x, long ld_x, int n_rows, int d,
+                                                                    const uint16_t* __restrict__ g, float eps,
+                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  __shared__ float sums[8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int pitch = (d + 15) / 16 * 16, spitch = ((d + 127) / 128 + 3) / 4 * 4;
+  const size_t row = blockIdx.x;
+  const uint16_t* const xr = x + row * ld_x;
+  float sum = 0.f;
+  for (int col = tid * 8; col < d; col += 512 * 8) {
+    float v[8];
+    unpack8<T>(*reinterpret_cast<const uint4*>(xr + col), v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum += sums[k];
+  const float rinv = 1.0f / sqrtf(sum / static_cast<float>(d) + eps);
+  for (int col0 = wave * 512; col0 < spitch * 128; col0 += 512 * 8) {     // (uniform over the wave)
+    const int col = col0 + lane * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (col < d) {
+      unpack8<T>(*reinterpret_cast<const uint4*>(xr + col), v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= rinv;
+      if (g) {
+        float w[8];
+        unpack8<T>(*reinterpret_cast<const uint4*>(g + col), w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= w[k];
+      }
+    }
+    uint32_t byte;
+    uint2 c = block_codes(v, byte);
+    if (col >= d) c = make_uint2(0u, 0u);
+    if (col >= (d + 127) / 128 * 128) byte = kScaleOne;
+    const uint32_t word = __builtin_amdgcn_readlane(byte, 0) | (__builtin_amdgcn_readlane(byte, 16) << 8) |
+                          (__builtin_amdgcn_readlane(byte, 32) << 16) | (__builtin_amdgcn_readlane(byte, 48) << 24);
+    if (col < pitch) *reinterpret_cast<uint2*>(codes + row * pitch + col) = c;
+    if (lane == 0) *reinterpret_cast<uint32_t*>(scales + row * spitch + col0 / 128) = word;
+  }
+}
+
+// A weight [d_in, d_out] to codes [d_out, d_in], HBM-bound: a workgroup per block of 128 x 128.  A lane holds 8 input x 8 output
+// channels (eight 16-byte loads, 256 bytes of a row together), so that the instruction that makes codes of two values gets neighbours
+// along the input; the codes are turned in LDS and leave as 128 bytes of each output channel.
+constexpr int kTurnPitch = 128 + 8;    // bytes of an output channel in LDS (8-byte writes of 16 lanes fall into different banks)
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_w8_kernel(const uint16_t* __restrict__ W, int d_in, int d_out,
+                                                          uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  __shared__ __attribute__((aligned(16))) uint8_t turn[128 * kTurnPitch];
+  __shared__ uint32_t most[4];
+  const int tid = threadIdx.x;
+  const int i0 = blockIdx.y * 128, o0 = blockIdx.x * 128;
+  const int pitch = (d_in + 15) / 16 * 16, blocks = (d_in + 127) / 128, spitch = (blocks + 3) / 4 * 4;
+  const int ki = tid / 16 * 8, oc = tid % 16 * 8;      // the lane's channels within the block
+  uint4 raw[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    raw[k] = make_uint4(0u, 0u, 0u, 0u);
+    if (i0 + ki + k < d_in && o0 + oc < d_out) raw[k] = *reinterpret_cast<const uint4*>(W + static_cast<size_t>(i0 + ki + k) * d_out + o0 + oc);
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float v[8];
+    unpack8<T>(raw[k], v);
+    m = max_u32(m, largest8(v));
+  }
+  m = row_max(m);
+  m = max_u32(max_u32(__builtin_amdgcn_readlane(m, 0), __builtin_amdgcn_readlane(m, 16)),
+              max_u32(__builtin_amdgcn_readlane(m, 32), __builtin_amdgcn_readlane(m, 48)));
+  if ((tid & 63) == 0) most[tid >> 6] = m;
+  __syncthreads();
+  m = max_u32(max_u32(most[0], most[1]), max_u32(most[2], most[3]));
+  const bool fine = finite_bits(m);
+  const uint32_t byte = fine ? scale_byte(m) : kScaleOne;
+  const float unit = unscale(byte);
+  if (tid == 0) scales[static_cast<size_t>(blockIdx.x) * spitch + blockIdx.y] = static_cast<uint8_t>(byte);
+  if (tid < spitch - blocks && blockIdx.y == 0) scales[static_cast<size_t>(blockIdx.x) * spitch + blocks + tid] = kScaleOne;
+  float v[8][8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) unpack8<T>(raw[k], v[k]);
+#pragma unroll
+  for (int o = 0; o < 8; ++o) {
+    uint2 c = make_uint2(codes4(v[0][o], v[1][o], v[2][o], v[3][o], unit), codes4(v[4][o], v[5][o], v[6][o], v[7][o], unit));
+    if (!fine) c = make_uint2(kNanCodes, kNanCodes);
+    if (i0 + ki >= d_in) c = make_uint2(0u, 0u);       // (d_in is a multiple of 8)
+    *reinterpret_cast<uint2*>(turn + (oc + o) * kTurnPitch + ki) = c;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int o = p * 32 + tid / 8, piece = tid % 8 * 16;
+    if (o0 + o < d_out && i0 + piece < pitch) {
+      const uint2 lo = *reinterpret_cast<const uint2*>(turn + o * kTurnPitch + piece);
+      const uint2 hi = *reinterpret_cast<const uint2*>(turn + o * kTurnPitch + piece + 8);
+      *reinterpret_cast<uint4*>(codes + static_cast<size_t>(o0 + o) * pitch + i0 + piece) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  }
+}
+
+// ---- the product, many rows --------------------------------------------------------------------------------
+// v_mfma_scale_f32_32x32x64 (e4m3 both sides): its first operand holds output channels (lane l: channel l % 32, 32 codes along k from
+// 32 (l / 32) on), its second rows of x the same way; register r of lane l of the result is channel 8 (r / 4) + 4 (l / 32) + r % 4, row
+// l % 32.  A workgroup of 4 waves (2 x 2) owns 64 MO output channels x 64 MT rows, a wave 32 MO x 32 MT.
+//  * k-tiles of 64: 64 bytes of each row, brought straight into LDS, kStages tiles ahead; the 16-byte pieces of a row are exchanged by
+//    its number, so that the rows a read touches lie in different banks.  One barrier per k-tile: behind it the next tile is read
+//    while this one, in registers, is multiplied, and this one's stage takes the loads of the tile kStages further.
+//  * Scales of the rows: a word holds those of four blocks (eight k-tiles) of a row; words of all rows of the tile come into LDS with the
+//    first of the eight, and a byte is read per block.  A wave's channels lie in one block of the weight: its scale is uniform.
+// The sums are fp32, but the instruction adds the products of eight neighbours first, cut 13 bits below the largest one's exponent (found
+// by probing; the 8-bit instructions before it do the same).  A product has 7 bits behind its first, so only those 2^7 times smaller than a
+// neighbour lose any: 1.4e-5 of the result's norm on random data, 4e-5 with a few strong channels, where a 16-bit result rounds by 2e-4
+// (f16) or 1.7e-3, the codes by 2.6e-2, and a block's smallest code is 2^-18 of its largest.  Whole sums in bf16 cost more than twice the time.
+constexpr int kKTile8 = 64;
+constexpr int kStages8 = 4;
+
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void tile_landed() {
+  static_assert(N < 64, "vmcnt is a 6-bit field");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// 4 bytes per lane, lane l's to LDS byte lds_byte + 4 l
+__device__ __forceinline__ void load_words_to_lds(u32x4 buf, uint32_t lds_byte, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_byte), "v"(off), "s"(buf) : "m0");
+}
+
+// Tiles are numbered in bands of kBand8 tiles of rows, output channel by output channel inside a band; an XCD takes consecutive ones.
+constexpr int kBand8 = 4;
+struct TileAt8 { int m, o; };
+__device__ __forceinline__ TileAt8 tile_of8(int number, int tiles_m, int tiles_o) {
+  const int band = __builtin_amdgcn_readfirstlane(number / (kBand8 * tiles_o)), left = tiles_m - band * kBand8;
+  const int rows = left < kBand8 ? left : kBand8;
+  number -= band * kBand8 * tiles_o;
+  const int o = __builtin_amdgcn_readfirstlane(number / rows);
+  return {band * kBand8 + number - o * rows, o};
+}
+
+__device__ __forceinline__ uint2 pack_out4(F16, const float (&v)[4]) { return pack4<F16>(v); }
+__device__ __forceinline__ uint2 pack_out4(BF16, const float (&v)[4]) { return pack4<BF16>(v); }
+struct F32 {};                // logits that the caller's next step reads in full
+
+template <typename OUT, int MO, int MT>
+__global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel(Product8Args a) {
+  constexpr int TO = 64 * MO, TT = 64 * MT;
+  constexpr int kBytesO = TO * kKTile8, kBytesT = TT * kKTile8, kStageBytes = kBytesO + kBytesT;
+  constexpr int LO = kBytesO / 4096, LT = kBytesT / 4096, kLoads = LO + LT;      // wave-loads per wave and stage
+  constexpr int kScaleBytes = TT * 4;
+  constexpr int kRing = kStages8 * kStageBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[kRing + 2 * kScaleBytes];
+  __shared__ int last_flag;
+
+  const int tiles = a.tiles_m * a.tiles_o, jobs = tiles * a.splits;
+  const int per_xcd = (jobs + 7) >> 3;
+  const int job = static_cast<int>(blockIdx.x & 7) * per_xcd + static_cast<int>(blockIdx.x >> 3);
+  if (job >= jobs) return;
+  const int tile = __builtin_amdgcn_readfirstlane(job / a.splits), split = job - tile * a.splits;
+  const TileAt8 at = tile_of8(tile, a.tiles_m, a.tiles_o);
+  const int m0 = at.m * TT, o0 = at.o * TO;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wo = w >> 1, wt = w & 1;
+  const int pitch = (a.d_in + 15) / 16 * 16, blocks = (a.d_in + 127) / 128, spitch = (blocks + 3) / 4 * 4;
+  const int kb0 = split * a.blocks_per, kb1 = min(blocks, kb0 + a.blocks_per);
+  const int rows_o = min(TO, a.d_out - o0), rows_t = min(TT, a.n_rows - m0);
+
+  // ---- loads.  A panel's rows behind the last lie outside its buffer and arrive as zeros.
+  const u32x4 buf_o = raw_buffer(a.w.codes + static_cast<size_t>(o0) * pitch, static_cast<uint32_t>(rows_o) * pitch);
+  const u32x4 buf_t = raw_buffer(a.x.codes + static_cast<size_t>(m0) * pitch, static_cast<uint32_t>(rows_t) * pitch);
+  const u32x4 buf_s = raw_buffer(a.x.scales + static_cast<size_t>(m0) * spitch, static_cast<uint32_t>(rows_t) * spitch);
+  // wave-load q of wave w fills 16 rows from 16 (4 q + w) on; piece p of row r holds codes 16 (p ^ (r / 4 % 4)) .. + 15 of the k-tile
+  const int lrow = 16 * w + (lane >> 2), lpiece = 16 * ((lane & 3) ^ ((lane >> 4) & 3));
+  uint32_t off[LO > LT ? LO : LT];
+#pragma unroll
+  for (int q = 0; q < (LO > LT ? LO : LT); ++q) off[q] = static_cast<uint32_t>((64 * q + lrow) * pitch + lpiece);
+  const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char*)lds));
+  const int k_end = min(pitch, kb1 * 128);
+  int f_k = kb0 * 128, f_stage = 0;
+  auto fetch_piece = [&](int q) __attribute__((always_inline)) {
+    const uint32_t to = lds_base + f_stage * kStageBytes + w * 1024;
+    const bool in = f_k + lpiece < k_end;        // (pitch is a multiple of 16: a piece is inside or not)
+    if (q < LO) load_to_lds(buf_o, to + q * 4096, in ? off[q] + f_k : kOutside);
+    else load_to_lds(buf_t, to + kBytesO + (q - LO) * 4096, in ? off[q - LO] + f_k : kOutside);
+  };
+  // scale words of the four blocks from f_k on, with the first of their k-tiles and in front of its loads
+  const uint32_t off_s = static_cast<uint32_t>((64 * w + lane) * spitch);
+  auto fetch_scales = [&]() __attribute__((always_inline)) {
+    if (64 * w < TT && f_k < k_end)
+      load_words_to_lds(buf_s, lds_base + kRing + ((f_k >> 9) & 1) * kScaleBytes + w * 256, off_s + (f_k >> 9) * 4);
+  };
+  auto fetch_next = [&]() __attribute__((always_inline)) {
+    f_k += kKTile8;
+    f_stage = (f_stage + 1) & (kStages8 - 1);
+  };
+
+  // ---- operand reads: the two pieces of a lane's 32 codes
+  const int sw = (lane >> 2) & 3, half = lane >> 5;
+  const int adr_o = (wo * MO * 32 + (lane & 31)) * kKTile8 + ((2 * half) ^ sw) * 16;
+  const int adr_t = kBytesO + (wt * MT * 32 + (lane & 31)) * kKTile8 + ((2 * half) ^ sw) * 16;
+  auto read_piece = [&](int stage, int r, u32x4 (&v)[2 * (MO + MT)]) __attribute__((always_inline)) {
+    const int adr = (r < 2 * MO ? adr_o + (r >> 1) * (32 * kKTile8) : adr_t + ((r - 2 * MO) >> 1) * (32 * kKTile8)) ^ (16 * (r & 1));
+    v[r] = *(const __attribute__((address_space(3))) u32x4*)((const lds_char*)lds + stage * kStageBytes + adr);
+  };
+  auto operand = [&](const u32x4 (&v)[2 * (MO + MT)], int r) __attribute__((always_inline)) {
+    return __builtin_shufflevector(__builtin_bit_cast(__attribute__((ext_vector_type(4))) int, v[2 * r]),
+                                   __builtin_bit_cast(__attribute__((ext_vector_type(4))) int, v[2 * r + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const int adr_s = kRing + (wt * MT * 32 + (lane & 31)) * 4;
+  auto read_scales = [&](int kb, int (&s)[MT]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+      s[i] = *(const __attribute__((address_space(3))) uint8_t*)((const lds_char*)lds + adr_s + ((kb >> 2) & 1) * kScaleBytes + i * 128 + (kb & 3));
+  };
+  const int ob = min((o0 + wo * MO * 32) / 128, (a.d_out - 1) / 128);            // the wave's block of output channels
+  const uint32_t* const w_scales = reinterpret_cast<const uint32_t*>(a.w.scales + static_cast<size_t>(ob) * spitch);
+  uint32_t w_word = w_scales[kb0 >> 2], w_next = 0;
+  int s_w = 0, s_t[MT];
+
+  float16v acc[MO][MT];
+#pragma unroll
+  for (int i = 0; i < MO; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  // the products of one k-tile; between them the reads of the next (stage st) and the loads of a later one
+  auto products = [&](const u32x4 (&now)[2 * (MO + MT)], u32x4 (&next)[2 * (MO + MT)], int st) __attribute__((always_inline)) {
+    constexpr int P = MO * MT, R = 2 * (MO + MT);
+    static_for<P>([&](auto ij) {
+      constexpr int x = decltype(ij)::value;
+#pragma unroll
+      for (int r = x * R / P; r < (x + 1) * R / P; ++r) read_piece(st, r, next);
+#pragma unroll
+      for (int q = x * kLoads / P; q < (x + 1) * kLoads / P; ++q) fetch_piece(q);
+      acc[x / MT][x % MT] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(now, x / MT), operand(now, MO + x % MT),
+                                                                          acc[x / MT][x % MT], 0, 0, 0, s_w, 0, s_t[x % MT]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+
+  u32x4 v0[2 * (MO + MT)], v1[2 * (MO + MT)];
+  for (int i = 0; i < kStages8; ++i) {
+    if ((f_k & 511) == 0 || i == 0) fetch_scales();
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) fetch_piece(q);
+    fetch_next();
+  }
+  tile_landed<(kStages8 - 1) * kLoads>();
+#pragma unroll
+  for (int r = 0; r < 2 * (MO + MT); ++r) read_piece(0, r, v0);
+  int stage = 0;
+  for (int kb = kb0; kb < kb1; ++kb) {           // two k-tiles
+    if ((kb & 3) == 0 || kb == kb0) {            // (uniform)
+      if (kb > kb0) w_word = w_next;
+      if (((kb >> 2) + 1) * 4 < kb1) w_next = w_scales[(kb >> 2) + 1];
+    }
+    s_w = static_cast<int>((w_word >> (8 * (kb & 3))) & 255u);
+    tile_landed<(kStages8 - 2) * kLoads>();
+    read_scales(kb, s_t);
+    if ((f_k & 511) == 0) fetch_scales();
+    products(v0, v1, (stage + 1) & (kStages8 - 1));
+    fetch_next();
+    tile_landed<(kStages8 - 2) * kLoads>();
+    products(v1, v0, (stage + 2) & (kStages8 - 1));
+    fetch_next();
+    stage = (stage + 2) & (kStages8 - 1);
+  }
+  // every load has landed and every wave has left the operands behind
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  // ---- parts of the sum: handed over through memory as 16-byte accesses that are coherent across the chip (sc1, see
+  // gemv_core.hpp); the workgroup that arrives last adds them in their order.
+  if (a.splits > 1) {
+    constexpr int kPieces = MO * MT * 4, kPart = kPieces * 4096;    // 16-byte pieces of a lane; bytes of a part
+    constexpr int kCoherent = 16;
+    const __amdgpu_buffer_rsrc_t parts = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<char*>(a.partial) + static_cast<size_t>(tile) * a.splits * kPart, 0, a.splits * kPart, 0x00027000);
+    static_for<MO * MT>([&](auto ij) {
+      constexpr int x = decltype(ij)::value;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float16v& c = acc[x / MT][x % MT];
+        const u32x4 v = {__float_as_uint(c[4 * p]), __float_as_uint(c[4 * p + 1]), __float_as_uint(c[4 * p + 2]), __float_as_uint(c[4 * p + 3])};
+        __builtin_amdgcn_raw_buffer_store_b128(v, parts, split * kPart + (4 * x + p) * 4096 + tid * 16, 0, kCoherent);
+      }
+    });
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (tid == 0) {
+      const unsigned old = __hip_atomic_fetch_add(a.counters + static_cast<size_t>(tile) * kCounterStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last_flag = old == static_cast<unsigned>(a.splits - 1);
+    }
+    __syncthreads();
+    if (!last_flag) return;
+    if (tid == 0) __hip_atomic_store(a.counters + static_cast<size_t>(tile) * kCounterStride, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    static_for<MO * MT>([&](auto ij) {
+      constexpr int x = decltype(ij)::value;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x / MT][x % MT][r] = 0.0f;
+    });
+    for (int s = 0; s < a.splits; ++s)
+      static_for<MO * MT>([&](auto ij) {
+        constexpr int x = decltype(ij)::value;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(parts, s * kPart + (4 * x + p) * 4096 + tid * 16, 0, kCoherent);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[x / MT][x % MT][4 * p + e] += __uint_as_float(v[e]);
+        }
+      });
+  }
+
+  // ---- store: 32 rows at a time through the wave's own part of the LDS, so that memory sees whole runs of a row
+  constexpr int kCols = 32 * MO;
+  constexpr bool kWide = std::is_same<OUT, F32>::value;
+  constexpr int kPitch = kWide ? kCols * 4 + 16 : kCols * 2 + 16;                // bytes of a row
+  static_assert(4 * 32 * kPitch <= kRing, "the strips of four waves fit the LDS");
+  char* const strip = lds + w * (32 * kPitch);
+  const int ow = o0 + wo * kCols;
+  static_for<MT>([&](auto jc) {
+    constexpr int j = decltype(jc)::value;
+    static_for<MO>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float v[4] = {acc[i][j][4 * p], acc[i][j][4 * p + 1], acc[i][j][4 * p + 2], acc[i][j][4 * p + 3]};
+        const int col = i * 32 + 8 * p + 4 * half;
+        if constexpr (kWide) *reinterpret_cast<float4*>(strip + (lane & 31) * kPitch + col * 4) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2*>(strip + (lane & 31) * kPitch + col * 2) = pack_out4(OUT{}, v);
+      }
+    });
+    wave_lds_order();
+    constexpr int kSize = kWide ? 4 : 2, kLanes = kCols * kSize / 16, kRowsPer = 64 / kLanes;
+#pragma unroll
+    for (int p = 0; p < 32 / kRowsPer; ++p) {
+      const int r = p * kRowsPer + lane / kLanes, c = lane % kLanes * (16 / kSize);
+      const int row = m0 + (wt * MT + j) * 32 + r;
+      const uint4 v = *reinterpret_cast<const uint4*>(strip + r * kPitch + c * kSize);
+      if (row < a.n_rows && ow + c < a.d_out)
+        *reinterpret_cast<uint4*>(static_cast<char*>(a.y) + (row * a.ld_y + ow + c) * kSize) = v;
+    }
+    wave_lds_order();
+  });
+}
+
+// ---- the product, few rows: HBM-bound, one pass over the weight --------------------------------------------
+// A workgroup of 8 waves owns 16 output channels: their codes are one contiguous run of 16 pitch bytes where the weight is dense.  The
+// waves share the blocks of 128 (block b goes to wave b % 8); a lane takes 32 codes of one channel and of one row of x, turns both into
+// bf16 with their scales (exact: four significant bits times a power of two) and multiplies them by v_mfma_f32_16x16x32_bf16, whose
+// sums are fp32 throughout: the matrix cores idle here anyway, and no bits are lost between neighbours.
+constexpr int kFewRows = 16;
+constexpr int kFewWaves = 8;
+
+__device__ __forceinline__ void bf16_of_codes(const u32x4& lo, const u32x4& hi, float unit, bfloat8 (&out)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t w0 = j < 2 ? lo[2 * j] : hi[2 * j - 4], w1 = j < 2 ? lo[2 * j + 1] : hi[2 * j - 3];
+    const bfloat2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, unit, true);
+    const bfloat2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, unit, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, unit, true);
+    out[j] = bfloat8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+}
+
+template <typename OUT>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void few_rows8_kernel(Product8Args a) {
+  __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16][16 + 4];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+  const int pitch = (a.d_in + 15) / 16 * 16, blocks = (a.d_in + 127) / 128, spitch = (blocks + 3) / 4 * 4;
+  const int o0 = blockIdx.x * 16, r = lane & 15, q = lane >> 4;
+  const int rows_o = min(16, a.d_out - o0);
+  const __amdgpu_buffer_rsrc_t buf_o = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(a.w.codes) + static_cast<size_t>(o0) * pitch, 0, rows_o * pitch, 0x00027000);
+  const __amdgpu_buffer_rsrc_t buf_t = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x.codes), 0, a.n_rows * pitch, 0x00027000);
+  const __amdgpu_buffer_rsrc_t buf_s = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x.scales), 0, a.n_rows * spitch, 0x00027000);
+  const uint8_t* const w_scales = a.w.scales + static_cast<size_t>(o0 / 128) * spitch;
+  const int base = r * pitch + 32 * q;
+  float4v acc = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kAtOnce = 4;
+  for (int b0 = w; b0 < blocks; b0 += kFewWaves * kAtOnce) {
+    u32x4 wc[kAtOnce][2], xc[kAtOnce][2];
+    uint32_t xs[kAtOnce], ws[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int b = b0 + u * kFewWaves, k = b * 128 + 32 * q;
+      // pieces behind the row's end are the next row's (or outside the buffer): they are asked for at an offset outside
+      const uint32_t at = static_cast<uint32_t>(base + b * 128);
+      const uint32_t at0 = k < pitch ? at : kOutside, at1 = k + 16 < pitch ? at + 16 : kOutside;
+      wc[u][0] = __builtin_amdgcn_raw_buffer_load_b128(buf_o, at0, 0, 2);
+      wc[u][1] = __builtin_amdgcn_raw_buffer_load_b128(buf_o, at1, 0, 2);
+      xc[u][0] = __builtin_amdgcn_raw_buffer_load_b128(buf_t, at0, 0, 0);
+      xc[u][1] = __builtin_amdgcn_raw_buffer_load_b128(buf_t, at1, 0, 0);
+      xs[u] = __builtin_amdgcn_raw_buffer_load_b8(buf_s, b < blocks ? static_cast<uint32_t>(r * spitch + b) : kOutside, 0, 0);
+      ws[u] = w_scales[min(b, blocks - 1)];
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      bfloat8 wv[4], xv[4];
+      bf16_of_codes(wc[u][0], wc[u][1], __uint_as_float(ws[u] << 23), wv);
+      bf16_of_codes(xc[u][0], xc[u][1], __uint_as_float(xs[u] << 23), xv);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[j], xv[j], acc, 0, 0, 0);
+    }
+  }
+  // lane (q, r): channels 4 q .. + 3 of row r
+  *reinterpret_cast<float4*>(&sums[w][r][4 * q]) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kFewWaves; ++k) {
+      const float4 s = *reinterpret_cast<const float4*>(&sums[k][r][4 * q]);
+      v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
+    }
+    const int o = o0 + 4 * q;
+    if (r < a.n_rows && o < a.d_out) {
+      if constexpr (std::is_same<OUT, F32>::value) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + r * a.ld_y + o) = make_float4(v[0], v[1], v[2], v[3]);
+      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + r * a.ld_y + o) = pack_out4(OUT{}, v);
+    }
+  }
+}
+
+template <typename OUT>
+hipError_t launch_out(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
+  if (p.kind == 0) {
+    few_rows8_kernel<OUT><<<dim3(p.tiles_o), 64 * kFewWaves, 0, s>>>(a);
+  } else {
+    const int jobs = p.tiles_m * p.tiles_o * p.splits, grid = (jobs + 7) / 8 * 8;
+    if (p.kind == 1) tile_product8_kernel<OUT, 4, 4><<<dim3(grid), 256, 0, s>>>(a);
+    else if (p.kind == 2) tile_product8_kernel<OUT, 2, 2><<<dim3(grid), 256, 0, s>>>(a);
+    else tile_product8_kernel<OUT, 2, 1><<<dim3(grid), 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s) {
+  const dim3 grid((d_out + 127) / 128, (d_in + 127) / 128);
+  if (bf16) quantize_w8_kernel<BF16><<<grid, 256, 0, s>>>(W, d_in, d_out, codes, scales);
+  else quantize_w8_kernel<F16><<<grid, 256, 0, s>>>(W, d_in, d_out, codes, scales);
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize_rows8(const uint16_t* x, long ld_x, int n_rows, int d, const uint16_t* norm_scale, float norm_eps,
+                                 uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s) {
+  constexpr int kAtMost = 1 << 19;               // rows of one launch: 32768 workgroups along a side, or as many of 512 lanes
+  const int pitch = pitch8(d), spitch = scale_pitch8(d);
+  for (int row = 0; row < n_rows; row += kAtMost) {
+    const int n = n_rows - row < kAtMost ? n_rows - row : kAtMost;
+    const uint16_t* const from = x + row * ld_x;
+    uint8_t* const to = codes + static_cast<size_t>(row) * pitch;
+    uint8_t* const to_s = scales + static_cast<size_t>(row) * spitch;
+    const dim3 grid((d + 511) / 512, (n + 15) / 16);
+    if (norm_eps >= 0.f) {
+      if (bf16) quantize_normed_rows8_kernel<BF16><<<n, 512, 0, s>>>(from, ld_x, n, d, norm_scale, norm_eps, to, to_s);
+      else quantize_normed_rows8_kernel<F16><<<n, 512, 0, s>>>(from, ld_x, n, d, norm_scale, norm_eps, to, to_s);
+    } else if (bf16) quantize_rows8_kernel<BF16><<<grid, 256, 0, s>>>(from, ld_x, n, d, to, to_s);
+    else quantize_rows8_kernel<F16><<<grid, 256, 0, s>>>(from, ld_x, n, d, to, to_s);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
+}
+
+Product8Plan plan_product8(int n_rows, int d_in, int d_out) {
+  Product8Plan p{};
+  const int blocks = (d_in + 127) / 128;
+  p.splits = 1;
+  p.blocks_per = blocks;
+  if (n_rows <= kFewRows) {
+    p.kind = 0;
+    p.tiles_m = 1;
+    p.tiles_o = (d_out + 15) / 16;
+    return p;
+  }
+  const long big = static_cast<long>((n_rows + 255) / 256) * ((d_out + 255) / 256);
+  p.kind = n_rows <= 64 ? 3 : big >= 192 ? 1 : 2;
+  const int to = p.kind == 1 ? 256 : 128, tt = p.kind == 1 ? 256 : p.kind == 2 ? 128 : 64;
+  p.tiles_m = (n_rows + tt - 1) / tt;
+  p.tiles_o = (d_out + to - 1) / to;
+  const long tiles = static_cast<long>(p.tiles_m) * p.tiles_o;
+  if (p.kind != 1 && tiles < 256) {
+    long want = 512 / tiles;
+    if (want > blocks / 4) want = blocks / 4;
+    if (want > 1) {
+      p.blocks_per = (blocks + static_cast<int>(want) - 1) / static_cast<int>(want);
+      p.splits = (blocks + p.blocks_per - 1) / p.blocks_per;
+    }
+  }
+  if (p.splits > 1) p.partial_floats = static_cast<size_t>(tiles) * p.splits * to * tt;
+  return p;
+}
+
+hipError_t launch_product8(const Product8Args& args, const Product8Plan& p, hipStream_t s) {
+  Product8Args a = args;
+  a.tiles_m = p.tiles_m;
+  a.tiles_o = p.tiles_o;
+  a.splits = p.splits;
+  a.blocks_per = p.blocks_per;
+  if (a.out == kOutF32) return launch_out<F32>(a, p, s);
+  return a.out == kOutBF16 ? launch_out<BF16>(a, p, s) : launch_out<F16>(a, p, s);
+}
+
+}  // namespace larosa

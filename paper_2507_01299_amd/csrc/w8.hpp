@@ -1,0 +1,72 @@
+// Host-side launch interface of the operators on 8-bit floating-point weights and of the log probabilities (internal to liblarosa).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace larosa {
+
+// Rows (activations, or a weight's output channels) in e4m3 codes with scales 2^(byte - 127) for 128 neighbours.
+struct Held8 {
+  const uint8_t* codes;       // [rows, pitch]: pitch = d up to 16, zeros behind d
+  const uint8_t* scales;      // rows: [rows, scale_pitch]; a weight: [rows / 128 up, scale_pitch]; scale_pitch = d / 128 up, up to 4
+};
+inline int pitch8(int d) { return (d + 15) / 16 * 16; }
+inline int scale_pitch8(int d) { return ((d + 127) / 128 + 3) / 4 * 4; }
+
+constexpr int kWidthMax8 = 1 << 20;    // channels summed over: a panel of 256 rows stays below 2^28 bytes
+constexpr int kOutMax8 = 1 << 24;      // rows of a weight
+constexpr int kRowsMax8 = 1 << 24;
+
+hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s);
+// norm_scale nullable; norm_eps < 0: no norm
+hipError_t launch_quantize_rows8(const uint16_t* x, long ld_x, int n_rows, int d, const uint16_t* norm_scale, float norm_eps,
+                                 uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s);
+
+// y[m, o] = sum_i x[m, i] w[o, i]
+enum : int { kOutF16 = 0, kOutBF16 = 1, kOutF32 = 2 };
+struct Product8Args {
+  Held8 x, w;
+  void* y;                    // [n_rows, ld_y]
+  long ld_y;
+  int n_rows, d_in, d_out;
+  int out;                    // kOutF16, ..
+  // split of the work, from plan_product8
+  int tiles_m, tiles_o;       // tiles of rows and of output channels
+  int splits, blocks_per;     // parts of a tile's sum, blocks of 128 of each
+  float* partial;             // [tiles][splits][tile]
+  unsigned* counters;         // [tiles], kCounterStride apart, zero on entry and on exit
+};
+struct Product8Plan {
+  int kind;                   // which kernel
+  int tiles_m, tiles_o, splits, blocks_per;
+  size_t partial_floats;
+};
+Product8Plan plan_product8(int n_rows, int d_in, int d_out);
+hipError_t launch_product8(const Product8Args& a, const Product8Plan& p, hipStream_t s);
+
+// Log probabilities of logits [n_rows, ld], the first n_vocab of a row.
+enum : int { kLogitsF16 = 0, kLogitsBF16 = 1, kLogitsF32 = 2 };
+constexpr int kTopMax = 64;
+struct LogprobsArgs {
+  const void* logits;
+  long ld;
+  int n_rows, n_vocab;
+  float scale;
+  const int32_t* given;       // [n_rows, n_given]
+  int n_given;
+  float* logp;                // [n_rows, n_given]
+  float* entropy;             // [n_rows] or nullptr
+  int n_top;
+  int32_t* top_id;            // [n_rows, n_top]
+  float* top_logp;            // [n_rows, n_top] or nullptr
+  int slices, slice_len;      // of a row
+  float* sums;                // [n_rows][slices][4]
+  unsigned long long* best;   // [n_rows][slices][256]: the largest of each lane's logits with its place
+  unsigned* counters;         // [n_rows] words, zero on entry and on exit
+};
+struct LogprobsPlan { int slices, slice_len; size_t sums_bytes, best_bytes; };
+LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type);
+hipError_t launch_logprobs(const LogprobsArgs& a, int type, hipStream_t s);
+
+}  // namespace larosa

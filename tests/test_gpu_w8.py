@@ -1,0 +1,269 @@
+"""GPU parity of the operators on 8-bit floating-point weights, through the C ABI: codes and scales bit for bit against the oracle, products
+exactly where every sum is exact and within a derived bound elsewhere."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import w8_oracle as Q
+
+pytestmark = pytest.mark.gpu
+TYPE = {"f16": torch.float16, "bf16": torch.bfloat16}
+STEP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}       # half a unit in the last place, relative
+
+
+@pytest.fixture(scope="module")
+def api(gpu_device):
+    from paper_2507_01299_amd import api as A
+    A.lib()
+    return A
+
+
+def exact(t):
+    return t.double().cpu().numpy()
+
+
+def same_held(got, want):
+    assert np.array_equal(got[0].view(torch.uint8).cpu().numpy(), want[0])
+    assert np.array_equal(got[1].cpu().numpy(), want[1])
+
+
+def special(v, dtype):
+    """Blocks that are zero, hold a NaN or an infinity, are tiny or huge, have a largest magnitude at a scale's border; ties; -0."""
+    n, d = v.shape
+    top = 60000.0 if dtype == "f16" else 3.3e38
+    for r in range(n):
+        at = (r % 9, r % max(1, min(d, 128)))
+        b = v[r, :min(d, 128)]
+        if at[0] == 0:
+            b[:] = 0
+        elif at[0] == 1:
+            b[at[1]] = float("nan")
+        elif at[0] == 2:
+            b[at[1]] = float("-inf")
+        elif at[0] == 3:
+            b *= 2.0 ** -20 if dtype == "f16" else 1e-30
+        elif at[0] == 4:
+            b[at[1]] = -top
+        elif at[0] == 5:
+            b.clamp_(-1.0, 1.0)
+            b[at[1]] = 1.75                     # 448 * 2^-8
+        elif at[0] == 6:
+            b.clamp_(-1.0, 1.0)
+            b[at[1]] = 1.7578125                # the next code's side of it
+            b[0] = 1.0625                       # a tie
+        elif at[0] == 7:
+            b[0] = -0.0
+    return v
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,d", [(1, 8), (3, 16), (9, 120), (16, 128), (17, 136), (5, 504), (33, 512), (18, 520), (2, 4104), (40, 1032)])
+def test_rows_bit_for_bit(api, dtype, n, d):
+    print(f"quantize_rows8 {dtype} {n}x{d}", flush=True)
+    g = torch.Generator().manual_seed(n * 1000 + d)
+    x = special(torch.randn(n, d, generator=g) * torch.rand(1, d, generator=g) * 3, dtype).to(TYPE[dtype])
+    same_held(api.quantize_rows8(x.cuda(), dtype), Q.quantize_rows(exact(x)))
+
+
+def test_rows_of_a_wider_matrix(api):
+    x = torch.randn(21, 1000, generator=torch.Generator().manual_seed(5)).bfloat16()
+    part = x.cuda()[3:20, 200:336]
+    same_held(api.quantize_rows8(part, "bf16"), Q.quantize_rows(exact(x[3:20, 200:336])))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,d,scaled", [(1, 8, True), (2, 136, False), (5, 4096, True), (3, 4104, True), (2, 16392, False)])
+def test_rows_behind_a_norm(api, dtype, n, d, scaled):
+    """fp32 norms differ from 64-bit ones by (d / 8 lanes' partial sums, then 9 levels, a root and a quotient) under 64 * 2^-24 = 4e-6 of a
+    value; the code is nearest to that value, so it is off the 64-bit value by at most half a code step and 4e-6."""
+    print(f"normed rows {dtype} {n}x{d}", flush=True)
+    g = torch.Generator().manual_seed(d)
+    x = (torch.randn(n, d, generator=g) * 3).to(TYPE[dtype])
+    rms = (1 + 0.3 * torch.randn(d, generator=g)).to(TYPE[dtype]) if scaled else None
+    codes, scales = api.quantize_rows8(x.cuda(), dtype, rms=None if rms is None else rms.cuda(), rms_eps=1e-5)
+    v = Q.normed(exact(x), None if rms is None else exact(rms), 1e-5)
+    codes, scales = codes.view(torch.uint8).cpu().numpy(), scales.cpu().numpy()
+    unit = np.repeat(2.0 ** (scales.astype(float) - 127), 128, 1)[:, :d]
+    assert np.all(np.abs(v) <= 448 * unit * (1 + 4e-6))
+    blocks = np.pad(np.abs(v), ((0, 0), (0, -d % 128))).reshape(n, -1, 128).max(-1)
+    own = 2.0 ** (scales[:, :blocks.shape[1]].astype(float) - 127)
+    assert np.all(blocks >= 224 * own * (1 - 4e-6))                                     # (the least scale)
+    half = np.maximum(np.abs(v) * 2.0 ** -4, 2.0 ** -10 * unit)
+    assert np.all(np.abs(Q.values(codes, scales, 1, d) - v) <= half + 4e-6 * np.abs(v))
+    assert np.all(codes[:, d:] == 0) and np.all(scales[:, -(-d // 128):] == 127)
+
+
+def test_a_norm_of_a_row_with_a_nan_is_nan(api):
+    x = torch.randn(3, 256).half()
+    x[1, 7] = float("nan")
+    codes, scales = api.quantize_rows8(x.cuda(), "f16", rms_eps=1e-5)
+    v = Q.values(codes.view(torch.uint8).cpu().numpy(), scales.cpu().numpy(), 1, 256)
+    assert np.all(np.isnan(v[1])) and np.all(np.isfinite(v[[0, 2]]))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d_in,d_out", [(8, 8), (128, 128), (136, 264), (120, 1032), (1000, 392), (24, 16), (520, 136), (4104, 128)])
+def test_weight_bit_for_bit(api, dtype, d_in, d_out):
+    print(f"quantize_w8 {dtype} {d_in}x{d_out}", flush=True)
+    g = torch.Generator().manual_seed(d_in + d_out)
+    W = (torch.randn(d_in, d_out, generator=g) * 0.02)
+    W[:128, :128] = 0
+    if d_out > 256:
+        W[5, 200] = float("inf")
+        W[:, 256:] *= 1e-4
+    W = W.to(TYPE[dtype])
+    same_held(api.quantize_w8(W.cuda(), dtype), Q.quantize_weight(exact(W)))
+
+
+# ---- products ------------------------------------------------------------------------------------------------
+
+# The 8-bit instruction aligns the products of eight neighbours to the largest sum of two exponents and cuts them, towards zero, 13 bits below it (256 * 256
+# beside 30 gives 65536 + 24, beside 7 nothing): each but the largest is off by less than 2^-13 of the largest, so the sum by less than
+# 7 * 2^-13 < 2^-10 of the sum of magnitudes.
+CUT = 2.0 ** -10
+SHAPES = [
+    (1, 8, 8), (1, 128, 16), (2, 136, 24), (5, 4104, 136), (15, 512, 264), (16, 1032, 520), (16, 24, 1000),          # few rows
+    (17, 8, 8), (17, 136, 24), (33, 1032, 264), (64, 4104, 136), (64, 512, 1160),                                    # tiles of 64 rows
+    (65, 16, 8), (65, 520, 264), (100, 4104, 392), (129, 128, 136), (257, 1000, 520), (300, 2056, 1032),             # of 128
+    (1100, 136, 9992), (3001, 648, 4104),                                                                            # of 256
+]
+
+
+def test_the_shapes_take_every_kernel():
+    """By the launch rules: up to 16 rows, up to 64, and from 192 tiles of 256 x 256 on."""
+    kinds = {0 if n <= 16 else 3 if n <= 64 else 1 if -(-n // 256) * -(-o // 256) >= 192 else 2 for n, _, o in SHAPES}
+    assert kinds == {0, 1, 2, 3}
+
+
+def held(api, x, W, dtype):
+    return api.quantize_w8(W.to(TYPE[dtype]).cuda(), dtype), api.quantize_rows8(x.to(TYPE[dtype]).cuda(), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,d_in,d_out", SHAPES)
+def test_product_of_small_integers_is_exact(api, dtype, n, d_in, d_out):
+    """Integers up to 2: codes hold them, products and sums (at most 4 d_in < 2^24) are whole numbers, so only the last rounding is left.  Blocks
+    are scaled by powers of two, differently for every row and every block of the weight.  Rows and columns behind y's are left as they were."""
+    print(f"exact product {dtype} {n}x{d_in}x{d_out}", flush=True)
+    g = torch.Generator().manual_seed(n + d_in + d_out)
+    x = torch.randint(-2, 3, (n, d_in), generator=g).float() * 2.0 ** torch.randint(-2, 3, (n, 1), generator=g)
+    W = torch.randint(-2, 3, (d_in, d_out), generator=g).float()
+    for o in range(0, d_out, 128):
+        W[:, o:o + 128] *= 2.0 ** ((o // 128) % 5 - 2)
+    (wc, ws), (xc, xs) = held(api, x, W, dtype)
+    wide = torch.full((n + 3, d_out + 24), -77.0, dtype=TYPE[dtype], device="cuda")
+    y = wide[:n, 8:8 + d_out]
+    work = api.product8_workspace(n, d_in, d_out)
+    api.product8(wc, ws, xc, xs, d_in, y, dtype, work)
+    want = (x.double() @ W.double()).to(TYPE[dtype])
+    assert torch.equal(y.cpu(), want)
+    assert torch.all(wide[n:] == -77) and torch.all(wide[:, :8] == -77) and torch.all(wide[:, 8 + d_out:] == -77)
+    assert int(work.buf[work.ptr - work.buf.data_ptr():][:1 << 20].count_nonzero()) == 0
+    again = torch.empty(n, d_out, dtype=TYPE[dtype], device="cuda")
+    api.dense_w8(wc, ws, x.to(TYPE[dtype]).cuda(), again, dtype, api.dense_w8_workspace(n, d_in, d_out))
+    assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,d_in,d_out", SHAPES)
+def test_product_within_its_bound(api, dtype, n, d_in, d_out):
+    """Up to 16 rows sums are fp32: at most (d_in + 8) roundings of 2^-24 of the sum of magnitudes.  Above, see CUT.  Then half a step of the type.
+    In the norm: seven cuts in eight products, each below 2^-13 of the largest, whose square is at most the sum of the eight squares, of
+    random sign and uniform size: sqrt(7 / 3) 2^-13 < 2^-12 of the products' root sum of squares, which is the result's norm."""
+    print(f"product {dtype} {n}x{d_in}x{d_out}", flush=True)
+    g = torch.Generator().manual_seed(n * 7 + d_in + d_out)
+    strong = torch.where(torch.rand(1, d_in, generator=g) < 0.02, 20.0, 1.0)
+    x, W = torch.randn(n, d_in, generator=g) * strong, torch.randn(d_in, d_out, generator=g) * 0.05
+    (wc, ws), (xc, xs) = held(api, x, W, dtype)
+    y = torch.empty(n, d_out, dtype=TYPE[dtype], device="cuda")
+    api.product8(wc, ws, xc, xs, d_in, y, dtype, api.product8_workspace(n, d_in, d_out))
+    want, most = Q.product(wc.view(torch.uint8).cpu().numpy(), ws.cpu().numpy(), xc.view(torch.uint8).cpu().numpy(), xs.cpu().numpy(), d_in)
+    off = np.abs(exact(y) - want)
+    sums = (d_in + 8) * 2.0 ** -24 + (0 if n <= 16 else CUT)
+    least = 2.0 ** -25 if dtype == "f16" else 0.0            # half of f16's smallest step
+    assert np.all(off <= sums * most + STEP[dtype] * (np.abs(want) + sums * most) + least)
+    assert np.linalg.norm(off) <= (STEP[dtype] + 2.0 ** -12) * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("n", [3, 40, 200, 2100])
+def test_nan_reaches_its_row_and_its_channels_only(api, n):
+    d_in, d_out = 400, 6200
+    x, W = torch.randn(n, d_in), torch.randn(d_in, d_out)
+    x[n - 1, 390] = float("nan")
+    x[0, 3] = float("inf")
+    W[399, 300] = float("nan")
+    (wc, ws), (xc, xs) = held(api, x, W, "bf16")
+    y = torch.empty(n, d_out, dtype=torch.bfloat16, device="cuda")
+    api.product8(wc, ws, xc, xs, d_in, y, "bf16", api.product8_workspace(n, d_in, d_out))
+    want = torch.zeros(n, d_out, dtype=torch.bool)
+    want[[0, n - 1]] = True
+    want[:, 256:384] = True
+    assert torch.equal(y.isnan().cpu(), want)
+
+
+@pytest.mark.parametrize("n", [4, 50, 130, 2100])
+def test_codes_of_others_with_extreme_scales(api, n):
+    """Codes and scale bytes that a caller brings: every code, scales from 2^-63 to 2^63; results that stay in fp32."""
+    d_in, d_out = 256, 6200
+    g = torch.Generator().manual_seed(n)
+    wc = torch.randint(0, 127, (d_out, d_in), generator=g, dtype=torch.uint8) + 128 * torch.randint(0, 2, (d_out, d_in), generator=g, dtype=torch.uint8)
+    xc = torch.randint(0, 127, (n, d_in), generator=g, dtype=torch.uint8) + 128 * torch.randint(0, 2, (n, d_in), generator=g, dtype=torch.uint8)
+    e = torch.randint(-63, 64, (-(-d_out // 128), 1), generator=g)
+    ws, xs = (e + 127).expand(-1, 4).to(torch.uint8).contiguous(), torch.full((n, 4), 127, dtype=torch.uint8)
+    xs[:, 1] = 125
+    y = torch.empty(n, d_out, dtype=torch.bfloat16, device="cuda")
+    api.product8(wc.cuda(), ws.cuda(), xc.cuda(), xs.cuda(), d_in, y, "bf16", api.product8_workspace(n, d_in, d_out))
+    want, most = Q.product(wc.numpy(), ws.numpy(), xc.numpy(), xs.numpy(), d_in)
+    sums = (d_in + 8) * 2.0 ** -24 + (0 if n <= 16 else CUT)
+    assert np.all(np.abs(exact(y) - want) <= sums * most + STEP["bf16"] * (np.abs(want) + sums * most))
+
+
+def test_dense_behind_a_norm_is_its_parts(api):
+    for n in (2, 300):
+        x, rms = torch.randn(n, 520).half().cuda(), (1 + 0.1 * torch.randn(520)).half().cuda()
+        wc, ws = api.quantize_w8(torch.randn(520, 264).half().cuda(), "f16")
+        y, z = (torch.empty(n, 264, dtype=torch.float16, device="cuda") for _ in range(2))
+        api.dense_w8(wc, ws, x, y, "f16", api.dense_w8_workspace(n, 520, 264), rms=rms, rms_eps=1e-5)
+        xc, xs = api.quantize_rows8(x, "f16", rms=rms, rms_eps=1e-5)
+        api.product8(wc, ws, xc, xs, 520, z, "f16", api.product8_workspace(n, 520, 264))
+        assert torch.equal(y, z)
+
+
+def test_same_bits_every_time_and_on_another_stream(api):
+    """Parts of a sum are added in their order whatever workgroup comes last."""
+    n, d_in, d_out = 70, 8192, 520
+    x, W = torch.randn(n, d_in).half().cuda(), torch.randn(d_in, d_out).half().cuda()
+    wc, ws = api.quantize_w8(W, "f16")
+    work = api.dense_w8_workspace(n, d_in, d_out)
+    first = api.dense_w8(wc, ws, x, torch.empty(n, d_out, dtype=torch.float16, device="cuda"), "f16", work).clone()
+    for _ in range(5):
+        assert torch.equal(first, api.dense_w8(wc, ws, x, torch.empty_like(first), "f16", work))
+    other, busy = torch.cuda.Stream(), api.dense_w8_workspace(n, d_in, d_out)
+    torch.cuda.synchronize()
+    ys = [torch.empty_like(first) for _ in range(6)]
+    for i in range(0, 6, 2):
+        api.dense_w8(wc, ws, x, ys[i], "f16", work)
+        with torch.cuda.stream(other):
+            api.dense_w8(wc, ws, x, ys[i + 1], "f16", busy)
+    torch.cuda.synchronize()
+    assert all(torch.equal(first, y) for y in ys)
+
+
+@pytest.mark.parametrize("n", [1, 40, 150])
+def test_captured_and_replayed(api, n):
+    d_in, d_out = 2056, 264
+    wc, ws = api.quantize_w8(torch.randn(d_in, d_out).bfloat16().cuda(), "bf16")
+    x, y = torch.randn(n, d_in).bfloat16().cuda(), torch.empty(n, d_out, dtype=torch.bfloat16, device="cuda")
+    work, eager_work = api.dense_w8_workspace(n, d_in, d_out), api.dense_w8_workspace(n, d_in, d_out)
+    api.dense_w8(wc, ws, x, y, "bf16", work, rms_eps=1e-5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.dense_w8(wc, ws, x, y, "bf16", work, rms_eps=1e-5)
+    for i in range(4):
+        x.copy_(torch.randn(n, d_in).bfloat16() * (i + 1))
+        y.zero_()
+        graph.replay()
+        want = api.dense_w8(wc, ws, x, torch.empty_like(y), "bf16", eager_work, rms_eps=1e-5)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
