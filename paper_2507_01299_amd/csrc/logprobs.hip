@@ -7,10 +7,10 @@
 // never rescaled on the way.  Several slices of a row meet through memory: the workgroup that arrives last at the row joins them.
 //  * One logit of the largest value is left out of S and counted: ln S = log1p(the others), which keeps its bits where one token
 //    holds nearly all of the probability.
-//  * The most probable tokens.  Each lane keeps the largest of its logits and where it first stood (its lane's `best`).  The n tokens
-//    sought lie among the logits of the n lanes with the largest `best` (ties: the earlier place): any other lane's logits are beaten by
-//    n of those.  So only these lanes' logits are read again, and the pass over the row does nothing but take maxima, whatever
-//    the order of the logits.  One wave selects, in registers, 64 candidates at a time.
+//  * The most probable tokens.  128 logits (the 16 groups of one lane, or of 2, 4, .. lanes with fewer) are a holder, which keeps the largest
+//    of them and where it first stood.  The n tokens sought lie among the logits of the n holders with the largest (ties: the earlier
+//    place): any other holder's logits are beaten by n of those.  So only these are read again, and the pass over the row does
+//    nothing but take maxima, whatever the order of the logits.  One wave selects, in registers, 64 candidates at a time.
 // Exponentials are the hardware's exp2 of (logit - M) times scale / ln 2: the difference first, so that a row of nothing but the type's
 // lowest value, a common mask, is a row like any other.
 #include "kernels.hpp"
@@ -89,9 +89,29 @@ __device__ __forceinline__ u64 candidate(float v, int place) {
 }
 __device__ __forceinline__ int place_of(u64 c) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(c)); }
 
-__device__ __forceinline__ u64 shuffle_xor(u64 v, int mask) {
-  const int lo = __shfl_xor(static_cast<int>(static_cast<uint32_t>(v)), mask), hi = __shfl_xor(static_cast<int>(v >> 32), mask);
-  return (static_cast<u64>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo);
+// The value of lane ^ D, without an LDS round trip: quads and rows of 16 lanes by DPP, wider by the lane swaps.
+template <int D>
+__device__ __forceinline__ uint32_t exchanged(uint32_t v) {
+  static_assert(D == 1 || D == 2 || D == 4 || D == 8 || D == 16 || D == 32, "a power of two");
+  const int i = static_cast<int>(v);
+  if constexpr (D == 1) return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(i, i, 0xB1, 0xF, 0xF, false));        // quad_perm 1 0 3 2
+  else if constexpr (D == 2) return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(i, i, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
+  else if constexpr (D == 4) {                 // four lanes up for the even quads, down for the odd ones
+    const int up = __builtin_amdgcn_update_dpp(i, i, 0x104, 0xF, 0x5, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(up, i, 0x114, 0xF, 0xA, false));
+  } else if constexpr (D == 8) return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(i, i, 0x128, 0xF, 0xF, false));  // row_ror 8
+  else {
+    const auto x = D == 16 ? __builtin_amdgcn_permlane16_swap(v, v, false, false) : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (threadIdx.x & D) ? x[0] : x[1];    // x[0]: the lower half's values in both halves, x[1]: the upper's
+  }
+}
+template <int D>
+__device__ __forceinline__ u64 exchanged64(u64 v) {
+  const uint32_t lo = exchanged<D>(static_cast<uint32_t>(v)), hi = exchanged<D>(static_cast<uint32_t>(v >> 32));
+  return (static_cast<u64>(hi) << 32) | lo;
+}
+__device__ __forceinline__ u64 reversed(u64 v) {       // lane 63 - l
+  return exchanged64<1>(exchanged64<2>(exchanged64<4>(exchanged64<8>(exchanged64<16>(exchanged64<32>(v))))));
 }
 __device__ __forceinline__ u64 shuffle_from(u64 v, int lane) {
   const int lo = __shfl(static_cast<int>(static_cast<uint32_t>(v)), lane), hi = __shfl(static_cast<int>(v >> 32), lane);
@@ -101,20 +121,26 @@ __device__ __forceinline__ u64 lane_value(u64 v, int lane) {          // lane: u
   const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), lane), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), lane);
   return (static_cast<u64>(hi) << 32) | lo;
 }
-// the wave's 64 values, largest first
-template <int FROM>
-__device__ __forceinline__ u64 bitonic(u64 v, int lane) {
-#pragma unroll
-  for (int k = FROM; k <= 64; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2) {
-      const u64 other = shuffle_xor(v, j);
-      const bool larger = ((lane & j) == 0) == ((lane & k) == 0);
-      v = (v > other) == larger ? v : other;
-    }
-  return v;
+// One step of a bitonic network: blocks of K lanes fall and rise in turn; J: distance
+template <int K, int J>
+__device__ __forceinline__ u64 bitonic_step(u64 v, int lane) {
+  const u64 other = exchanged64<J>(v);
+  const bool larger = ((lane & J) == 0) == ((lane & K) == 0);
+  return (v > other) == larger ? v : other;
 }
-__device__ __forceinline__ u64 sorted(u64 v, int lane) { return bitonic<2>(v, lane); }
+template <int K, int J>
+__device__ __forceinline__ u64 bitonic_merge(u64 v, int lane) {
+  v = bitonic_step<K, J>(v, lane);
+  if constexpr (J > 1) return bitonic_merge<K, J / 2>(v, lane);
+  else return v;
+}
+// the wave's 64 values, largest first
+template <int K = 2>
+__device__ __forceinline__ u64 sorted(u64 v, int lane) {
+  v = bitonic_merge<K, K / 2>(v, lane);
+  if constexpr (K < 64) return sorted<2 * K>(v, lane);
+  else return v;
+}
 
 // The largest 64 of all values offered, in a wave's lanes.
 struct Largest {
@@ -128,8 +154,12 @@ struct Largest {
   }
   __device__ __forceinline__ void merge(u64 v) {
     v = sorted(v, lane);
-    const u64 back = shuffle_xor(v, 63);
-    best = bitonic<64>(best > back ? best : back, lane);
+    if (lane_value(best, 0) == 0) {
+      best = v;
+      return;
+    }
+    const u64 back = reversed(v);              // beside best: the larger of each pair are the 64 largest of both, falling and rising
+    best = bitonic_merge<64, 32>(best > back ? best : back, lane);
   }
   __device__ __forceinline__ void offer(u64 v) {       // 0: nothing
     const bool in = v >= least && v != 0;
@@ -162,14 +192,30 @@ struct Largest {
 struct Sums { float most, left_out, others, moment; };   // largest logit, how many of it are left out, sum of the other exponentials, sum of exponential times exponent
 
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  v = fmaxf(v, __uint_as_float(exchanged<32>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(exchanged<16>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(exchanged<8>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(exchanged<4>(__float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(exchanged<2>(__float_as_uint(v))));
+  return fmaxf(v, __uint_as_float(exchanged<1>(__float_as_uint(v))));
+}
+
+// Holders of W lanes: the largest of each, in all its lanes.
+template <int W>
+__device__ __forceinline__ u64 holders_largest(u64 v) {
+  if constexpr (W > 1) {
+    const u64 other = exchanged64<W / 2>(v);
+    return holders_largest<W / 2>(v > other ? v : other);
+  } else {
+    return v;
+  }
 }
 
 template <typename L, int G>
-__global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
-  __shared__ u64 bests[kLanes];
+__global__ __launch_bounds__(kLanes, 4) void logprobs_kernel(LogprobsArgs a) {
+  constexpr int W = 16 / G;                    // lanes of a holder: 16 groups
+  constexpr int kHolders = kLanes / W;         // of a slice
+  __shared__ __attribute__((aligned(16))) u64 bests[kHolders];
   __shared__ u64 buf[128];
   __shared__ float red[4][4];
   __shared__ int last_flag;
@@ -207,15 +253,21 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
     if (lane == 0) red[wave][0] = m;
   }
   if (a.n_top > 0) {
-    const u64 mine = first + tid < stop ? candidate(most, where * 8) : 0;
-    if (a.slices > 1) __hip_atomic_store(a.best + (row_no * a.slices + slice) * kLanes + tid, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    else bests[tid] = mine;
+    const u64 mine = holders_largest<W>(first + tid < stop ? candidate(most, where * 8) : 0);
+    if (tid % W == 0) {
+      if (a.slices > 1) __hip_atomic_store(a.best + (row_no * a.slices + slice) * kHolders + tid / W, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      else bests[tid / W] = mine;
+    }
   }
   __syncthreads();
   const float top = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
   __syncthreads();
 
-  // ---- the exponentials
+  // ---- the exponentials.  The logits wait as they came: without this the compiler would keep them unpacked, in twice the registers.
+#pragma unroll
+  for (int i = 0; i < G; ++i)
+#pragma unroll
+    for (int h = 0; h < 8 / L::kPer; ++h) asm volatile("" : "+v"(raw[i][h].x), "+v"(raw[i][h].y), "+v"(raw[i][h].z), "+v"(raw[i][h].w));
   const float c = a.scale * kLog2E;
   const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f, moment = 0.f;
@@ -337,28 +389,47 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
     return;
   }
   const int n = a.n_top;
-  const long count = static_cast<long>(a.slices) * kLanes;
-  auto best_of = [&](long i) __attribute__((always_inline)) {
-    return a.slices > 1 ? __hip_atomic_load(a.best + row_no * count + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : bests[i];
+  // candidates come 16 to a lane (eight 16-byte loads, coherent across the chip); up to 1024 are read once
+  const int count = a.slices * kHolders;
+  constexpr int kAtOnce = 16;
+  u64 held_by[kAtOnce];
+  auto load_holders = [&](int i0) __attribute__((always_inline)) {
+    if (a.slices > 1) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(a.best + row_no * count, 0, count * 8, 0x00027000);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; i += 2) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(all, (i0 + i * 64 + lane * 2) * 8, 0, 16);
+        held_by[i] = (static_cast<u64>(v.y) << 32) | v.x;
+        held_by[i + 1] = (static_cast<u64>(v.w) << 32) | v.z;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) held_by[i] = i0 + i * 64 + lane < kHolders ? bests[i0 + i * 64 + lane] : 0;
+    }
   };
   u64 mine = 0;
-  for (long i = lane; i < count; i += 64) {
-    const u64 b = best_of(i);
-    if (b > mine) mine = b;
+  for (int i0 = 0; i0 < count; i0 += 64 * kAtOnce) {
+    load_holders(i0);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) mine = held_by[i] > mine ? held_by[i] : mine;
   }
   Largest holders(buf, lane, n, lane_value(sorted(mine, lane), n - 1));
-  for (long i = lane; i < count; i += 64) holders.offer(best_of(i));
+  for (int i0 = 0; i0 < count; i0 += 64 * kAtOnce) {
+    if (count > 64 * kAtOnce) load_holders(i0);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) holders.offer(held_by[i]);
+  }
   holders.done();
   const u64 nth = lane_value(holders.best, n - 1);
   Largest tokens(buf, lane, n, nth ? nth - 7 : 0);     // (its place is its group's first: the logit lies at most 7 further)
-  constexpr int kPart = 16;                    // lanes that share a holder's groups
-  for (int h0 = 0; h0 < n; h0 += 64 / kPart) {
-    const int h = h0 + lane / kPart;
+  for (int h0 = 0; h0 < n; h0 += 4) {          // 16 lanes to a holder, a group each
+    const int h = h0 + lane / 16;
     const u64 holder = shuffle_from(holders.best, h & 63);
-    const int group0 = place_of(holder) / 8;   // one of the lane's groups: the others are multiples of kLanes away in its slice
+    const int group0 = place_of(holder) / 8;   // one of the holder's groups: its lane and its slice
     const int from_slice = group0 / per, in_slice = group0 - from_slice * per;
-    const int group = from_slice * per + in_slice % kLanes + (lane % kPart) * kLanes;
-    const bool valid = h < n && holder != 0 && (lane % kPart) < G && group < min((from_slice + 1) * per, (row.end + 7) / 8);
+    const int group = from_slice * per + in_slice % kLanes / W * W + lane % 16 % W + lane % 16 / W * kLanes;
+    const bool valid = h < n && holder != 0 && group < min((from_slice + 1) * per, (row.end + 7) / 8);
     float v[8];
     uint4 again[8 / L::kPer];
     if (valid) {
@@ -385,8 +456,8 @@ hipError_t launch_type(const LogprobsArgs& a, hipStream_t s) {
   if (groups <= 1) logprobs_kernel<L, 1><<<grid, kLanes, 0, s>>>(a);
   else if (groups <= 2) logprobs_kernel<L, 2><<<grid, kLanes, 0, s>>>(a);
   else if (groups <= 4) logprobs_kernel<L, 4><<<grid, kLanes, 0, s>>>(a);
-  else if (groups <= 8) logprobs_kernel<L, 8><<<grid, kLanes, 0, s>>>(a);
-  else logprobs_kernel<L, 16><<<grid, kLanes, 0, s>>>(a);
+  else if (L::kBytes == 4 || groups <= 8) logprobs_kernel<L, 8><<<grid, kLanes, 0, s>>>(a);
+  else if constexpr (L::kBytes == 2) logprobs_kernel<L, 16><<<grid, kLanes, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -405,7 +476,9 @@ LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type) {
   p.slices = static_cast<int>((places + p.slice_len - 1) / p.slice_len);
   if (p.slices > 1) {
     p.sums_bytes = static_cast<size_t>(p.slices) * 4 * sizeof(float);
-    p.best_bytes = n_top > 0 ? static_cast<size_t>(p.slices) * kLanes * sizeof(u64) : 0;
+    const int groups = (p.slice_len / kGroup + kLanes - 1) / kLanes;
+    const int holders = groups <= 1 ? 16 : groups <= 2 ? 32 : groups <= 4 ? 64 : groups <= 8 ? 128 : 256;    // of a slice
+    p.best_bytes = n_top > 0 ? static_cast<size_t>(p.slices) * holders * sizeof(u64) : 0;
   }
   return p;
 }

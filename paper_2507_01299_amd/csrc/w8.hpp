@@ -62,7 +62,7 @@ struct LogprobsArgs {
   float* top_logp;            // [n_rows, n_top] or nullptr
   int slices, slice_len;      // of a row
   float* sums;                // [n_rows][slices][4]
-  unsigned long long* best;   // [n_rows][slices][256]: the largest of each lane's logits with its place
+  unsigned long long* best;   // [n_rows][slices][holders]: the largest of 128 logits with its place
   unsigned* counters;         // [n_rows] words, zero on entry and on exit
 };
 struct LogprobsPlan { int slices, slice_len; size_t sums_bytes, best_bytes; };
