@@ -2,9 +2,8 @@
 //
 //   z = scale * logit,  M = max z,  S = sum exp(z - M):   log p(i) = z_i - M - ln S,   H = ln S - sum exp(z - M) (z - M) / S
 //
-// HBM-bound: every logit is read once.  A workgroup of 256 lanes takes a slice of a row, at most 16 groups of 8 logits a lane, which
-// wait in registers while the slice's maximum is found: the exponentials are taken once, against the slice's own maximum, and sums are
-// never rescaled on the way.  Several slices of a row meet through memory: the workgroup that arrives last at the row joins them.
+// HBM-bound: every logit is read once.  A workgroup of four waves takes a row, or a slice of it where rows are few; a wave goes through it
+// by itself, chunk after chunk, against the largest logit it has seen.  Slices meet through memory: the workgroup that arrives last joins them.
 //  * One logit of the largest value is left out of S and counted: ln S = log1p(the others), which keeps its bits where one token
 //    holds nearly all of the probability.
 //  * The most probable tokens.  128 logits (the 16 groups of one lane, or of 2, 4, .. lanes with fewer) are a holder, which keeps the largest
@@ -25,12 +24,26 @@ typedef unsigned long long u64;
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kLanes = 256;
 constexpr int kGroup = 8;                      // logits of a group
+constexpr int kHoldersMax = 2048;              // of a slice: one of 262144 logits
+constexpr int kSmallSlice = 4096;              // up to here a wave's chunks are of one group a lane, so that all four have some
+constexpr int kLeastSlice = 2048;              // few rows: no shorter slices
+constexpr int kWorkgroups = 1024;              // and no more of them than this many in all
 
-struct Logits16 { using Raw = uint4; static constexpr int kPer = 8, kBytes = 2; };
-struct LF16 : Logits16 { static __device__ __forceinline__ void unpack(const uint4 (&r)[1], float (&v)[8]) { unpack8<F16>(r[0], v); } };
-struct LBF16 : Logits16 { static __device__ __forceinline__ void unpack(const uint4 (&r)[1], float (&v)[8]) { unpack8<BF16>(r[0], v); } };
+__device__ __forceinline__ uint32_t& word_of(uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+struct Logits16 {
+  static constexpr int kPer = 8, kBytes = 2;   // logits of 16 bytes, bytes of one
+};
+struct LF16 : Logits16 {
+  static constexpr uint32_t kNothing = 0xFC00FC00u;    // -infinity
+  static __device__ __forceinline__ void unpack(const uint4 (&r)[1], float (&v)[8]) { unpack8<F16>(r[0], v); }
+};
+struct LBF16 : Logits16 {
+  static constexpr uint32_t kNothing = 0xFF80FF80u;
+  static __device__ __forceinline__ void unpack(const uint4 (&r)[1], float (&v)[8]) { unpack8<BF16>(r[0], v); }
+};
 struct LF32 {
-  static constexpr int kPer = 4, kBytes = 4;   // logits of 16 bytes
+  static constexpr int kPer = 4, kBytes = 4;
+  static constexpr uint32_t kNothing = 0xFF800000u;
   static __device__ __forceinline__ void unpack(const uint4 (&r)[2], float (&v)[8]) {
     v[0] = __uint_as_float(r[0].x); v[1] = __uint_as_float(r[0].y); v[2] = __uint_as_float(r[0].z); v[3] = __uint_as_float(r[0].w);
     v[4] = __uint_as_float(r[1].x); v[5] = __uint_as_float(r[1].y); v[6] = __uint_as_float(r[1].z); v[7] = __uint_as_float(r[1].w);
@@ -50,22 +63,29 @@ struct Row {
     head = off / L::kBytes;
     end = head + n_vocab;
   }
-  __device__ __forceinline__ void load(int group, uint4 (&raw)[8 / L::kPer], bool stream) const {
+  // A piece behind the last that holds a logit is read as that one: no lane takes a branch around its loads (trim sees to the rest).
+  template <bool STREAM>
+  __device__ __forceinline__ void load(int group, uint4 (&raw)[8 / L::kPer]) const {
 #pragma unroll
     for (int h = 0; h < 8 / L::kPer; ++h) {
       typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-      const u32x4* p = reinterpret_cast<const u32x4*>(base + (static_cast<long>(group) * 8 + h * L::kPer) * L::kBytes);
-      const u32x4 v = group * 8 + h * L::kPer < end ? (stream ? __builtin_nontemporal_load(p) : *p) : u32x4{0u, 0u, 0u, 0u};
+      const int piece = min(group * (8 / L::kPer) + h, (end - 1) / L::kPer);
+      const u32x4* const p = reinterpret_cast<const u32x4*>(base) + piece;
+      const u32x4 v = STREAM ? __builtin_nontemporal_load(p) : *p;
       raw[h] = make_uint4(v.x, v.y, v.z, v.w);
     }
   }
-  __device__ __forceinline__ void values(int group, const uint4 (&raw)[8 / L::kPer], float (&v)[8]) const {
-    L::unpack(raw, v);
-    const int first = group * 8;
-    if (first < head || first + 8 > end) {     // (the row's two ends)
+  // logit e of a group becomes -infinity where `out`
+  static __device__ __forceinline__ void remove(uint4 (&raw)[8 / L::kPer], int e, bool out) {
+    uint32_t& w = word_of(raw[L::kBytes == 4 ? e / 4 : 0], L::kBytes == 4 ? e % 4 : e / 2);
+    const uint32_t part = L::kBytes == 4 ? 0xFFFFFFFFu : e % 2 ? 0xFFFF0000u : 0x0000FFFFu;
+    w = out ? (w & ~part) | (L::kNothing & part) : w;
+  }
+  // what lies outside the row (or behind group `stop`) becomes -infinity
+  __device__ __forceinline__ void trim(int group, int stop, uint4 (&raw)[8 / L::kPer]) const {
+    const int last = min(end, stop * 8);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = first + e >= head && first + e < end ? v[e] : -INFINITY;
-    }
+    for (int e = 0; e < 8; ++e) remove(raw, e, (group * 8 + e < head) | (group * 8 + e >= last));
   }
   __device__ __forceinline__ float at(int id) const {
     const char* p = base + (static_cast<long>(head) + id) * L::kBytes;
@@ -189,8 +209,6 @@ struct Largest {
   }
 };
 
-struct Sums { float most, left_out, others, moment; };   // largest logit, how many of it are left out, sum of the other exponentials, sum of exponential times exponent
-
 __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, __uint_as_float(exchanged<32>(__float_as_uint(v))));
   v = fmaxf(v, __uint_as_float(exchanged<16>(__float_as_uint(v))));
@@ -211,156 +229,175 @@ __device__ __forceinline__ u64 holders_largest(u64 v) {
   }
 }
 
+// What is known of a part of a row: its largest logit, how many logits of that value are left out (one at most of a wave's), the sum of
+// the other exponentials against it, and the sum of exponential times exponent (in powers of 2).
+struct Part { float most, left_out, others, moment; };
+
+// The parts in the lanes, as one (in all lanes).
+__device__ __forceinline__ Part joined(Part p, float c) {
+  const float M = wave_max(p.most);
+  const bool nan = !(p.others < INFINITY);
+  if (p.most < M) {
+    const float n = p.most > -INFINITY ? p.left_out + p.others : 0.f;
+    const float u = fmaxf((p.most - M) * c, -200.f), f = p.most > -INFINITY ? __builtin_amdgcn_exp2f(u) : 0.f;
+    p.moment = f * fmaf(n, u, p.moment);
+    p.others = n * f;
+    p.left_out = 0.f;
+  }
+  p.others = wave_sum(p.others);
+  p.moment = wave_sum(p.moment);
+  p.left_out = wave_sum(p.left_out);
+  if (__ballot(nan)) p.others = NAN;
+  p.most = M;
+  return p;
+}
+
+// A wave goes through its chunks (64 lanes x G groups, each wave of the workgroup every fourth) with the next one's loads on the way.  Chunks
+// are taken against the largest logit so far: sums are rescaled only when it grows, a few times a row.
 template <typename L, int G>
-__global__ __launch_bounds__(kLanes, 4) void logprobs_kernel(LogprobsArgs a) {
+__global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
   constexpr int W = 16 / G;                    // lanes of a holder: 16 groups
-  constexpr int kHolders = kLanes / W;         // of a slice
-  __shared__ __attribute__((aligned(16))) u64 bests[kHolders];
+  constexpr int kHolders = 64 / W;             // of a chunk
+  __shared__ __attribute__((aligned(16))) u64 bests[kHoldersMax];
   __shared__ u64 buf[128];
-  __shared__ float red[4][4];
-  __shared__ int last_flag;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const long row_no = blockIdx.x / static_cast<unsigned>(a.slices);
-  const int slice = static_cast<int>(blockIdx.x - row_no * a.slices);
+  __shared__ Part parts[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row_int = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x / static_cast<unsigned>(a.slices)));
+  const long row_no = row_int;
+  const int slice = static_cast<int>(blockIdx.x) - row_int * a.slices;
   const Row<L> row(a.logits, a.ld, row_no, a.n_vocab);
   const int per = a.slice_len / kGroup, first = slice * per;
   const int stop = min(first + per, (row.end + 7) / 8);                 // groups of the slice
+  const int chunks = (per + 64 * G - 1) / (64 * G), count = a.slices * chunks * kHolders;
+  const float c = a.scale * kLog2E;
 
-  // ---- the slice, its maxima
-  uint4 raw[G][8 / L::kPer];
+  uint4 raw[G][8 / L::kPer], next[G][8 / L::kPer];
+  auto load = [&](int chunk, uint4 (&to)[G][8 / L::kPer]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < G; ++i) {
-    const int group = first + i * kLanes + tid;
-    if (group < stop) row.load(group, raw[i], true);
-  }
-  float most = -INFINITY;
-  int where = first + tid;
+    for (int i = 0; i < G; ++i) {
+      row.template load<true>(first + (chunk * G + i) * 64 + lane, to[i]);
+    }
+  };
+  float M = -INFINITY, left_out = 0.f, sum = 0.f, moment = 0.f;         // of the wave so far; M and left_out uniform
+  auto process = [&](int chunk, uint4 (&raw)[G][8 / L::kPer]) __attribute__((always_inline)) {
+    const int g0 = first + chunk * G * 64;
+    if (g0 * 8 < row.head || (g0 + G * 64) * 8 > row.end || g0 + G * 64 > stop) {       // (uniform: a chunk at an end of the row)
 #pragma unroll
-  for (int i = 0; i < G; ++i) {
-    const int group = first + i * kLanes + tid;
-    if (group < stop) {
+      for (int i = 0; i < G; ++i) row.trim(g0 + i * 64 + lane, stop, raw[i]);
+    }
+    float most = -INFINITY;
+    int where = 0;
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
       float v[8];
-      row.values(group, raw[i], v);
+      L::unpack(raw[i], v);
       const float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
       if (m > most) {
         most = m;
-        where = group;
+        where = i;
       }
     }
-  }
-  {
-    const float m = wave_max(most);
-    if (lane == 0) red[wave][0] = m;
-  }
-  if (a.n_top > 0) {
-    const u64 mine = holders_largest<W>(first + tid < stop ? candidate(most, where * 8) : 0);
-    if (tid % W == 0) {
-      if (a.slices > 1) __hip_atomic_store(a.best + (row_no * a.slices + slice) * kHolders + tid / W, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      else bests[tid / W] = mine;
+    if (a.n_top > 0) {
+      const u64 mine = holders_largest<W>(g0 + lane < stop ? candidate(most, (g0 + where * 64 + lane) * 8) : 0);
+      const int at = chunk * kHolders + lane / W;
+      if (lane % W == 0) {
+        if (a.slices > 1) __hip_atomic_store(a.best + row_no * count + slice * (chunks * kHolders) + at, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        else bests[at] = mine;
+      }
     }
-  }
-  __syncthreads();
-  const float top = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
-  __syncthreads();
-
-  // ---- the exponentials.  The logits wait as they came: without this the compiler would keep them unpacked, in twice the registers.
+    // the logits wait as they came: without this the compiler would keep them unpacked, in twice the registers
 #pragma unroll
-  for (int i = 0; i < G; ++i)
+    for (int i = 0; i < G; ++i)
 #pragma unroll
-    for (int h = 0; h < 8 / L::kPer; ++h) asm volatile("" : "+v"(raw[i][h].x), "+v"(raw[i][h].y), "+v"(raw[i][h].z), "+v"(raw[i][h].w));
-  const float c = a.scale * kLog2E;
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, moment = 0.f;
-  const bool holds = most == top && top > -INFINITY;
-  bool out = !holds;                           // one of the largest logits is left out
+      for (int h = 0; h < 8 / L::kPer; ++h) asm volatile("" : "+v"(raw[i][h].x), "+v"(raw[i][h].y), "+v"(raw[i][h].z), "+v"(raw[i][h].w));
+    const float top = wave_max(most);
+    if (top > M) {                             // (uniform) the largest so far: one of it is left out, the one before counts again
+      if (M > -INFINITY) {
+        const float u = fmaxf((M - top) * c, -200.f), f = __builtin_amdgcn_exp2f(u);
+        if (lane == 0) sum += left_out;
+        moment = f * fmaf(sum, u, moment);
+        sum *= f;
+      }
+      M = top;
+      left_out = 1.f;
+      bool out = lane != static_cast<int>(__builtin_ctzll(__ballot(most == top)));
 #pragma unroll
-  for (int i = 0; i < G; ++i) {
-    const int group = first + i * kLanes + tid;
-    if (group < stop) {
+      for (int i = 0; i < G; ++i) {
+        float v[8];
+        L::unpack(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool now = !out & (v[e] == top);
+          Row<L>::remove(raw[i], e, now);
+          out |= now;
+        }
+      }
+    }
+    const float ref = M == -INFINITY ? 0.f : M;
+    float s = 0.f, t = 0.f;
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
       float v[8];
-      row.values(group, raw[i], v);
-      if (holds) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!out && v[e] == top) {
-            v[e] = -INFINITY;
-            out = true;
-          }
-      }
+      L::unpack(raw[i], v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float u = (v[e] - ref) * c;
         const float x = __builtin_amdgcn_exp2f(u);
-        sum += x;
-        moment = fmaf(x, fmaxf(u, -200.f), moment);    // (0 times -infinity)
+        s += x;
+        t = fmaf(x, fmaxf(u, -200.f), t);      // (0 times -infinity)
       }
     }
+    sum += s;
+    moment += t;
+  };
+  // (two chunks a turn: copied into place, the next one's loads would be waited for at once)
+  load(wave, raw);
+  for (int chunk = wave; chunk < chunks; chunk += 8) {
+    load(chunk + 4, next);
+    process(chunk, raw);
+    if (chunk + 4 >= chunks) break;
+    load(chunk + 8, raw);
+    process(chunk + 4, next);
   }
   sum = wave_sum(sum);
   moment = wave_sum(moment);
-  const int held = __popcll(__ballot(holds));
-  if (lane == 0) {
-    red[wave][0] = static_cast<float>(held);
-    red[wave][1] = sum;
-    red[wave][2] = moment;
-  }
-  __syncthreads();
-  Sums s{top, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    s.left_out += red[k][0];
-    s.others += red[k][1];
-    s.moment += red[k][2];
-  }
+  if (lane == 0) parts[wave] = Part{M, left_out, sum, moment};
 
   // ---- the row's slices meet
-  if (a.slices > 1) {
-    float* const to = a.sums + (row_no * a.slices + slice) * 4;
-    if (tid < 4) {
-      const float v = tid == 0 ? s.most : tid == 1 ? s.left_out : tid == 2 ? s.others : s.moment;
-      __hip_atomic_store(to + tid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-      const unsigned old = __hip_atomic_fetch_add(a.counters + row_no, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last_flag = old == static_cast<unsigned>(a.slices - 1);
-    }
-    __syncthreads();
-    if (!last_flag) return;
-    if (tid == 0) __hip_atomic_store(a.counters + row_no, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("" ::: "memory");
-  }
+  if (a.slices > 1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the wave's holders
+  __syncthreads();
   if (wave != 0) return;
-  float M = s.most, left_out = s.left_out, others = s.others, moments = s.moment;
+  const Part none{-INFINITY, 0.f, 0.f, 0.f};
+  Part p = joined(lane < 4 ? parts[lane & 3] : none, c);
   if (a.slices > 1) {
-    const float* const from = a.sums + row_no * a.slices * 4;
-    M = -INFINITY;
-    bool nan = false;
-    for (int i = lane; i < a.slices; i += 64) M = fmaxf(M, __hip_atomic_load(from + 4 * i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    M = wave_max(M);
-    others = moments = left_out = 0.f;
-    for (int i = lane; i < a.slices; i += 64) {
-      const float m = __hip_atomic_load(from + 4 * i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float n = __hip_atomic_load(from + 4 * i + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float x = __hip_atomic_load(from + 4 * i + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const float t = __hip_atomic_load(from + 4 * i + 3, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      nan = nan || !(x < INFINITY);
-      if (m == M) {
-        left_out += n;
-        others += x;
-        moments += t;
-      } else if (m > -INFINITY) {
-        const float u = (m - M) * c, f = __builtin_amdgcn_exp2f(u);      // the slice's largest against the row's
-        others = fmaf(n + x, f, others);
-        moments += f * fmaf(n + x, fmaxf(u, -200.f), t);
+    float* const sums = a.sums + row_no * a.slices * 4;
+    if (lane < 4)
+      __hip_atomic_store(sums + slice * 4 + lane, lane == 0 ? p.most : lane == 1 ? p.left_out : lane == 2 ? p.others : p.moment, __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    unsigned old = 0;
+    if (lane == 0) old = __hip_atomic_fetch_add(a.counters + row_no, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__builtin_amdgcn_readfirstlane(old) != static_cast<unsigned>(a.slices - 1)) return;
+    if (lane == 0) __hip_atomic_store(a.counters + row_no, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::: "memory");
+    Part all = none;
+    for (int i0 = 0; i0 < a.slices; i0 += 64) {
+      Part q = none;
+      if (i0 + lane < a.slices) {
+        const float* const from = sums + (i0 + lane) * 4;
+        q.most = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        q.left_out = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        q.others = __hip_atomic_load(from + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        q.moment = __hip_atomic_load(from + 3, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
+      q = joined(q, c);
+      all = i0 == 0 ? q : joined(lane == 0 ? all : lane == 1 ? q : none, c);
     }
-    others = wave_sum(others);
-    moments = wave_sum(moments);
-    left_out = wave_sum(left_out);
-    if (__ballot(nan)) others = NAN;
+    p = all;
   }
+  M = p.most;
+  left_out = p.left_out;
+  const float others = p.others, moments = p.moment;
   const bool undefined = !(others < INFINITY) || M == INFINITY;
   const bool nothing = M == -INFINITY && !undefined;
   const float log_sum = log1pf(left_out - 1.f + others);
@@ -390,7 +427,6 @@ __global__ __launch_bounds__(kLanes, 4) void logprobs_kernel(LogprobsArgs a) {
   }
   const int n = a.n_top;
   // candidates come 16 to a lane (eight 16-byte loads, coherent across the chip); up to 1024 are read once
-  const int count = a.slices * kHolders;
   constexpr int kAtOnce = 16;
   u64 held_by[kAtOnce];
   auto load_holders = [&](int i0) __attribute__((always_inline)) {
@@ -405,7 +441,7 @@ __global__ __launch_bounds__(kLanes, 4) void logprobs_kernel(LogprobsArgs a) {
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) held_by[i] = i0 + i * 64 + lane < kHolders ? bests[i0 + i * 64 + lane] : 0;
+      for (int i = 0; i < kAtOnce; ++i) held_by[i] = i0 + i * 64 + lane < count ? bests[i0 + i * 64 + lane] : 0;
     }
   };
   u64 mine = 0;
@@ -428,13 +464,13 @@ __global__ __launch_bounds__(kLanes, 4) void logprobs_kernel(LogprobsArgs a) {
     const u64 holder = shuffle_from(holders.best, h & 63);
     const int group0 = place_of(holder) / 8;   // one of the holder's groups: its lane and its slice
     const int from_slice = group0 / per, in_slice = group0 - from_slice * per;
-    const int group = from_slice * per + in_slice % kLanes / W * W + lane % 16 % W + lane % 16 / W * kLanes;
+    const int group = from_slice * per + in_slice / (64 * G) * (64 * G) + in_slice % 64 / W * W + lane % 16 % W + lane % 16 / W * 64;
     const bool valid = h < n && holder != 0 && group < min((from_slice + 1) * per, (row.end + 7) / 8);
     float v[8];
     uint4 again[8 / L::kPer];
     if (valid) {
-      row.load(group, again, false);
-      row.values(group, again, v);
+      row.template load<false>(group, again);
+      L::unpack(again, v);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -452,12 +488,8 @@ __global__ __launch_bounds__(kLanes, 4) void logprobs_kernel(LogprobsArgs a) {
 template <typename L>
 hipError_t launch_type(const LogprobsArgs& a, hipStream_t s) {
   const unsigned grid = static_cast<unsigned>(a.n_rows) * static_cast<unsigned>(a.slices);
-  const int groups = (a.slice_len / kGroup + kLanes - 1) / kLanes;
-  if (groups <= 1) logprobs_kernel<L, 1><<<grid, kLanes, 0, s>>>(a);
-  else if (groups <= 2) logprobs_kernel<L, 2><<<grid, kLanes, 0, s>>>(a);
-  else if (groups <= 4) logprobs_kernel<L, 4><<<grid, kLanes, 0, s>>>(a);
-  else if (L::kBytes == 4 || groups <= 8) logprobs_kernel<L, 8><<<grid, kLanes, 0, s>>>(a);
-  else if constexpr (L::kBytes == 2) logprobs_kernel<L, 16><<<grid, kLanes, 0, s>>>(a);
+  if (a.slice_len <= kSmallSlice) logprobs_kernel<L, 1><<<grid, kLanes, 0, s>>>(a);
+  else logprobs_kernel<L, 4><<<grid, kLanes, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -466,19 +498,18 @@ hipError_t launch_type(const LogprobsArgs& a, hipStream_t s) {
 LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type) {
   LogprobsPlan p{};
   const long places = static_cast<long>(n_vocab) + 7;                   // a row may start inside a group
-  const long most = kLanes * kGroup * (type == kLogitsF32 ? 8 : 16);
-  long slices = (places + most - 1) / most;
-  if (n_rows * slices < 512) {                                          // few rows: slices for all compute units
-    const long fine = (places + kLanes * kGroup - 1) / (kLanes * kGroup), want = (512 + n_rows - 1) / n_rows;
-    slices = want < fine ? want : fine;
+  constexpr long kMost = kHoldersMax / 16 * 2048;                       // a slice's holders lie in LDS
+  long slices = (places + kMost - 1) / kMost;
+  if (n_rows * slices < kWorkgroups) {                                  // few rows: slices for all compute units
+    const long fine = (places + kLeastSlice - 1) / kLeastSlice, want = (kWorkgroups + n_rows - 1) / n_rows;
+    slices = want < fine ? want : fine > slices ? fine : slices;
   }
   p.slice_len = static_cast<int>(((places + slices - 1) / slices + kGroup - 1) / kGroup * kGroup);
   p.slices = static_cast<int>((places + p.slice_len - 1) / p.slice_len);
   if (p.slices > 1) {
     p.sums_bytes = static_cast<size_t>(p.slices) * 4 * sizeof(float);
-    const int groups = (p.slice_len / kGroup + kLanes - 1) / kLanes;
-    const int holders = groups <= 1 ? 16 : groups <= 2 ? 32 : groups <= 4 ? 64 : groups <= 8 ? 128 : 256;    // of a slice
-    p.best_bytes = n_top > 0 ? static_cast<size_t>(p.slices) * holders * sizeof(u64) : 0;
+    const int chunk = p.slice_len <= kSmallSlice ? 512 : 2048, holders = chunk / 128;
+    p.best_bytes = n_top > 0 ? static_cast<size_t>(p.slices) * ((p.slice_len + chunk - 1) / chunk) * holders * sizeof(u64) : 0;
   }
   return p;
 }
