@@ -9,10 +9,12 @@
 //  * The most probable tokens.  128 logits (the 16 groups of one lane, or of 2, 4, .. lanes with fewer) are a holder, which keeps the largest
 //    of them and where it first stood.  The n tokens sought lie among the logits of the n holders with the largest (ties: the earlier
 //    place): any other holder's logits are beaten by n of those.  So only these are read again, and the pass over the row does
-//    nothing but take maxima, whatever the order of the logits.  One wave selects, in registers, 64 candidates at a time.
+//    nothing but take maxima, whatever the order of the logits.  One wave selects.  Its code runs once, so what it costs is fetching it:
+//    loops are left as loops (unrolled, with a sorting network for each step, 8 alternatives cost 5 us of latency more).
 // Exponentials are the hardware's exp2 of (logit - M) times scale / ln 2: the difference first, so that a row of nothing but the type's
 // lowest value, a common mask, is a row like any other.
 #include "kernels.hpp"
+#include "lds_load.hpp"
 #include "numeric.hpp"
 #include "w8.hpp"
 
@@ -26,8 +28,8 @@ constexpr int kLanes = 256;
 constexpr int kGroup = 8;                      // logits of a group
 constexpr int kHoldersMax = 2048;              // of a slice: one of 262144 logits
 constexpr int kSmallSlice = 4096;              // up to here a wave's chunks are of one group a lane, so that all four have some
-constexpr int kLeastSlice = 2048;              // few rows: no shorter slices
-constexpr int kWorkgroups = 1024;              // and no more of them than this many in all
+constexpr int kLeastSlice = 4096, kLeastOfMany = 24576;   // few rows: no shorter slices, from 128 rows on
+constexpr int kWorkgroups = 512;               // and no more of them than this many in all
 
 __device__ __forceinline__ uint32_t& word_of(uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 struct Logits16 {
@@ -162,6 +164,10 @@ __device__ __forceinline__ u64 sorted(u64 v, int lane) {
   else return v;
 }
 
+__device__ __forceinline__ int lanes_before(u64 mask) {        // of the mask's, before this one
+  return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0)));
+}
+
 // The largest 64 of all values offered, in a wave's lanes.
 struct Largest {
   u64 best, least;                             // sorted; what an offered value has to reach
@@ -174,7 +180,7 @@ struct Largest {
   }
   __device__ __forceinline__ void merge(u64 v) {
     v = sorted(v, lane);
-    if (lane_value(best, 0) == 0) {
+    if (best_empty()) {
       best = v;
       return;
     }
@@ -185,7 +191,7 @@ struct Largest {
     const bool in = v >= least && v != 0;
     const u64 mask = __ballot(in);
     if (!mask) return;
-    const int at = count + static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0)));
+    const int at = count + lanes_before(mask);
     if (in) buf[at] = v;
     count += __popcll(mask);
     if (count >= 64) {
@@ -200,6 +206,7 @@ struct Largest {
       if (nth > least) least = nth;
     }
   }
+  __device__ __forceinline__ bool best_empty() const { return lane_value(best, 0) == 0; }
   __device__ __forceinline__ void done() {
     if (count == 0) return;
     order();
@@ -278,6 +285,14 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
       row.template load<true>(first + (chunk * G + i) * 64 + lane, to[i]);
     }
   };
+  // the given tokens' logits (64 at most) are on their way before they are needed
+  int id = -1;
+  float id_logit = 0.f;
+  if (wave == 0 && lane < a.n_given) {
+    id = a.given[row_no * a.n_given + lane];
+    if (id >= 0 && id < a.n_vocab) id_logit = row.at(id);
+  }
+
   float M = -INFINITY, left_out = 0.f, sum = 0.f, moment = 0.f;         // of the wave so far; M and left_out uniform
   auto process = [&](int chunk, uint4 (&raw)[G][8 / L::kPer]) __attribute__((always_inline)) {
     const int g0 = first + chunk * G * 64;
@@ -364,6 +379,24 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
   if (lane == 0) parts[wave] = Part{M, left_out, sum, moment};
 
   // ---- the row's slices meet
+  // candidates come 16 to a lane (eight 16-byte loads, coherent across the chip); up to 1024 are read once
+  constexpr int kAtOnce = 16;
+  u64 held_by[kAtOnce];
+  auto load_holders = [&](int i0) __attribute__((always_inline)) {
+    if (a.slices > 1) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(a.best + row_no * count, 0, count * 8, 0x00027000);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; i += 2) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(all, (i0 + i * 64 + lane * 2) * 8, 0, 16);
+        held_by[i] = (static_cast<u64>(v.y) << 32) | v.x;
+        held_by[i + 1] = (static_cast<u64>(v.w) << 32) | v.z;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) held_by[i] = i0 + i * 64 + lane < count ? bests[i0 + i * 64 + lane] : 0;
+    }
+  };
   if (a.slices > 1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the wave's holders
   __syncthreads();
   if (wave != 0) return;
@@ -380,6 +413,7 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
     if (__builtin_amdgcn_readfirstlane(old) != static_cast<unsigned>(a.slices - 1)) return;
     if (lane == 0) __hip_atomic_store(a.counters + row_no, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("" ::: "memory");
+    if (a.n_top > 0) load_holders(0);          // (with the slices' sums, not behind them)
     Part all = none;
     for (int i0 = 0; i0 < a.slices; i0 += 64) {
       Part q = none;
@@ -407,11 +441,11 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
   };
   if (a.entropy && lane == 0) a.entropy[row_no] = undefined ? NAN : nothing ? 0.f : log_sum - kLn2 * moments / (left_out + others);
   for (int i = lane; i < a.n_given; i += 64) {
-    const int id = a.given[row_no * a.n_given + i];
-    float p = NAN;
-    if (id < 0) p = 0.f;
-    else if (id < a.n_vocab) p = logp_of(row.at(id));
-    a.logp[row_no * a.n_given + i] = p;
+    if (i >= 64) {
+      id = a.given[row_no * a.n_given + i];
+      id_logit = id >= 0 && id < a.n_vocab ? row.at(id) : 0.f;
+    }
+    a.logp[row_no * a.n_given + i] = id < 0 ? 0.f : id < a.n_vocab ? logp_of(id_logit) : NAN;
   }
   if (a.n_top == 0) return;
 
@@ -426,62 +460,113 @@ __global__ __launch_bounds__(kLanes) void logprobs_kernel(LogprobsArgs a) {
     return;
   }
   const int n = a.n_top;
-  // candidates come 16 to a lane (eight 16-byte loads, coherent across the chip); up to 1024 are read once
-  constexpr int kAtOnce = 16;
-  u64 held_by[kAtOnce];
-  auto load_holders = [&](int i0) __attribute__((always_inline)) {
-    if (a.slices > 1) {
-      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-      const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(a.best + row_no * count, 0, count * 8, 0x00027000);
-#pragma unroll
-      for (int i = 0; i < kAtOnce; i += 2) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(all, (i0 + i * 64 + lane * 2) * 8, 0, 16);
-        held_by[i] = (static_cast<u64>(v.y) << 32) | v.x;
-        held_by[i + 1] = (static_cast<u64>(v.w) << 32) | v.z;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) held_by[i] = i0 + i * 64 + lane < count ? bests[i0 + i * 64 + lane] : 0;
-    }
-  };
+  // n lanes at least have a largest holder of key t or more, so n candidates do
   u64 mine = 0;
+  if (a.slices == 1) load_holders(0);
   for (int i0 = 0; i0 < count; i0 += 64 * kAtOnce) {
-    load_holders(i0);
+    if (i0 > 0) load_holders(i0);
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) mine = held_by[i] > mine ? held_by[i] : mine;
   }
-  Largest holders(buf, lane, n, lane_value(sorted(mine, lane), n - 1));
+  const uint32_t mine_key = static_cast<uint32_t>(mine >> 32);
+  uint32_t t = 0;
+#pragma unroll 1
+  for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+    if (__popcll(__ballot(mine_key >= (t | bit))) >= n) t |= bit;
+  u64 least = static_cast<u64>(t) << 32;
+  // holders that reach it: a few more than n, unless logits are alike
+  int found = 0;
   for (int i0 = 0; i0 < count; i0 += 64 * kAtOnce) {
     if (count > 64 * kAtOnce) load_holders(i0);
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) holders.offer(held_by[i]);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const bool in = held_by[i] >= least && held_by[i] != 0;
+      const u64 mask = __ballot(in);
+      const int at = found + lanes_before(mask);
+      if (in && at < 64) buf[at] = held_by[i];
+      found += __popcll(mask);
+    }
   }
-  holders.done();
-  const u64 nth = lane_value(holders.best, n - 1);
-  Largest tokens(buf, lane, n, nth ? nth - 7 : 0);     // (its place is its group's first: the logit lies at most 7 further)
-  for (int h0 = 0; h0 < n; h0 += 4) {          // 16 lanes to a holder, a group each
-    const int h = h0 + lane / 16;
-    const u64 holder = shuffle_from(holders.best, h & 63);
-    const int group0 = place_of(holder) / 8;   // one of the holder's groups: its lane and its slice
+  Largest::order();
+  u64 mine_held = lane < found ? buf[lane] : 0;
+  Largest::order();
+  if (found > 64) {                            // the n largest of them
+    Largest holders(buf, lane, n, least);
+    for (int i = lane; i - lane < count; i += 64)
+      holders.offer(i >= count ? 0 : a.slices > 1 ? __hip_atomic_load(a.best + row_no * count + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : bests[i]);
+    holders.done();
+    found = n;
+    mine_held = holders.best;
+    least = lane_value(holders.best, n - 1) - 7;       // (its place is its group's first: the logit lies at most 7 further)
+  }
+  const float least_value = value_of(static_cast<uint32_t>(least >> 32));      // (of nothing: NaN, see below)
+
+  // The holders' logits, 16 lanes to a holder, a group each: straight into LDS, so that all are on their way at once.
+  int holder0 = -1, holder_stop = 0;           // of the lane's holder: its first group, where its slice ends
+  if (lane < found && mine_held != 0) {
+    const int group0 = place_of(mine_held) / 8;        // one of its groups: its lane and its slice
     const int from_slice = group0 / per, in_slice = group0 - from_slice * per;
-    const int group = from_slice * per + in_slice / (64 * G) * (64 * G) + in_slice % 64 / W * W + lane % 16 % W + lane % 16 / W * 64;
-    const bool valid = h < n && holder != 0 && group < min((from_slice + 1) * per, (row.end + 7) / 8);
-    float v[8];
-    uint4 again[8 / L::kPer];
-    if (valid) {
-      row.template load<false>(group, again);
-      L::unpack(again, v);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int place = group * 8 + e;
-      tokens.offer(valid && place >= row.head && place < row.end ? candidate(v[e], place) : 0);
-    }
+    holder0 = from_slice * per + in_slice / (64 * G) * (64 * G) + in_slice % 64 / W * W;
+    holder_stop = min((from_slice + 1) * per, (row.end + 7) / 8);
   }
-  tokens.done();
-  if (lane < n) {
-    ids[lane] = place_of(tokens.best) - row.head;
-    if (tops) tops[lane] = logp_of(value_of(static_cast<uint32_t>(tokens.best >> 32)));
+  const int within = lane % 16 % W + lane % 16 / W * 64;
+  auto group_of = [&](int j) __attribute__((always_inline)) {
+    const int h = 4 * j + lane / 16, first = __shfl(holder0, h), end = __shfl(holder_stop, h);   // (both by all lanes)
+    return first >= 0 && first + within < end ? first + within : -1;
+  };
+  constexpr int kPieces = 8 / L::kPer, kReads = kHoldersMax * 8 / (1024 * kPieces);
+  const auto buffer = raw_buffer(row.base, static_cast<uint32_t>((row.end - 1) / L::kPer + 1) * 16u);
+  const uint32_t staged = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char*)bests));
+  Largest tokens(buf, lane, n, least);
+  for (int j0 = 0; 4 * j0 < found; j0 += kReads) {
+    const int reads = min(kReads, (found + 3) / 4 - j0);
+#pragma unroll 1
+    for (int j = 0; j < reads; ++j) {
+      const int group = group_of(j0 + j);
+#pragma unroll
+      for (int h = 0; h < kPieces; ++h)
+        load_to_lds(buffer, staged + (j * kPieces + h) * 1024, group < 0 ? kOutside : static_cast<uint32_t>((group * kPieces + h) * 16));
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll 1
+    for (int j = 0; j < reads; ++j) {
+      const int group = group_of(j0 + j);
+      uint4 again[kPieces];
+#pragma unroll
+      for (int h = 0; h < kPieces; ++h) again[h] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(bests) + (j * kPieces + h) * 1024 + lane * 16);
+      float v[8];
+      L::unpack(again, v);
+      uint32_t bits = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bits |= v[e] < least_value ? 0u : 1u << e;
+      if (group < 0) bits = 0;
+#pragma unroll 1
+      while (__ballot(bits != 0)) {
+        const int e = __ffs(static_cast<int>(bits)) - 1;
+        float x = v[0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) x = e == k ? v[k] : x;
+        const int place = group * 8 + e;
+        tokens.offer(bits != 0 && place >= row.head && place < row.end ? candidate(x, place) : 0);
+        bits &= bits - 1;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+  auto answer = [&](int at, u64 token) __attribute__((always_inline)) {
+    ids[at] = place_of(token) - row.head;
+    if (tops) tops[at] = logp_of(value_of(static_cast<uint32_t>(token >> 32)));
+  };
+  if (tokens.best_empty()) {                   // at most 63 came: each finds its place by counting
+    Largest::order();
+    const u64 token = lane < tokens.count ? buf[lane] : 0;
+    int rank = 0;
+#pragma unroll 1
+    for (int i = 0; i < tokens.count; ++i) rank += lane_value(token, i) > token;
+    if (lane < tokens.count && rank < n) answer(rank, token);
+  } else {
+    tokens.done();
+    if (lane < n) answer(lane, tokens.best);
   }
 }
 
@@ -501,8 +586,9 @@ LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type) {
   constexpr long kMost = kHoldersMax / 16 * 2048;                       // a slice's holders lie in LDS
   long slices = (places + kMost - 1) / kMost;
   if (n_rows * slices < kWorkgroups) {                                  // few rows: slices for all compute units
-    const long fine = (places + kLeastSlice - 1) / kLeastSlice, want = (kWorkgroups + n_rows - 1) / n_rows;
-    slices = want < fine ? want : fine > slices ? fine : slices;
+    const long fine = places / (n_rows < 128 ? kLeastSlice : kLeastOfMany), want = (kWorkgroups + n_rows - 1) / n_rows;
+    const long more = want < fine ? want : fine;
+    if (more > slices) slices = more;
   }
   p.slice_len = static_cast<int>(((places + slices - 1) / slices + kGroup - 1) / kGroup * kGroup);
   p.slices = static_cast<int>((places + p.slice_len - 1) / p.slice_len);

@@ -48,6 +48,7 @@ hipError_t launch_product8(const Product8Args& a, const Product8Plan& p, hipStre
 // Log probabilities of logits [n_rows, ld], the first n_vocab of a row.
 enum : int { kLogitsF16 = 0, kLogitsBF16 = 1, kLogitsF32 = 2 };
 constexpr int kTopMax = 64;
+constexpr int kVocabMax = 1 << 28;     // bytes of a row are below 2^31
 struct LogprobsArgs {
   const void* logits;
   long ld;

@@ -79,7 +79,7 @@ def test_logprobs_refusals(lib, kw):
 def test_logprobs_beyond_the_kernels(lib):
     assert call(lib.larosa_logprobs, LOGPROBS, n_top=65) == EUNSUPPORTED
     assert call(lib.larosa_logprobs, LOGPROBS, n_rows=(1 << 24) + 1) == EUNSUPPORTED
-    assert call(lib.larosa_logprobs, LOGPROBS, n_vocab=(1 << 30) + 1, ld=(1 << 30) + 1) == EUNSUPPORTED
+    assert call(lib.larosa_logprobs, LOGPROBS, n_vocab=(1 << 28) + 1, ld=(1 << 28) + 1) == EUNSUPPORTED
 
 
 @pytest.mark.parametrize("kw", [dict(x=ODD), dict(ld_x=252), dict(rms_eps=float("nan")), dict(n_vocab=0), dict(scale=0.0), dict(given=None), dict(t=2),
