@@ -73,10 +73,18 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], uint32_t& byte
   return fine ? make_uint2(lo, hi) : make_uint2(kNanCodes, kNanCodes);
 }
 
+// Where the codes of columns col .. + 7 of a row go: its own line of `pitch` bytes, or (TILED, rows that only a product of this library reads)
+// the 16 x 64 codes that one load of the tile kernel takes as one kilobyte.
+template <bool TILED>
+__device__ __forceinline__ size_t code_at(size_t row, int col, int pitch) {
+  if constexpr (TILED) return ((row >> 4) * ((pitch + 63) >> 6) + (col >> 6)) * 1024 + (row & 15) * 64 + (col & 63);
+  else return row * pitch + col;
+}
+
 // Rows to codes, HBM-bound (2 bytes in, 1 out).  A wave takes 512 columns (16 bytes a lane, four blocks) of four rows at once; a
 // row's four scale bytes are one word.
 constexpr int kRowsAtOnce = 4;
-template <typename T>
+template <typename T, bool TILED>
 __global__ __launch_bounds__(256) void quantize_rows8_kernel(const uint16_t* __restrict__ x, long ld_x, int n_rows, int d,
                                                              uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -100,7 +108,7 @@ __global__ __launch_bounds__(256) void quantize_rows8_kernel(const uint16_t* __r
     const uint32_t word = __builtin_amdgcn_readlane(byte, 0) | (__builtin_amdgcn_readlane(byte, 16) << 8) |
                           (__builtin_amdgcn_readlane(byte, 32) << 16) | (__builtin_amdgcn_readlane(byte, 48) << 24);
     if (row0 + r < n_rows) {
-      if (col < pitch) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(row0 + r) * pitch + col) = c;
+      if (col < pitch) *reinterpret_cast<uint2*>(codes + code_at<TILED>(row0 + r, col, pitch)) = c;
       if (lane == 0) *reinterpret_cast<uint32_t*>(scales + static_cast<size_t>(row0 + r) * spitch + blockIdx.x * 4) = word;
     }
   }
@@ -108,7 +116,7 @@ __global__ __launch_bounds__(256) void quantize_rows8_kernel(const uint16_t* __r
 
 // The same behind a norm, v = x / sqrt(mean(x^2) + eps) * g in fp32 and not rounded before the codes: a workgroup per row, which
 // reads it twice (the second time from the caches).
-template <typename T>
+template <typename T, bool TILED>
 __global__ __launch_bounds__(512) void quantize_normed_rows8_kernel(const uint16_t* __restrict__ x, long ld_x, int n_rows, int d,
                                                                     const uint16_t* __restrict__ g, float eps,
                                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -151,7 +159,7 @@ __global__ __launch_bounds__(512) void quantize_normed_rows8_kernel(const uint16
     if (col >= (d + 127) / 128 * 128) byte = kScaleOne;
     const uint32_t word = __builtin_amdgcn_readlane(byte, 0) | (__builtin_amdgcn_readlane(byte, 16) << 8) |
                           (__builtin_amdgcn_readlane(byte, 32) << 16) | (__builtin_amdgcn_readlane(byte, 48) << 24);
-    if (col < pitch) *reinterpret_cast<uint2*>(codes + row * pitch + col) = c;
+    if (col < pitch) *reinterpret_cast<uint2*>(codes + code_at<TILED>(row, col, pitch)) = c;
     if (lane == 0) *reinterpret_cast<uint32_t*>(scales + row * spitch + col0 / 128) = word;
   }
 }
@@ -218,7 +226,7 @@ __global__ __launch_bounds__(256) void quantize_w8_kernel(const uint16_t* __rest
 // ---- the product, many rows --------------------------------------------------------------------------------
 // v_mfma_scale_f32_32x32x64 (e4m3 both sides): its first operand holds output channels (lane l: channel l % 32, 32 codes along k from
 // 32 (l / 32) on), its second rows of x the same way; register r of lane l of the result is channel 8 (r / 4) + 4 (l / 32) + r % 4, row
-// l % 32.  A workgroup of 4 waves (2 x 2) owns 64 MO output channels x 64 MT rows, a wave 32 MO x 32 MT.
+// l % 32.  A workgroup of 2 x WT waves owns 64 MO output channels x 32 WT MT rows, a wave 32 MO x 32 MT.
 //  * k-tiles of 64: 64 bytes of each row, brought straight into LDS, kStages tiles ahead; the 16-byte pieces of a row are exchanged by
 //    its number, so that the rows a read touches lie in different banks.  One barrier per k-tile: behind it the next tile is read
 //    while this one, in registers, is multiplied, and this one's stage takes the loads of the tile kStages further.
@@ -229,7 +237,6 @@ __global__ __launch_bounds__(256) void quantize_w8_kernel(const uint16_t* __rest
 // neighbour lose any: 1.4e-5 of the result's norm on random data, 4e-5 with a few strong channels, where a 16-bit result rounds by 2e-4
 // (f16) or 1.7e-3, the codes by 2.6e-2, and a block's smallest code is 2^-18 of its largest.  Whole sums in bf16 cost more than twice the time.
 constexpr int kKTile8 = 64;
-constexpr int kStages8 = 4;
 
 template <int N, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
@@ -266,18 +273,29 @@ __device__ __forceinline__ TileAt8 tile_of8(int number, int tiles_m, int tiles_o
   return {band * kBand8 + number - o * rows, o};
 }
 
+// Rounded to nearest even by the instruction: in integer steps, as elsewhere in the library, with a branch around NaN, the 256 sums of a
+// lane of the large tile took 6 us of each tile.
 __device__ __forceinline__ uint2 pack_out4(F16, const float (&v)[4]) { return pack4<F16>(v); }
-__device__ __forceinline__ uint2 pack_out4(BF16, const float (&v)[4]) { return pack4<BF16>(v); }
+__device__ __forceinline__ uint2 pack_out4(BF16, const float (&v)[4]) {
+  const bfloat2 lo = {static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1])}, hi = {static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
+  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
 struct F32 {};                // logits that the caller's next step reads in full
 
-template <typename OUT, int MO, int MT>
-__global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel(Product8Args a) {
-  constexpr int TO = 64 * MO, TT = 64 * MT;
+template <typename OUT, bool TILED, int MO, int MT, int WT, int kStages>
+__global__ __launch_bounds__(128 * WT, MO * MT == 16 ? 1 : 2) void tile_product8_kernel(Product8Args a) {
+  constexpr int kWaves = 2 * WT;
+  constexpr int TO = 64 * MO, TT = 32 * WT * MT;
   constexpr int kBytesO = TO * kKTile8, kBytesT = TT * kKTile8, kStageBytes = kBytesO + kBytesT;
-  constexpr int LO = kBytesO / 4096, LT = kBytesT / 4096, kLoads = LO + LT;      // wave-loads per wave and stage
+  constexpr int kSweep = kWaves * 1024;            // bytes that one load of each wave fills
+  constexpr int LO = kBytesO / kSweep, LT = kBytesT / kSweep, kLoads = LO + LT;      // wave-loads per wave and stage
   constexpr int kScaleBytes = TT * 4;
-  constexpr int kRing = kStages8 * kStageBytes;
-  __shared__ __attribute__((aligned(1024))) char lds[kRing + 2 * kScaleBytes];
+  constexpr int kRing = kStages * kStageBytes;
+  constexpr int kCols = 32 * MO;
+  constexpr bool kWide = std::is_same<OUT, F32>::value;
+  constexpr int kPitch = kWide ? kCols * 4 + 16 : kCols * 2 + 16;                // bytes of a row of sums on its way out
+  constexpr int kStrips = kWaves * 32 * kPitch, kOperands = kRing + 2 * kScaleBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[kStrips > kOperands ? kStrips : kOperands];
   __shared__ int last_flag;
 
   const int tiles = a.tiles_m * a.tiles_o, jobs = tiles * a.splits;
@@ -290,28 +308,32 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wo = w >> 1, wt = w & 1;
+  const int wo = w / WT, wt = w % WT;
   const int pitch = (a.d_in + 15) / 16 * 16, blocks = (a.d_in + 127) / 128, spitch = (blocks + 3) / 4 * 4;
   const int kb0 = split * a.blocks_per, kb1 = min(blocks, kb0 + a.blocks_per);
   const int rows_o = min(TO, a.d_out - o0), rows_t = min(TT, a.n_rows - m0);
 
   // ---- loads.  A panel's rows behind the last lie outside its buffer and arrive as zeros.
   const u32x4 buf_o = raw_buffer(a.w.codes + static_cast<size_t>(o0) * pitch, static_cast<uint32_t>(rows_o) * pitch);
-  const u32x4 buf_t = raw_buffer(a.x.codes + static_cast<size_t>(m0) * pitch, static_cast<uint32_t>(rows_t) * pitch);
+  const int x_pitch = TILED ? (pitch + 63) / 64 * 64 : pitch;           // bytes of a row, on the average
+  const u32x4 buf_t = raw_buffer(a.x.codes + static_cast<size_t>(m0) * x_pitch, static_cast<uint32_t>(TILED ? (rows_t + 15) / 16 * 16 : rows_t) * x_pitch);
   const u32x4 buf_s = raw_buffer(a.x.scales + static_cast<size_t>(m0) * spitch, static_cast<uint32_t>(rows_t) * spitch);
-  // wave-load q of wave w fills 16 rows from 16 (4 q + w) on; piece p of row r holds codes 16 (p ^ (r / 4 % 4)) .. + 15 of the k-tile
+  // wave-load q of wave w fills 16 rows from 16 (kWaves q + w) on; piece p of row r holds codes 16 (p ^ (r / 4 % 4)) .. + 15 of the k-tile
   const int lrow = 16 * w + (lane >> 2), lpiece = 16 * ((lane & 3) ^ ((lane >> 4) & 3));
-  uint32_t off[LO > LT ? LO : LT];
+  uint32_t off_o[LO], off_t[LT];
 #pragma unroll
-  for (int q = 0; q < (LO > LT ? LO : LT); ++q) off[q] = static_cast<uint32_t>((64 * q + lrow) * pitch + lpiece);
+  for (int q = 0; q < LO; ++q) off_o[q] = static_cast<uint32_t>((16 * kWaves * q + lrow) * pitch + lpiece);
+#pragma unroll
+  for (int q = 0; q < LT; ++q)
+    off_t[q] = TILED ? static_cast<uint32_t>((kWaves * q + w) * 16 * x_pitch + (lane >> 2) * 64 + lpiece) : static_cast<uint32_t>((16 * kWaves * q + lrow) * pitch + lpiece);
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char*)lds));
   const int k_end = min(pitch, kb1 * 128);
-  int f_k = kb0 * 128, f_stage = 0;
+  int f_k = kb0 * 128;                           // the k-tile to load next, and its stage
+  uint32_t f_lds = lds_base + w * 1024;
   auto fetch_piece = [&](int q) __attribute__((always_inline)) {
-    const uint32_t to = lds_base + f_stage * kStageBytes + w * 1024;
     const bool in = f_k + lpiece < k_end;        // (pitch is a multiple of 16: a piece is inside or not)
-    if (q < LO) load_to_lds(buf_o, to + q * 4096, in ? off[q] + f_k : kOutside);
-    else load_to_lds(buf_t, to + kBytesO + (q - LO) * 4096, in ? off[q - LO] + f_k : kOutside);
+    if (q < LO) load_to_lds(buf_o, f_lds + q * kSweep, in ? off_o[q] + f_k : kOutside);
+    else load_to_lds(buf_t, f_lds + kBytesO + (q - LO) * kSweep, in ? off_t[q - LO] + f_k * (TILED ? 16 : 1) : kOutside);
   };
   // scale words of the four blocks from f_k on, with the first of their k-tiles and in front of its loads
   const uint32_t off_s = static_cast<uint32_t>((64 * w + lane) * spitch);
@@ -321,7 +343,7 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
   };
   auto fetch_next = [&]() __attribute__((always_inline)) {
     f_k += kKTile8;
-    f_stage = (f_stage + 1) & (kStages8 - 1);
+    f_lds = f_lds >= lds_base + (kStages - 1) * kStageBytes ? f_lds - (kStages - 1) * kStageBytes : f_lds + kStageBytes;
   };
 
   // ---- operand reads: the two pieces of a lane's 32 codes
@@ -330,7 +352,7 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
   const int adr_t = kBytesO + (wt * MT * 32 + (lane & 31)) * kKTile8 + ((2 * half) ^ sw) * 16;
   auto read_piece = [&](int stage, int r, u32x4 (&v)[2 * (MO + MT)]) __attribute__((always_inline)) {
     const int adr = (r < 2 * MO ? adr_o + (r >> 1) * (32 * kKTile8) : adr_t + ((r - 2 * MO) >> 1) * (32 * kKTile8)) ^ (16 * (r & 1));
-    v[r] = *(const __attribute__((address_space(3))) u32x4*)((const lds_char*)lds + stage * kStageBytes + adr);
+    v[r] = *(const __attribute__((address_space(3))) u32x4*)((const lds_char*)lds + stage + adr);
   };
   auto operand = [&](const u32x4 (&v)[2 * (MO + MT)], int r) __attribute__((always_inline)) {
     return __builtin_shufflevector(__builtin_bit_cast(__attribute__((ext_vector_type(4))) int, v[2 * r]),
@@ -371,31 +393,33 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
   };
 
   u32x4 v0[2 * (MO + MT)], v1[2 * (MO + MT)];
-  for (int i = 0; i < kStages8; ++i) {
+  for (int i = 0; i < kStages; ++i) {
     if ((f_k & 511) == 0 || i == 0) fetch_scales();
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) fetch_piece(q);
     fetch_next();
   }
-  tile_landed<(kStages8 - 1) * kLoads>();
+  tile_landed<(kStages - 1) * kLoads>();
 #pragma unroll
   for (int r = 0; r < 2 * (MO + MT); ++r) read_piece(0, r, v0);
   int stage = 0;
+  auto after = [](int st) { return st == (kStages - 1) * kStageBytes ? 0 : st + kStageBytes; };
   for (int kb = kb0; kb < kb1; ++kb) {           // two k-tiles
     if ((kb & 3) == 0 || kb == kb0) {            // (uniform)
       if (kb > kb0) w_word = w_next;
       if (((kb >> 2) + 1) * 4 < kb1) w_next = w_scales[(kb >> 2) + 1];
     }
     s_w = static_cast<int>((w_word >> (8 * (kb & 3))) & 255u);
-    tile_landed<(kStages8 - 2) * kLoads>();
+    tile_landed<(kStages - 2) * kLoads>();
     read_scales(kb, s_t);
     if ((f_k & 511) == 0) fetch_scales();
-    products(v0, v1, (stage + 1) & (kStages8 - 1));
+    stage = after(stage);
+    products(v0, v1, stage);
     fetch_next();
-    tile_landed<(kStages8 - 2) * kLoads>();
-    products(v1, v0, (stage + 2) & (kStages8 - 1));
+    tile_landed<(kStages - 2) * kLoads>();
+    stage = after(stage);
+    products(v1, v0, stage);
     fetch_next();
-    stage = (stage + 2) & (kStages8 - 1);
   }
   // every load has landed and every wave has left the operands behind
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -403,7 +427,7 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
   // ---- parts of the sum: handed over through memory as 16-byte accesses that are coherent across the chip (sc1, see
   // gemv_core.hpp); the workgroup that arrives last adds them in their order.
   if (a.splits > 1) {
-    constexpr int kPieces = MO * MT * 4, kPart = kPieces * 4096;    // 16-byte pieces of a lane; bytes of a part
+    constexpr int kPiece = kWaves * 1024, kPart = MO * MT * 4 * kPiece;      // bytes of a 16-byte piece of all lanes, of a part
     constexpr int kCoherent = 16;
     const __amdgpu_buffer_rsrc_t parts = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<char*>(a.partial) + static_cast<size_t>(tile) * a.splits * kPart, 0, a.splits * kPart, 0x00027000);
@@ -413,7 +437,7 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
       for (int p = 0; p < 4; ++p) {
         const float16v& c = acc[x / MT][x % MT];
         const u32x4 v = {__float_as_uint(c[4 * p]), __float_as_uint(c[4 * p + 1]), __float_as_uint(c[4 * p + 2]), __float_as_uint(c[4 * p + 3])};
-        __builtin_amdgcn_raw_buffer_store_b128(v, parts, split * kPart + (4 * x + p) * 4096 + tid * 16, 0, kCoherent);
+        __builtin_amdgcn_raw_buffer_store_b128(v, parts, split * kPart + (4 * x + p) * kPiece + tid * 16, 0, kCoherent);
       }
     });
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
@@ -434,7 +458,7 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
         constexpr int x = decltype(ij)::value;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(parts, s * kPart + (4 * x + p) * 4096 + tid * 16, 0, kCoherent);
+          const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(parts, s * kPart + (4 * x + p) * kPiece + tid * 16, 0, kCoherent);
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[x / MT][x % MT][4 * p + e] += __uint_as_float(v[e]);
         }
@@ -442,10 +466,6 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
   }
 
   // ---- store: 32 rows at a time through the wave's own part of the LDS, so that memory sees whole runs of a row
-  constexpr int kCols = 32 * MO;
-  constexpr bool kWide = std::is_same<OUT, F32>::value;
-  constexpr int kPitch = kWide ? kCols * 4 + 16 : kCols * 2 + 16;                // bytes of a row
-  static_assert(4 * 32 * kPitch <= kRing, "the strips of four waves fit the LDS");
   char* const strip = lds + w * (32 * kPitch);
   const int ow = o0 + wo * kCols;
   static_for<MT>([&](auto jc) {
@@ -467,8 +487,12 @@ __global__ __launch_bounds__(256, MO * MT > 4 ? 1 : 2) void tile_product8_kernel
       const int r = p * kRowsPer + lane / kLanes, c = lane % kLanes * (16 / kSize);
       const int row = m0 + (wt * MT + j) * 32 + r;
       const uint4 v = *reinterpret_cast<const uint4*>(strip + r * kPitch + c * kSize);
-      if (row < a.n_rows && ow + c < a.d_out)
-        *reinterpret_cast<uint4*>(static_cast<char*>(a.y) + (row * a.ld_y + ow + c) * kSize) = v;
+      u32x4* const to = reinterpret_cast<u32x4*>(static_cast<char*>(a.y) + (row * a.ld_y + ow + c) * kSize);
+      if (row < a.n_rows && ow + c < a.d_out) {
+        // many tiles: y is larger than the L2 and would drive the operands out of it (4096 x 4096 x 28672: 458 -> 438 us)
+        if constexpr (MO * MT == 16 && !kWide) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), to);
+        else *to = __builtin_bit_cast(u32x4, v);
+      }
     }
     wave_lds_order();
   });
@@ -551,16 +575,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_rows8_kernel(Product8Ar
   }
 }
 
+template <typename OUT, bool TILED>
+void launch_tiles(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
+  const int jobs = p.tiles_m * p.tiles_o * p.splits;
+  const dim3 grid((jobs + 7) / 8 * 8);
+  if (p.kind == 1) tile_product8_kernel<OUT, TILED, 4, 4, 2, 4><<<grid, 256, 0, s>>>(a);
+  else if (p.kind == 2) tile_product8_kernel<OUT, TILED, 2, 2, 2, 4><<<grid, 256, 0, s>>>(a);
+  else tile_product8_kernel<OUT, TILED, 2, 1, 2, 4><<<grid, 256, 0, s>>>(a);
+}
+
 template <typename OUT>
 hipError_t launch_out(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
-  if (p.kind == 0) {
-    few_rows8_kernel<OUT><<<dim3(p.tiles_o), 64 * kFewWaves, 0, s>>>(a);
-  } else {
-    const int jobs = p.tiles_m * p.tiles_o * p.splits, grid = (jobs + 7) / 8 * 8;
-    if (p.kind == 1) tile_product8_kernel<OUT, 4, 4><<<dim3(grid), 256, 0, s>>>(a);
-    else if (p.kind == 2) tile_product8_kernel<OUT, 2, 2><<<dim3(grid), 256, 0, s>>>(a);
-    else tile_product8_kernel<OUT, 2, 1><<<dim3(grid), 256, 0, s>>>(a);
-  }
+  if (p.kind == 0) few_rows8_kernel<OUT><<<dim3(p.tiles_o), 64 * kFewWaves, 0, s>>>(a);
+  else if (a.tiled) launch_tiles<OUT, true>(a, p, s);
+  else launch_tiles<OUT, false>(a, p, s);
   return hipGetLastError();
 }
 
@@ -573,24 +601,33 @@ hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* c
   return hipGetLastError();
 }
 
-hipError_t launch_quantize_rows8(const uint16_t* x, long ld_x, int n_rows, int d, const uint16_t* norm_scale, float norm_eps,
-                                 uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s) {
+namespace {
+
+template <typename T, bool TILED>
+hipError_t launch_rows(const uint16_t* x, long ld_x, int n_rows, int d, const uint16_t* norm_scale, float norm_eps, uint8_t* codes,
+                       uint8_t* scales, hipStream_t s) {
   constexpr int kAtMost = 1 << 19;               // rows of one launch: 32768 workgroups along a side, or as many of 512 lanes
   const int pitch = pitch8(d), spitch = scale_pitch8(d);
   for (int row = 0; row < n_rows; row += kAtMost) {
     const int n = n_rows - row < kAtMost ? n_rows - row : kAtMost;
     const uint16_t* const from = x + row * ld_x;
-    uint8_t* const to = codes + static_cast<size_t>(row) * pitch;
+    uint8_t* const to = codes + static_cast<size_t>(row) * (TILED ? (pitch + 63) / 64 * 64 : pitch);       // (a multiple of 16 rows)
     uint8_t* const to_s = scales + static_cast<size_t>(row) * spitch;
-    const dim3 grid((d + 511) / 512, (n + 15) / 16);
-    if (norm_eps >= 0.f) {
-      if (bf16) quantize_normed_rows8_kernel<BF16><<<n, 512, 0, s>>>(from, ld_x, n, d, norm_scale, norm_eps, to, to_s);
-      else quantize_normed_rows8_kernel<F16><<<n, 512, 0, s>>>(from, ld_x, n, d, norm_scale, norm_eps, to, to_s);
-    } else if (bf16) quantize_rows8_kernel<BF16><<<grid, 256, 0, s>>>(from, ld_x, n, d, to, to_s);
-    else quantize_rows8_kernel<F16><<<grid, 256, 0, s>>>(from, ld_x, n, d, to, to_s);
+    if (norm_eps >= 0.f) quantize_normed_rows8_kernel<T, TILED><<<n, 512, 0, s>>>(from, ld_x, n, d, norm_scale, norm_eps, to, to_s);
+    else quantize_rows8_kernel<T, TILED><<<dim3((d + 511) / 512, (n + 15) / 16), 256, 0, s>>>(from, ld_x, n, d, to, to_s);
     if (hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_quantize_rows8(const uint16_t* x, long ld_x, int n_rows, int d, const uint16_t* norm_scale, float norm_eps,
+                                 uint8_t* codes, uint8_t* scales, bool tiled, bool bf16, hipStream_t s) {
+  if (tiled) return bf16 ? launch_rows<BF16, true>(x, ld_x, n_rows, d, norm_scale, norm_eps, codes, scales, s)
+                         : launch_rows<F16, true>(x, ld_x, n_rows, d, norm_scale, norm_eps, codes, scales, s);
+  return bf16 ? launch_rows<BF16, false>(x, ld_x, n_rows, d, norm_scale, norm_eps, codes, scales, s)
+              : launch_rows<F16, false>(x, ld_x, n_rows, d, norm_scale, norm_eps, codes, scales, s);
 }
 
 Product8Plan plan_product8(int n_rows, int d_in, int d_out) {

@@ -15,18 +15,21 @@ inline int pitch8(int d) { return (d + 15) / 16 * 16; }
 inline int scale_pitch8(int d) { return ((d + 127) / 128 + 3) / 4 * 4; }
 
 constexpr int kWidthMax8 = 1 << 20;    // channels summed over: a panel of 256 rows stays below 2^28 bytes
-constexpr int kOutMax8 = 1 << 24;      // rows of a weight
+constexpr int kOutMax8 = (1 << 21) - 16;    // rows of a weight, values between rows of y: 256 rows of y stay below 2^31 bytes
 constexpr int kRowsMax8 = 1 << 24;
 
 hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s);
-// norm_scale nullable; norm_eps < 0: no norm
+// norm_scale nullable; norm_eps < 0: no norm; tiled: pieces of 16 rows x 64 codes, for launch_product8 only
 hipError_t launch_quantize_rows8(const uint16_t* x, long ld_x, int n_rows, int d, const uint16_t* norm_scale, float norm_eps,
-                                 uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s);
+                                 uint8_t* codes, uint8_t* scales, bool tiled, bool bf16, hipStream_t s);
+// bytes of the codes of n_rows rows, tiled
+inline size_t tiled_bytes8(int n_rows, int d) { return (static_cast<size_t>(n_rows) + 15) / 16 * 16 * ((pitch8(d) + 63) / 64 * 64); }
 
 // y[m, o] = sum_i x[m, i] w[o, i]
 enum : int { kOutF16 = 0, kOutBF16 = 1, kOutF32 = 2 };
 struct Product8Args {
   Held8 x, w;
+  bool tiled;                 // x's codes (never where plan_product8 says kind 0)
   void* y;                    // [n_rows, ld_y]
   long ld_y;
   int n_rows, d_in, d_out;

@@ -52,7 +52,7 @@ struct Carver {
 
 struct RowsSpace { size_t codes, scales; };
 RowsSpace take_rows(Carver& c, int n_rows, int d) {
-  const size_t codes = c.take(static_cast<size_t>(n_rows) * pitch8(d));
+  const size_t codes = c.take(tiled_bytes8(n_rows, d));
   return {codes, c.take(static_cast<size_t>(n_rows) * scale_pitch8(d))};
 }
 
@@ -122,7 +122,7 @@ ScoreSpace score_space(int n_rows, int d_in, int n_vocab, int n_top) {
   s.at_once = score_rows(n_rows, n_vocab);
   s.ld = static_cast<long>(round_up(n_vocab, 16));
   const int tail = n_rows % s.at_once;
-  s.rows = take_rows(c, n_rows, d_in);
+  s.rows = take_rows(c, s.at_once, d_in);
   size_t partial = plan_product8(s.at_once, d_in, n_vocab).partial_floats;
   size_t probs = logprobs_space(plan_logprobs(s.at_once, n_vocab, n_top, kLogitsF32), s.at_once);
   if (tail) {                                    // the last part may be divided otherwise
@@ -174,7 +174,7 @@ int larosa_quantize_rows8(const void* x, int ld_x, int n_rows, int d, const void
   if (int rc = check_width(d)) return rc;
   if (int rc = check_rows(x, ld_x, n_rows, d, rms)) return rc;
   return status_of(launch_quantize_rows8(static_cast<const uint16_t*>(x), ld_x, n_rows, d, static_cast<const uint16_t*>(rms), rms_eps,
-                                         static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), t == LAROSA_BF16,
+                                         static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), false, t == LAROSA_BF16,
                                          stream_of(stream)));
 }
 
@@ -191,6 +191,7 @@ int larosa_product8(const void* w_codes, const void* w_scales, const void* x_cod
   if (int rc = check_held(w_codes, w_scales)) return rc;
   if (int rc = check_held(x_codes, x_scales)) return rc;
   if (int rc = check_product(n_rows, d_in, d_out)) return rc;
+  if (ld_y > kOutMax8) return LAROSA_EUNSUPPORTED;
   if (!ws || !aligned(ws, 256) || ws_bytes < larosa_product8_workspace_bytes(n_rows, d_in, d_out)) return LAROSA_EWORKSPACE;
   const Product8Args a = product_args(w_codes, w_scales, x_codes, x_scales, y, ld_y, n_rows, d_in, d_out,
                                       t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, kCounterBytes);
@@ -211,17 +212,21 @@ int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, in
   if (int rc = check_held(w_codes, w_scales)) return rc;
   if (int rc = check_product(n_rows, d_in, d_out)) return rc;
   if (int rc = check_rows(x, ld_x, n_rows, d_in, rms)) return rc;
+  if (ld_y > kOutMax8) return LAROSA_EUNSUPPORTED;
   if (!ws || !aligned(ws, 256) || ws_bytes < larosa_dense_w8_workspace_bytes(n_rows, d_in, d_out)) return LAROSA_EWORKSPACE;
   Carver c;
   const RowsSpace r = take_rows(c, n_rows, d_in);
   char* const w = static_cast<char*>(ws);
+  const Product8Plan plan = plan_product8(n_rows, d_in, d_out);
+  const bool tiled = plan.kind != 0;
   if (hipError_t e = launch_quantize_rows8(static_cast<const uint16_t*>(x), ld_x, n_rows, d_in, static_cast<const uint16_t*>(rms),
                                            rms_eps, reinterpret_cast<uint8_t*>(w + r.codes), reinterpret_cast<uint8_t*>(w + r.scales),
-                                           t == LAROSA_BF16, stream_of(stream)))
+                                           tiled, t == LAROSA_BF16, stream_of(stream)))
     return status_of(e);
-  const Product8Args a = product_args(w_codes, w_scales, w + r.codes, w + r.scales, y, ld_y, n_rows, d_in, d_out,
-                                      t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, c.at);
-  return status_of(launch_product8(a, plan_product8(n_rows, d_in, d_out), stream_of(stream)));
+  Product8Args a = product_args(w_codes, w_scales, w + r.codes, w + r.scales, y, ld_y, n_rows, d_in, d_out,
+                                t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, c.at);
+  a.tiled = tiled;
+  return status_of(launch_product8(a, plan, stream_of(stream)));
 }
 
 size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, larosa_dtype t) {
@@ -268,15 +273,16 @@ int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, in
   const hipStream_t s = stream_of(stream);
   uint8_t* const codes = reinterpret_cast<uint8_t*>(w + sp.rows.codes);
   uint8_t* const scales = reinterpret_cast<uint8_t*>(w + sp.rows.scales);
-  if (hipError_t e = launch_quantize_rows8(static_cast<const uint16_t*>(x), ld_x, n_rows, d_in, static_cast<const uint16_t*>(rms),
-                                           rms_eps, codes, scales, t == LAROSA_BF16, s))
-    return status_of(e);
   for (int row = 0; row < n_rows; row += sp.at_once) {
     const int n = n_rows - row < sp.at_once ? n_rows - row : sp.at_once;
-    const Product8Args a = product_args(w_codes, w_scales, codes + static_cast<size_t>(row) * pitch8(d_in),
-                                        scales + static_cast<size_t>(row) * scale_pitch8(d_in), w + sp.logits, sp.ld, n, d_in, n_vocab,
-                                        kOutF32, ws, sp.partial);
-    if (hipError_t e = launch_product8(a, plan_product8(n, d_in, n_vocab), s)) return status_of(e);
+    const Product8Plan plan = plan_product8(n, d_in, n_vocab);
+    const bool tiled = plan.kind != 0;
+    if (hipError_t e = launch_quantize_rows8(static_cast<const uint16_t*>(x) + static_cast<long>(row) * ld_x, ld_x, n, d_in,
+                                             static_cast<const uint16_t*>(rms), rms_eps, codes, scales, tiled, t == LAROSA_BF16, s))
+      return status_of(e);
+    Product8Args a = product_args(w_codes, w_scales, codes, scales, w + sp.logits, sp.ld, n, d_in, n_vocab, kOutF32, ws, sp.partial);
+    a.tiled = tiled;
+    if (hipError_t e = launch_product8(a, plan, s)) return status_of(e);
     LogprobsArgs b{};
     b.logits = w + sp.logits;
     b.ld = sp.ld;
