@@ -499,12 +499,17 @@ __global__ __launch_bounds__(128 * WT, MO * MT == 16 ? 1 : 2) void tile_product8
 }
 
 // ---- the product, few rows: HBM-bound, one pass over the weight --------------------------------------------
-// A workgroup of 8 waves owns 16 output channels: their codes are one contiguous run of 16 pitch bytes where the weight is dense.  The
-// waves share the blocks of 128 (block b goes to wave b % 8); a lane takes 32 codes of one channel and of one row of x, turns both into
+// A workgroup of 8 waves owns 16 STRIPS output channels, whose codes are one contiguous run where the weight is dense.  The waves
+// share the blocks of 128 (block b goes to wave b % 8); a lane takes 32 codes of one channel of each strip and of one row of x, turns both into
 // bf16 with their scales (exact: four significant bits times a power of two) and multiplies them by v_mfma_f32_16x16x32_bf16, whose
 // sums are fp32 throughout: the matrix cores idle here anyway, and no bits are lost between neighbours.
+//  * A wave's next codes are on their way while it multiplies (8 KiB of the weight a wave, 128 KiB a compute unit).
+//  * The rows' codes serve STRIPS strips.
+//  * X = F16, BF16: x itself where its codes are few (kShortRows / STRIPS bytes); the waves bring it to 8 bits together, into LDS, while their first codes
+//    of the weight are on the way: one launch, not two.
 constexpr int kFewRows = 16;
 constexpr int kFewWaves = 8;
+struct Held {};                        // rows that are in 8 bits already
 
 __device__ __forceinline__ void bf16_of_codes(const u32x4& lo, const u32x4& hi, float unit, bfloat8 (&out)[4]) {
 #pragma unroll
@@ -516,63 +521,116 @@ __device__ __forceinline__ void bf16_of_codes(const u32x4& lo, const u32x4& hi, 
   }
 }
 
-template <typename OUT>
+template <typename OUT, typename X, int STRIPS>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void few_rows8_kernel(Product8Args a) {
-  __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16][16 + 4];
+  constexpr bool kHeld = std::is_same<X, Held>::value;
+  constexpr int kAtOnce = 4 / STRIPS;            // blocks of a turn
+  constexpr int kTurn = kFewWaves * kAtOnce;
+  constexpr int kCols = 16 * STRIPS;
+  __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16][kCols + 4];
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kHeld ? 16 : kShortRows / STRIPS + 16 * 16];
+  __shared__ uint8_t scales[kHeld ? 16 : kShortRows / STRIPS / 128];
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
   const int pitch = (a.d_in + 15) / 16 * 16, blocks = (a.d_in + 127) / 128, spitch = (blocks + 3) / 4 * 4;
-  const int o0 = blockIdx.x * 16, r = lane & 15, q = lane >> 4;
-  const int rows_o = min(16, a.d_out - o0);
+  const int o0 = blockIdx.x * kCols, r = lane & 15, q = lane >> 4;
+  const int rows_o = min(kCols, a.d_out - o0);
   const __amdgpu_buffer_rsrc_t buf_o = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<uint8_t*>(a.w.codes) + static_cast<size_t>(o0) * pitch, 0, rows_o * pitch, 0x00027000);
-  const __amdgpu_buffer_rsrc_t buf_t = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x.codes), 0, a.n_rows * pitch, 0x00027000);
-  const __amdgpu_buffer_rsrc_t buf_s = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x.scales), 0, a.n_rows * spitch, 0x00027000);
+  const __amdgpu_buffer_rsrc_t buf_t = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x.codes), 0, kHeld ? a.n_rows * pitch : 0, 0x00027000);
+  const __amdgpu_buffer_rsrc_t buf_s = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x.scales), 0, kHeld ? a.n_rows * spitch : 0, 0x00027000);
   const uint8_t* const w_scales = a.w.scales + static_cast<size_t>(o0 / 128) * spitch;
-  const int base = r * pitch + 32 * q;
-  float4v acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int kAtOnce = 4;
-  for (int b0 = w; b0 < blocks; b0 += kFewWaves * kAtOnce) {
-    u32x4 wc[kAtOnce][2], xc[kAtOnce][2];
-    uint32_t xs[kAtOnce], ws[kAtOnce];
+
+  // a lane's codes of a block: 16 from 16 q on and 16 from 64 + 16 q on, of channel r of each strip and of row r.  Pieces behind the end of a
+  // row are asked for at an offset outside the buffer.
+  u32x4 wc[kAtOnce][STRIPS][2], xc[kAtOnce][2];
+  uint32_t ws[kAtOnce], xs[kAtOnce];
+  auto load = [&](int b0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      const int b = b0 + u * kFewWaves, k = b * 128 + 32 * q;
-      // pieces behind the row's end are the next row's (or outside the buffer): they are asked for at an offset outside
-      const uint32_t at = static_cast<uint32_t>(base + b * 128);
-      const uint32_t at0 = k < pitch ? at : kOutside, at1 = k + 16 < pitch ? at + 16 : kOutside;
-      wc[u][0] = __builtin_amdgcn_raw_buffer_load_b128(buf_o, at0, 0, 2);
-      wc[u][1] = __builtin_amdgcn_raw_buffer_load_b128(buf_o, at1, 0, 2);
-      xc[u][0] = __builtin_amdgcn_raw_buffer_load_b128(buf_t, at0, 0, 0);
-      xc[u][1] = __builtin_amdgcn_raw_buffer_load_b128(buf_t, at1, 0, 0);
-      xs[u] = __builtin_amdgcn_raw_buffer_load_b8(buf_s, b < blocks ? static_cast<uint32_t>(r * spitch + b) : kOutside, 0, 0);
+      const int b = b0 + u * kFewWaves, k = b * 128 + 16 * q;
+#pragma unroll
+      for (int i = 0; i < STRIPS; ++i) {
+        const uint32_t at = static_cast<uint32_t>((16 * i + r) * pitch + k);
+        wc[u][i][0] = __builtin_amdgcn_raw_buffer_load_b128(buf_o, k < pitch ? at : kOutside, 0, 2);
+        wc[u][i][1] = __builtin_amdgcn_raw_buffer_load_b128(buf_o, k + 64 < pitch ? at + 64 : kOutside, 0, 2);
+      }
       ws[u] = w_scales[min(b, blocks - 1)];
+      if constexpr (kHeld) {
+        const uint32_t at = static_cast<uint32_t>(r * pitch + k);
+        xc[u][0] = __builtin_amdgcn_raw_buffer_load_b128(buf_t, k < pitch ? at : kOutside, 0, 0);
+        xc[u][1] = __builtin_amdgcn_raw_buffer_load_b128(buf_t, k + 64 < pitch ? at + 64 : kOutside, 0, 0);
+        xs[u] = __builtin_amdgcn_raw_buffer_load_b8(buf_s, b < blocks ? static_cast<uint32_t>(r * spitch + b) : kOutside, 0, 0);
+      }
     }
+  };
+  load(w);
+  const int stride = blocks * 128 + 16;          // of a row's codes in LDS: 16 more, so that the rows of a column lie in different banks
+  if constexpr (!kHeld) {
+    // 16 lanes to 128 values
+    const int all = a.n_rows * blocks;
+    for (int i = threadIdx.x / 16; i < all; i += 4 * kFewWaves) {
+      const int row = i / blocks, b = i - row * blocks, c = b * 128 + 8 * r;
+      float v[8];
+      unpack8<X>(c < a.d_in ? *reinterpret_cast<const uint4*>(a.x16 + row * a.ld_x + c) : make_uint4(0, 0, 0, 0), v);
+      uint32_t byte;
+      *reinterpret_cast<uint2*>(codes + row * stride + c) = block_codes(v, byte);
+      if (r == 0) scales[i] = static_cast<uint8_t>(byte);
+    }
+    __syncthreads();
+  }
+
+  float4v acc[STRIPS];
+#pragma unroll
+  for (int i = 0; i < STRIPS; ++i) acc[i] = float4v{0.f, 0.f, 0.f, 0.f};
+  for (int b0 = w; b0 < blocks; b0 += kTurn) {
+    bfloat8 xv[kAtOnce][4], wv[kAtOnce][STRIPS][4];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      bfloat8 wv[4], xv[4];
-      bf16_of_codes(wc[u][0], wc[u][1], __uint_as_float(ws[u] << 23), wv);
-      bf16_of_codes(xc[u][0], xc[u][1], __uint_as_float(xs[u] << 23), xv);
+      if constexpr (!kHeld) {
+        // (behind the last block the weight is 0; the block again keeps out what lies there; rows behind the last are row 0 again)
+        const int b = min(b0 + u * kFewWaves, blocks - 1), row = r < a.n_rows ? r : 0;
+        xc[u][0] = *reinterpret_cast<const u32x4*>(codes + row * stride + b * 128 + 16 * q);
+        xc[u][1] = *reinterpret_cast<const u32x4*>(codes + row * stride + b * 128 + 64 + 16 * q);
+        xs[u] = scales[row * blocks + b];
+      }
+      bf16_of_codes(xc[u][0], xc[u][1], __uint_as_float(xs[u] << 23), xv[u]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[j], xv[j], acc, 0, 0, 0);
+      for (int i = 0; i < STRIPS; ++i) bf16_of_codes(wc[u][i][0], wc[u][i][1], __uint_as_float(ws[u] << 23), wv[u][i]);
     }
+    load(b0 + kTurn);                            // (behind the last block: nothing is read)
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < STRIPS; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][i][j], xv[u][j], acc[i], 0, 0, 0);
   }
-  // lane (q, r): channels 4 q .. + 3 of row r
-  *reinterpret_cast<float4*>(&sums[w][r][4 * q]) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+  // lane (q, r): channels 4 q .. + 3 of each strip, row r
+#pragma unroll
+  for (int i = 0; i < STRIPS; ++i) *reinterpret_cast<float4*>(&sums[w][r][16 * i + 4 * q]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
   __syncthreads();
-  if (threadIdx.x < 64) {
+  if (threadIdx.x < 64 * STRIPS) {
+    const int row = threadIdx.x / (4 * STRIPS), col = threadIdx.x % (4 * STRIPS) * 4;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < kFewWaves; ++k) {
-      const float4 s = *reinterpret_cast<const float4*>(&sums[k][r][4 * q]);
+      const float4 s = *reinterpret_cast<const float4*>(&sums[k][row][col]);
       v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
     }
-    const int o = o0 + 4 * q;
-    if (r < a.n_rows && o < a.d_out) {
-      if constexpr (std::is_same<OUT, F32>::value) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + r * a.ld_y + o) = make_float4(v[0], v[1], v[2], v[3]);
-      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + r * a.ld_y + o) = pack_out4(OUT{}, v);
+    const int o = o0 + col;
+    if (row < a.n_rows && o < a.d_out) {
+      if constexpr (std::is_same<OUT, F32>::value) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + row * a.ld_y + o) = make_float4(v[0], v[1], v[2], v[3]);
+      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + row * a.ld_y + o) = pack_out4(OUT{}, v);
     }
   }
+}
+
+template <typename OUT, typename X>
+void launch_few(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
+  const dim3 grid(p.tiles_o);
+  if (p.strips == 4) few_rows8_kernel<OUT, X, 4><<<grid, 64 * kFewWaves, 0, s>>>(a);
+  else few_rows8_kernel<OUT, X, 1><<<grid, 64 * kFewWaves, 0, s>>>(a);
 }
 
 template <typename OUT, bool TILED>
@@ -586,7 +644,9 @@ void launch_tiles(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
 
 template <typename OUT>
 hipError_t launch_out(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
-  if (p.kind == 0) few_rows8_kernel<OUT><<<dim3(p.tiles_o), 64 * kFewWaves, 0, s>>>(a);
+  if (p.kind == 0 && !a.x16) launch_few<OUT, Held>(a, p, s);
+  else if (p.kind == 0 && a.x_bf16) launch_few<OUT, BF16>(a, p, s);
+  else if (p.kind == 0) launch_few<OUT, F16>(a, p, s);
   else if (a.tiled) launch_tiles<OUT, true>(a, p, s);
   else launch_tiles<OUT, false>(a, p, s);
   return hipGetLastError();
@@ -638,7 +698,10 @@ Product8Plan plan_product8(int n_rows, int d_in, int d_out) {
   if (n_rows <= kFewRows) {
     p.kind = 0;
     p.tiles_m = 1;
-    p.tiles_o = (d_out + 15) / 16;
+    // Four strips a workgroup where that leaves one for each compute unit, or, where the rows' share counts, most of them.  Both sides in us:
+    // 4096 x 28672, 1 row 30.4 (one strip: 32.3), 16 rows 33 (49); 4096 x 11008, 1 row 16.7 (15.2), 16 rows 19 (23); 4096 x 4096, 1 row 13.5 (7.1).
+    p.strips = d_out >= 64 * (n_rows > 2 ? 160 : 256) ? 4 : 1;
+    p.tiles_o = (d_out + 16 * p.strips - 1) / (16 * p.strips);
     return p;
   }
   const long big = static_cast<long>((n_rows + 255) / 256) * ((d_out + 255) / 256);

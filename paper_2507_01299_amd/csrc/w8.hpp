@@ -17,6 +17,9 @@ inline int scale_pitch8(int d) { return ((d + 127) / 128 + 3) / 4 * 4; }
 constexpr int kWidthMax8 = 1 << 20;    // channels summed over: a panel of 256 rows stays below 2^28 bytes
 constexpr int kOutMax8 = (1 << 21) - 16;    // rows of a weight, values between rows of y: 256 rows of y stay below 2^31 bytes
 constexpr int kRowsMax8 = 1 << 24;
+// Bytes of rows' codes, times strips, that the product of few rows makes for itself.  Both sides in us: 4 x 4096 x 4096 8.7 (two launches 10.5), but
+// with four strips, whose workgroups are many, 4 x 4096 x 128256 120 (112).
+constexpr int kShortRows = 16384;
 
 hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s);
 // norm_scale nullable; norm_eps < 0: no norm; tiled: pieces of 16 rows x 64 codes, for launch_product8 only
@@ -30,6 +33,9 @@ enum : int { kOutF16 = 0, kOutBF16 = 1, kOutF32 = 2 };
 struct Product8Args {
   Held8 x, w;
   bool tiled;                 // x's codes (never where plan_product8 says kind 0)
+  const uint16_t* x16;        // kind 0: x itself [n_rows, ld_x] instead of its codes, or nullptr; only where takes_rows16 says so
+  long ld_x;
+  bool x_bf16;
   void* y;                    // [n_rows, ld_y]
   long ld_y;
   int n_rows, d_in, d_out;
@@ -41,11 +47,15 @@ struct Product8Args {
   unsigned* counters;         // [tiles], kCounterStride apart, zero on entry and on exit
 };
 struct Product8Plan {
-  int kind;                   // which kernel
+  int kind;                   // which kernel (0: up to 16 rows)
+  int strips;                 // kind 0: of 16 output channels a workgroup
   int tiles_m, tiles_o, splits, blocks_per;
   size_t partial_floats;
 };
 Product8Plan plan_product8(int n_rows, int d_in, int d_out);
+inline bool takes_rows16(const Product8Plan& p, int n_rows, int d_in) {
+  return p.kind == 0 && n_rows * ((d_in + 127) / 128) * p.strips <= kShortRows / 128;
+}
 hipError_t launch_product8(const Product8Args& a, const Product8Plan& p, hipStream_t s);
 
 // Log probabilities of logits [n_rows, ld], the first n_vocab of a row.

@@ -32,6 +32,24 @@ int check_rows(const void* x, int ld_x, int n_rows, int d, const void* rms) {
   return n_rows > kRowsMax8 ? LAROSA_EUNSUPPORTED : LAROSA_OK;
 }
 
+// A product of n rows of x: the rows to 8 bits at `codes` and `scales`, unless the product takes them as they are, then the product.
+int run_product(Product8Args a, const void* x, int ld_x, const void* rms, float rms_eps, larosa_dtype t, uint8_t* codes,
+                uint8_t* scales, hipStream_t s) {
+  const Product8Plan plan = plan_product8(a.n_rows, a.d_in, a.d_out);
+  const uint16_t* const rows = static_cast<const uint16_t*>(x);
+  if (rms_eps < 0.f && takes_rows16(plan, a.n_rows, a.d_in)) {
+    a.x16 = rows;
+    a.ld_x = ld_x;
+    a.x_bf16 = t == LAROSA_BF16;
+  } else {
+    a.tiled = plan.kind != 0;
+    if (hipError_t e = launch_quantize_rows8(rows, ld_x, a.n_rows, a.d_in, static_cast<const uint16_t*>(rms), rms_eps, codes, scales, a.tiled,
+                                             t == LAROSA_BF16, s))
+      return status_of(e);
+  }
+  return status_of(launch_product8(a, plan, s));
+}
+
 // Sizes of a product; d_out need not be a multiple of 8 here.
 int check_product(int n_rows, int d_in, int d_out) {
   if (n_rows < 1 || d_out < 1) return LAROSA_EINVAL;
@@ -217,16 +235,10 @@ int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, in
   Carver c;
   const RowsSpace r = take_rows(c, n_rows, d_in);
   char* const w = static_cast<char*>(ws);
-  const Product8Plan plan = plan_product8(n_rows, d_in, d_out);
-  const bool tiled = plan.kind != 0;
-  if (hipError_t e = launch_quantize_rows8(static_cast<const uint16_t*>(x), ld_x, n_rows, d_in, static_cast<const uint16_t*>(rms),
-                                           rms_eps, reinterpret_cast<uint8_t*>(w + r.codes), reinterpret_cast<uint8_t*>(w + r.scales),
-                                           tiled, t == LAROSA_BF16, stream_of(stream)))
-    return status_of(e);
-  Product8Args a = product_args(w_codes, w_scales, w + r.codes, w + r.scales, y, ld_y, n_rows, d_in, d_out,
-                                t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, c.at);
-  a.tiled = tiled;
-  return status_of(launch_product8(a, plan, stream_of(stream)));
+  const Product8Args a = product_args(w_codes, w_scales, w + r.codes, w + r.scales, y, ld_y, n_rows, d_in, d_out,
+                                      t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, c.at);
+  return run_product(a, x, ld_x, rms, rms_eps, t, reinterpret_cast<uint8_t*>(w + r.codes), reinterpret_cast<uint8_t*>(w + r.scales),
+                     stream_of(stream));
 }
 
 size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, larosa_dtype t) {
@@ -275,14 +287,8 @@ int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, in
   uint8_t* const scales = reinterpret_cast<uint8_t*>(w + sp.rows.scales);
   for (int row = 0; row < n_rows; row += sp.at_once) {
     const int n = n_rows - row < sp.at_once ? n_rows - row : sp.at_once;
-    const Product8Plan plan = plan_product8(n, d_in, n_vocab);
-    const bool tiled = plan.kind != 0;
-    if (hipError_t e = launch_quantize_rows8(static_cast<const uint16_t*>(x) + static_cast<long>(row) * ld_x, ld_x, n, d_in,
-                                             static_cast<const uint16_t*>(rms), rms_eps, codes, scales, tiled, t == LAROSA_BF16, s))
-      return status_of(e);
-    Product8Args a = product_args(w_codes, w_scales, codes, scales, w + sp.logits, sp.ld, n, d_in, n_vocab, kOutF32, ws, sp.partial);
-    a.tiled = tiled;
-    if (hipError_t e = launch_product8(a, plan, s)) return status_of(e);
+    const Product8Args a = product_args(w_codes, w_scales, codes, scales, w + sp.logits, sp.ld, n, d_in, n_vocab, kOutF32, ws, sp.partial);
+    if (int rc = run_product(a, static_cast<const uint16_t*>(x) + static_cast<long>(row) * ld_x, ld_x, rms, rms_eps, t, codes, scales, s)) return rc;
     LogprobsArgs b{};
     b.logits = w + sp.logits;
     b.ld = sp.ld;

@@ -123,6 +123,7 @@ def test_weight_bit_for_bit(api, dtype, d_in, d_out):
 CUT = 2.0 ** -10
 SHAPES = [
     (1, 8, 8), (1, 128, 16), (2, 136, 24), (5, 4104, 136), (15, 512, 264), (16, 1032, 520), (16, 24, 1000),          # few rows
+    (3, 136, 10264), (16, 520, 10248), (1, 264, 16392), (9, 1160, 16416),                                              # of a wide weight
     (17, 8, 8), (17, 136, 24), (33, 1032, 264), (64, 4104, 136), (64, 512, 1160),                                    # tiles of 64 rows
     (65, 16, 8), (65, 520, 264), (100, 4104, 392), (129, 128, 136), (257, 1000, 520), (300, 2056, 1032),             # of 128
     (1100, 136, 9992), (3001, 648, 4104),                                                                            # of 256
@@ -216,6 +217,26 @@ def test_codes_of_others_with_extreme_scales(api, n):
     want, most = Q.product(wc.numpy(), ws.numpy(), xc.numpy(), xs.numpy(), d_in)
     sums = (d_in + 8) * 2.0 ** -24 + (0 if n <= 16 else CUT)
     assert np.all(np.abs(exact(y) - want) <= sums * most + STEP["bf16"] * (np.abs(want) + sums * most))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,d_in,d_out", [(1, 8, 8), (1, 4104, 136), (3, 136, 24), (4, 4096, 264), (5, 4096, 264), (16, 1024, 40), (16, 1032, 40),
+                                          (1, 16384, 16), (1, 16392, 16), (1, 264, 16392), (1, 4096, 16392), (2, 4096, 16392), (4, 1000, 10264),
+                                          (9, 136, 10264), (40, 264, 136), (130, 520, 264)])
+def test_dense_is_its_parts(api, dtype, n, d_in, d_out):
+    """Short rows are brought to 8 bits by the product itself, others before it: the same bits.  Rows lie apart, and one holds a NaN."""
+    print(f"dense {dtype} {n}x{d_in}x{d_out}", flush=True)
+    g = torch.Generator().manual_seed(n + d_in + d_out)
+    x = torch.full((n, d_in + 24), float("nan"), dtype=TYPE[dtype], device="cuda")
+    x[:, :d_in] = (torch.randn(n, d_in, generator=g) * 2.0 ** torch.randint(-4, 5, (n, 1), generator=g)).to(TYPE[dtype])
+    x[n // 2, d_in - 1] = float("nan")
+    wc, ws = api.quantize_w8((torch.randn(d_in, d_out, generator=g) * 0.05).to(TYPE[dtype]).cuda(), dtype)
+    y, z = (torch.full((n, d_out + 8), 7.0, dtype=TYPE[dtype], device="cuda") for _ in range(2))
+    api.dense_w8(wc, ws, x[:, :d_in], y[:, :d_out], dtype, api.dense_w8_workspace(n, d_in, d_out))
+    xc, xs = api.quantize_rows8(x[:, :d_in], dtype)
+    api.product8(wc, ws, xc, xs, d_in, z[:, :d_out], dtype, api.product8_workspace(n, d_in, d_out))
+    assert torch.equal(y.view(torch.int16), z.view(torch.int16)) and bool((y[:, d_out:] == 7).all())
+    assert bool(y[n // 2, :d_out].isnan().all()) and int(y.isnan().sum()) == d_out
 
 
 def test_dense_behind_a_norm_is_its_parts(api):
