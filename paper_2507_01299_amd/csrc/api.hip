@@ -989,6 +989,10 @@ int larosa_set_tuning(int key, int value) {
       if (value < 0 || value > 2) return LAROSA_EINVAL;
       tuning().contraction_tiles = value;
       return LAROSA_OK;
+    case 11:
+      if (value < 0 || value > 5) return LAROSA_EINVAL;
+      tuning().product8_tiles = value;
+      return LAROSA_OK;
     default:
       return LAROSA_EINVAL;
   }

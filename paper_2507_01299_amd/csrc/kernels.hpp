@@ -53,6 +53,7 @@ struct Tuning {
   int side_g = 0;             // workgroups of that adapter; 0 = by size (both jobs resident at once: at most 512 slots)
   int hinted = 1;             // decoder layer: 1 = the down projection takes its threshold from histograms that the gate|up launch builds
   int contraction_tiles = 0;  // offline contractions: 0 = workgroup tiles by size, 1 = 128 x 128, 2 = 256 x 256
+  int product8_tiles = 0;     // products over 8-bit weights: 0 = by size, 1 .. 5 = one of the tiles
 };
 Tuning& tuning();
 

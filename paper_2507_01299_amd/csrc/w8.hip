@@ -283,7 +283,7 @@ __device__ __forceinline__ uint2 pack_out4(BF16, const float (&v)[4]) {
 struct F32 {};                // logits that the caller's next step reads in full
 
 template <typename OUT, bool TILED, int MO, int MT, int WT, int kStages>
-__global__ __launch_bounds__(128 * WT, MO * MT == 16 ? 1 : 2) void tile_product8_kernel(Product8Args a) {
+__global__ __launch_bounds__(128 * WT, MO * MT >= 8 ? 1 : 2) void tile_product8_kernel(Product8Args a) {
   constexpr int kWaves = 2 * WT;
   constexpr int TO = 64 * MO, TT = 32 * WT * MT;
   constexpr int kBytesO = TO * kKTile8, kBytesT = TT * kKTile8, kStageBytes = kBytesO + kBytesT;
@@ -490,7 +490,7 @@ __global__ __launch_bounds__(128 * WT, MO * MT == 16 ? 1 : 2) void tile_product8
       u32x4* const to = reinterpret_cast<u32x4*>(static_cast<char*>(a.y) + (row * a.ld_y + ow + c) * kSize);
       if (row < a.n_rows && ow + c < a.d_out) {
         // many tiles: y is larger than the L2 and would drive the operands out of it (4096 x 4096 x 28672: 458 -> 438 us)
-        if constexpr (MO * MT == 16 && !kWide) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), to);
+        if constexpr (MO * MT >= 12 && !kWide) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), to);
         else *to = __builtin_bit_cast(u32x4, v);
       }
     }
@@ -638,7 +638,9 @@ void launch_tiles(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
   const int jobs = p.tiles_m * p.tiles_o * p.splits;
   const dim3 grid((jobs + 7) / 8 * 8);
   if (p.kind == 1) tile_product8_kernel<OUT, TILED, 4, 4, 2, 4><<<grid, 256, 0, s>>>(a);
-  else if (p.kind == 2) tile_product8_kernel<OUT, TILED, 2, 2, 2, 4><<<grid, 256, 0, s>>>(a);
+  else if (p.kind == 2) tile_product8_kernel<OUT, TILED, 4, 3, 2, 4><<<grid, 256, 0, s>>>(a);
+  else if (p.kind == 3) tile_product8_kernel<OUT, TILED, 2, 4, 2, 6><<<grid, 256, 0, s>>>(a);
+  else if (p.kind == 4) tile_product8_kernel<OUT, TILED, 2, 2, 2, 4><<<grid, 256, 0, s>>>(a);
   else tile_product8_kernel<OUT, TILED, 2, 1, 2, 4><<<grid, 256, 0, s>>>(a);
 }
 
@@ -690,6 +692,22 @@ hipError_t launch_quantize_rows8(const uint16_t* x, long ld_x, int n_rows, int d
               : launch_rows<F16, false>(x, ld_x, n_rows, d, norm_scale, norm_eps, codes, scales, s);
 }
 
+// Tiles of the product, kinds 1 .. 5: output channels and rows, workgroups of it that a compute unit holds, and microseconds that a block of 128
+// takes a compute unit with one of them and, with several, each.  Measured over nine weights (4096 x 4096 .. 8192 x 57344, 4096 x 128256) and 19
+// numbers of rows from 17 to 4096, each kind with 1 .. 16 parts: what the estimate below picks is within 0.3 % of the best of them on the average, and
+// 7 % off at most.  One tile of 256 x 256 wherever there are many, of 128 x 128 else, came to 6 % and 62 % (400 rows of 28672 x 8192: 175 us, 135).
+struct TileKind8 { int o, t, slots; float alone, each; };
+constexpr TileKind8 kTiles8[] = {{256, 256, 1, 1.45f, 1.45f}, {256, 192, 1, 1.2f, 1.2f}, {128, 256, 1, 0.9f, 0.9f}, {128, 128, 2, 0.7f, 0.6f}, {128, 64, 3, 0.6f, 0.6f}};
+constexpr int kPartsMax8 = 16;
+
+// The blocks of a round of workgroups, or the weight's way from memory where that is longer, then the tiles' stores and the joining of parts.
+float time8(const TileKind8& k, long jobs, int parts, int blocks_per, int d_in, int d_out) {
+  const long each = (jobs + 255) / 256, full = each / k.slots, rest = each % k.slots;
+  const float round = k.slots > 1 ? k.slots * k.each : k.alone, last = rest == 0 ? 0.f : rest == 1 ? k.alone : rest * k.each;
+  const float products = blocks_per * (full * round + last), memory = static_cast<float>(d_in) * d_out / 6e6f, size = k.o * k.t / 16384.f;
+  return (products > memory ? products : memory) + 2.5f * size * each + (parts > 1 ? 2.5f + 2.f * size * parts : 0.f);
+}
+
 Product8Plan plan_product8(int n_rows, int d_in, int d_out) {
   Product8Plan p{};
   const int blocks = (d_in + 127) / 128;
@@ -704,21 +722,25 @@ Product8Plan plan_product8(int n_rows, int d_in, int d_out) {
     p.tiles_o = (d_out + 16 * p.strips - 1) / (16 * p.strips);
     return p;
   }
-  const long big = static_cast<long>((n_rows + 255) / 256) * ((d_out + 255) / 256);
-  p.kind = n_rows <= 64 ? 3 : big >= 192 ? 1 : 2;
-  const int to = p.kind == 1 ? 256 : 128, tt = p.kind == 1 ? 256 : p.kind == 2 ? 128 : 64;
-  p.tiles_m = (n_rows + tt - 1) / tt;
-  p.tiles_o = (d_out + to - 1) / to;
-  const long tiles = static_cast<long>(p.tiles_m) * p.tiles_o;
-  if (p.kind != 1 && tiles < 256) {
-    long want = 512 / tiles;
-    if (want > blocks / 4) want = blocks / 4;
-    if (want > 1) {
-      p.blocks_per = (blocks + static_cast<int>(want) - 1) / static_cast<int>(want);
-      p.splits = (blocks + p.blocks_per - 1) / p.blocks_per;
+  const int forced = tuning().product8_tiles;
+  float best = 0.f;
+  for (int kind = 1; kind <= 5; ++kind) {
+    const TileKind8& k = kTiles8[kind - 1];
+    const long tiles_m = (n_rows + k.t - 1L) / k.t, tiles_o = (d_out + k.o - 1L) / k.o, tiles = tiles_m * tiles_o;
+    if (tiles > kTilesMax8 || (forced && kind != forced)) continue;
+    for (int want = 1; want == 1 || (want <= kPartsMax8 && want * 4 <= blocks && tiles * want <= 256 * k.slots); ++want) {
+      const int per = (blocks + want - 1) / want, parts = (blocks + per - 1) / per;
+      const float t = time8(k, tiles * parts, parts, per, d_in, d_out);
+      if (p.kind != 0 && t >= best) continue;
+      best = t;
+      p.kind = kind;
+      p.tiles_m = static_cast<int>(tiles_m);
+      p.tiles_o = static_cast<int>(tiles_o);
+      p.splits = parts;
+      p.blocks_per = per;
+      p.partial_floats = parts > 1 ? static_cast<size_t>(tiles) * parts * k.o * k.t : 0;
     }
   }
-  if (p.splits > 1) p.partial_floats = static_cast<size_t>(tiles) * p.splits * to * tt;
   return p;
 }
 

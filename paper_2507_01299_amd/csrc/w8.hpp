@@ -17,6 +17,7 @@ inline int scale_pitch8(int d) { return ((d + 127) / 128 + 3) / 4 * 4; }
 constexpr int kWidthMax8 = 1 << 20;    // channels summed over: a panel of 256 rows stays below 2^28 bytes
 constexpr int kOutMax8 = (1 << 21) - 16;    // rows of a weight, values between rows of y: 256 rows of y stay below 2^31 bytes
 constexpr int kRowsMax8 = 1 << 24;
+constexpr long kTilesMax8 = 1 << 23;   // of 256 threads each
 // Bytes of rows' codes, times strips, that the product of few rows makes for itself.  Both sides in us: 4 x 4096 x 4096 8.7 (two launches 10.5), but
 // with four strips, whose workgroups are many, 4 x 4096 x 128256 120 (112).
 constexpr int kShortRows = 16384;
@@ -47,7 +48,7 @@ struct Product8Args {
   unsigned* counters;         // [tiles], kCounterStride apart, zero on entry and on exit
 };
 struct Product8Plan {
-  int kind;                   // which kernel (0: up to 16 rows)
+  int kind;                   // which kernel (0: up to 16 rows, else by its tile)
   int strips;                 // kind 0: of 16 output channels a workgroup
   int tiles_m, tiles_o, splits, blocks_per;
   size_t partial_floats;

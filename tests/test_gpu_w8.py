@@ -124,16 +124,18 @@ CUT = 2.0 ** -10
 SHAPES = [
     (1, 8, 8), (1, 128, 16), (2, 136, 24), (5, 4104, 136), (15, 512, 264), (16, 1032, 520), (16, 24, 1000),          # few rows
     (3, 136, 10264), (16, 520, 10248), (1, 264, 16392), (9, 1160, 16416),                                              # of a wide weight
-    (17, 8, 8), (17, 136, 24), (33, 1032, 264), (64, 4104, 136), (64, 512, 1160),                                    # tiles of 64 rows
-    (65, 16, 8), (65, 520, 264), (100, 4104, 392), (129, 128, 136), (257, 1000, 520), (300, 2056, 1032),             # of 128
-    (1100, 136, 9992), (3001, 648, 4104),                                                                            # of 256
+    (17, 8, 8), (17, 136, 24), (33, 1032, 264), (64, 4104, 136), (64, 512, 1160),
+    (65, 16, 8), (65, 520, 264), (100, 4104, 392), (129, 128, 136), (193, 1000, 520), (300, 2056, 1032),
+    (1100, 136, 9992), (1025, 648, 4104), (257, 8200, 264),                                       # whole bands; many parts
 ]
 
 
-def test_the_shapes_take_every_kernel():
-    """By the launch rules: up to 16 rows, up to 64, and from 192 tiles of 256 x 256 on."""
-    kinds = {0 if n <= 16 else 3 if n <= 64 else 1 if -(-n // 256) * -(-o // 256) >= 192 else 2 for n, _, o in SHAPES}
-    assert kinds == {0, 1, 2, 3}
+@pytest.fixture(params=[0, 1, 2, 3, 4, 5])
+def tile(request, api):
+    """The tile by size, or each of them whatever the size."""
+    api.set_tuning(11, request.param)
+    yield request.param
+    api.set_tuning(11, 0)
 
 
 def held(api, x, W, dtype):
@@ -142,10 +144,12 @@ def held(api, x, W, dtype):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,d_in,d_out", SHAPES)
-def test_product_of_small_integers_is_exact(api, dtype, n, d_in, d_out):
+def test_product_of_small_integers_is_exact(api, tile, dtype, n, d_in, d_out):
     """Integers up to 2: codes hold them, products and sums (at most 4 d_in < 2^24) are whole numbers, so only the last rounding is left.  Blocks
     are scaled by powers of two, differently for every row and every block of the weight.  Rows and columns behind y's are left as they were."""
-    print(f"exact product {dtype} {n}x{d_in}x{d_out}", flush=True)
+    if n <= 16 and tile:
+        pytest.skip("tiles are for more rows")
+    print(f"exact product {tile} {dtype} {n}x{d_in}x{d_out}", flush=True)
     g = torch.Generator().manual_seed(n + d_in + d_out)
     x = torch.randint(-2, 3, (n, d_in), generator=g).float() * 2.0 ** torch.randint(-2, 3, (n, 1), generator=g)
     W = torch.randint(-2, 3, (d_in, d_out), generator=g).float()
@@ -167,11 +171,13 @@ def test_product_of_small_integers_is_exact(api, dtype, n, d_in, d_out):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,d_in,d_out", SHAPES)
-def test_product_within_its_bound(api, dtype, n, d_in, d_out):
+def test_product_within_its_bound(api, tile, dtype, n, d_in, d_out):
     """Up to 16 rows sums are fp32: at most (d_in + 8) roundings of 2^-24 of the sum of magnitudes.  Above, see CUT.  Then half a step of the type.
     In the norm: seven cuts in eight products, each below 2^-13 of the largest, whose square is at most the sum of the eight squares, of
     random sign and uniform size: sqrt(7 / 3) 2^-13 < 2^-12 of the products' root sum of squares, which is the result's norm."""
-    print(f"product {dtype} {n}x{d_in}x{d_out}", flush=True)
+    if n <= 16 and tile:
+        pytest.skip("tiles are for more rows")
+    print(f"product {tile} {dtype} {n}x{d_in}x{d_out}", flush=True)
     g = torch.Generator().manual_seed(n * 7 + d_in + d_out)
     strong = torch.where(torch.rand(1, d_in, generator=g) < 0.02, 20.0, 1.0)
     x, W = torch.randn(n, d_in, generator=g) * strong, torch.randn(d_in, d_out, generator=g) * 0.05

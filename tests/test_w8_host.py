@@ -140,3 +140,17 @@ def test_binding_refuses_what_would_be_misread():
                  (given, logp, None, torch.empty(4, 3, dtype=torch.int32), torch.empty(4, 2)), (given, None, None, None, None)):
         with pytest.raises(ValueError):
             api._outputs8(4, *args)
+
+
+def test_tiles_that_there_are():
+    """Each tile's workspace query answers, also where sums go in parts; others are refused."""
+    lib = api.lib()
+    for bad in (-1, 6):
+        assert lib.larosa_set_tuning(11, bad) == EINVAL
+    try:
+        for tile in range(6):
+            assert lib.larosa_set_tuning(11, tile) == api.OK
+            for n, d_in, d_out in ((17, 8, 8), (40, 4096, 264), (333, 11008, 4096), (1 << 14, 4096, 1 << 20)):
+                assert lib.larosa_product8_workspace_bytes(n, d_in, d_out) > 0
+    finally:
+        lib.larosa_set_tuning(11, 0)
