@@ -167,6 +167,9 @@ __global__ __launch_bounds__(512) void quantize_normed_rows8_kernel(const uint16
 // A weight [d_in, d_out] to codes [d_out, d_in], HBM-bound: a workgroup per block of 128 x 128.  A lane holds 8 input x 8 output
 // channels (eight 16-byte loads, 256 bytes of a row together), so that the instruction that makes codes of two values gets neighbours
 // along the input; the codes are turned in LDS and leave as 128 bytes of each output channel.
+// Blocks go to the XCDs in panels, so that lines that two blocks share (where a pitch is no multiple of 128 bytes) meet in one L2: 11016 x 13832
+// 149 us block by block across the XCDs, 129 in one panel, 109, 105, 100, 105 in panels of 1, 2, 4, 8.
+constexpr int kPanel8 = 4;
 constexpr int kTurnPitch = 128 + 8;    // bytes of an output channel in LDS (8-byte writes of 16 lanes fall into different banks)
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_w8_kernel(const uint16_t* __restrict__ W, int d_in, int d_out,
@@ -174,8 +177,15 @@ __global__ __launch_bounds__(256) void quantize_w8_kernel(const uint16_t* __rest
   __shared__ __attribute__((aligned(16))) uint8_t turn[128 * kTurnPitch];
   __shared__ uint32_t most[4];
   const int tid = threadIdx.x;
-  const int i0 = blockIdx.y * 128, o0 = blockIdx.x * 128;
   const int pitch = (d_in + 15) / 16 * 16, blocks = (d_in + 127) / 128, spitch = (blocks + 3) / 4 * 4;
+  // an XCD takes consecutive blocks, down the input in panels of kPanel8 blocks of output channels
+  const int blocks_o = (d_out + 127) / 128, all = blocks * blocks_o, per_xcd = (all + 7) >> 3;
+  const int within = static_cast<int>(blockIdx.y * (gridDim.x >> 3) + (blockIdx.x >> 3)), number = static_cast<int>(blockIdx.x & 7) * per_xcd + within;
+  if (within >= per_xcd || number >= all) return;
+  const int panel = number / (kPanel8 * blocks), wide = min(kPanel8, blocks_o - panel * kPanel8);
+  const int bi = __builtin_amdgcn_readfirstlane((number - panel * kPanel8 * blocks) / wide);
+  const int bo = __builtin_amdgcn_readfirstlane(panel * kPanel8 + (number - panel * kPanel8 * blocks) - bi * wide);
+  const int i0 = bi * 128, o0 = bo * 128;
   const int ki = tid / 16 * 8, oc = tid % 16 * 8;      // the lane's channels within the block
   uint4 raw[8];
 #pragma unroll
@@ -199,8 +209,8 @@ __global__ __launch_bounds__(256) void quantize_w8_kernel(const uint16_t* __rest
   const bool fine = finite_bits(m);
   const uint32_t byte = fine ? scale_byte(m) : kScaleOne;
   const float unit = unscale(byte);
-  if (tid == 0) scales[static_cast<size_t>(blockIdx.x) * spitch + blockIdx.y] = static_cast<uint8_t>(byte);
-  if (tid < spitch - blocks && blockIdx.y == 0) scales[static_cast<size_t>(blockIdx.x) * spitch + blocks + tid] = kScaleOne;
+  if (tid == 0) scales[static_cast<size_t>(bo) * spitch + bi] = static_cast<uint8_t>(byte);
+  if (tid < spitch - blocks && bi == 0) scales[static_cast<size_t>(bo) * spitch + blocks + tid] = kScaleOne;
   float v[8][8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) unpack8<T>(raw[k], v[k]);
@@ -657,7 +667,8 @@ hipError_t launch_out(const Product8Args& a, const Product8Plan& p, hipStream_t 
 }  // namespace
 
 hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s) {
-  const dim3 grid((d_out + 127) / 128, (d_in + 127) / 128);
+  const int per_xcd = ((d_out + 127) / 128 * ((d_in + 127) / 128) + 7) / 8, x = per_xcd < 1024 ? per_xcd : 1024;
+  const dim3 grid(8 * x, (per_xcd + x - 1) / x);
   if (bf16) quantize_w8_kernel<BF16><<<grid, 256, 0, s>>>(W, d_in, d_out, codes, scales);
   else quantize_w8_kernel<F16><<<grid, 256, 0, s>>>(W, d_in, d_out, codes, scales);
   return hipGetLastError();
