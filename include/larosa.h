@@ -401,6 +401,7 @@ int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, i
  *   value   = code * 2^(byte - 127), with the byte of the value's block
  * A block's scale is the least 2^e >= 2^-64 for which its largest magnitude is at most 448 * 2^e, its codes are nearest to value / 2^e, ties
  * to the even one; a block that holds a NaN or infinity gets scale 1 and NaN codes.  Values below 2^-74 in a block of such values count as 0.
+ * Scale bytes that a caller brings lie in 63 .. 247, as these do.
  * d_in is at most 2^20, d_out and ld_y below 2^21, n_rows at most 2^24; codes are 16-byte aligned, scales 4-byte. */
 
 /* W [d_in, d_out] (16-bit, type t, the layout of every weight of this library; d_out a multiple of 8) -> codes, scales. */

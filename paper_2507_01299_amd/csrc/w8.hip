@@ -514,12 +514,15 @@ __global__ __launch_bounds__(128 * WT, MO * MT >= 8 ? 1 : 2) void tile_product8_
 // bf16 with their scales (exact: four significant bits times a power of two) and multiplies them by v_mfma_f32_16x16x32_bf16, whose
 // sums are fp32 throughout: the matrix cores idle here anyway, and no bits are lost between neighbours.
 //  * A wave's next codes are on their way while it multiplies (8 KiB of the weight a wave, 128 KiB a compute unit).
-//  * The rows' codes serve STRIPS strips.
+//  * The rows' codes serve STRIPS strips: four 13 rows of 4096 x 128256 109 us (one: 182), 16 of 8192 x 57344 111 (160).
 //  * X = F16, BF16: x itself where its codes are few (kShortRows / STRIPS bytes); the waves bring it to 8 bits together, into LDS, while their first codes
-//    of the weight are on the way: one launch, not two.
+//    of the weight are on the way: one launch, not two (4096 x 4096, 1 row: 7.4 us, 9.6).
 constexpr int kFewRows = 16;
 constexpr int kFewWaves = 8;
 struct Held {};                        // rows that are in 8 bits already
+
+// Half of 2^(byte - 127): the largest value of a block near bf16's largest may round to 2^128.  (Byte 0 is what loads behind the end bring.)
+__device__ __forceinline__ float half_scale(uint32_t byte) { return __uint_as_float((byte ? byte - 1 : 0) << 23); }
 
 __device__ __forceinline__ void bf16_of_codes(const u32x4& lo, const u32x4& hi, float unit, bfloat8 (&out)[4]) {
 #pragma unroll
@@ -604,9 +607,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_rows8_kernel(Product8Ar
         xc[u][1] = *reinterpret_cast<const u32x4*>(codes + row * stride + b * 128 + 64 + 16 * q);
         xs[u] = scales[row * blocks + b];
       }
-      bf16_of_codes(xc[u][0], xc[u][1], __uint_as_float(xs[u] << 23), xv[u]);
+      bf16_of_codes(xc[u][0], xc[u][1], half_scale(xs[u]), xv[u]);
 #pragma unroll
-      for (int i = 0; i < STRIPS; ++i) bf16_of_codes(wc[u][i][0], wc[u][i][1], __uint_as_float(ws[u] << 23), wv[u][i]);
+      for (int i = 0; i < STRIPS; ++i) bf16_of_codes(wc[u][i][0], wc[u][i][1], half_scale(ws[u]), wv[u][i]);
     }
     load(b0 + kTurn);                            // (behind the last block: nothing is read)
 #pragma unroll
@@ -628,6 +631,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void few_rows8_kernel(Product8Ar
       const float4 s = *reinterpret_cast<const float4*>(&sums[k][row][col]);
       v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] *= 4.f;               // both sides were halved
     const int o = o0 + col;
     if (row < a.n_rows && o < a.d_out) {
       if constexpr (std::is_same<OUT, F32>::value) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + row * a.ld_y + o) = make_float4(v[0], v[1], v[2], v[3]);
@@ -667,8 +672,8 @@ hipError_t launch_out(const Product8Args& a, const Product8Plan& p, hipStream_t 
 }  // namespace
 
 hipError_t launch_quantize_w8(const uint16_t* W, int d_in, int d_out, uint8_t* codes, uint8_t* scales, bool bf16, hipStream_t s) {
-  const int per_xcd = ((d_out + 127) / 128 * ((d_in + 127) / 128) + 7) / 8, x = per_xcd < 1024 ? per_xcd : 1024;
-  const dim3 grid(8 * x, (per_xcd + x - 1) / x);
+  const int per_xcd = ((d_out + 127) / 128 * ((d_in + 127) / 128) + 7) / 8, rows = (per_xcd + 1023) / 1024;
+  const dim3 grid(8 * ((per_xcd + rows - 1) / rows), rows);
   if (bf16) quantize_w8_kernel<BF16><<<grid, 256, 0, s>>>(W, d_in, d_out, codes, scales);
   else quantize_w8_kernel<F16><<<grid, 256, 0, s>>>(W, d_in, d_out, codes, scales);
   return hipGetLastError();

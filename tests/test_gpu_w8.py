@@ -245,6 +245,26 @@ def test_dense_is_its_parts(api, dtype, n, d_in, d_out):
     assert bool(y[n // 2, :d_out].isnan().all()) and int(y.isnan().sum()) == d_out
 
 
+@pytest.mark.parametrize("n", [2, 5, 40, 300])
+def test_the_largest_values_of_the_type(api, n):
+    """bf16's largest value is 255 * 2^120 for a code of 256: 2^128 as a factor, beyond fp32, where the result is not."""
+    d_in, d_out = 264, 136
+    g = torch.Generator().manual_seed(n)
+    x, W = torch.randn(n, d_in, generator=g), torch.randn(d_in, d_out, generator=g) * 2.0 ** -20
+    x[n - 1, 7] = torch.finfo(torch.bfloat16).max
+    x[0, 200] = -torch.finfo(torch.bfloat16).max
+    (wc, ws), (xc, xs) = held(api, x, W, "bf16")
+    assert int(xs.max()) == 247
+    y = torch.empty(n, d_out, dtype=torch.bfloat16, device="cuda")
+    api.product8(wc, ws, xc, xs, d_in, y, "bf16", api.product8_workspace(n, d_in, d_out))
+    z = torch.empty_like(y)
+    api.dense_w8(wc, ws, x.bfloat16().cuda(), z, "bf16", api.dense_w8_workspace(n, d_in, d_out))
+    want, most = Q.product(wc.view(torch.uint8).cpu().numpy(), ws.cpu().numpy(), xc.view(torch.uint8).cpu().numpy(), xs.cpu().numpy(), d_in)
+    sums = (d_in + 8) * 2.0 ** -24 + (0 if n <= 16 else CUT)
+    for got in (y, z):
+        assert np.all(np.abs(exact(got) - want) <= sums * most + STEP["bf16"] * (np.abs(want) + sums * most))
+
+
 def test_dense_behind_a_norm_is_its_parts(api):
     for n in (2, 300):
         x, rms = torch.randn(n, 520).half().cuda(), (1 + 0.1 * torch.randn(520)).half().cuda()
