@@ -135,10 +135,6 @@ __device__ __forceinline__ u64 exchanged64(u64 v) {
 __device__ __forceinline__ u64 reversed(u64 v) {       // lane 63 - l
   return exchanged64<1>(exchanged64<2>(exchanged64<4>(exchanged64<8>(exchanged64<16>(exchanged64<32>(v))))));
 }
-__device__ __forceinline__ u64 shuffle_from(u64 v, int lane) {
-  const int lo = __shfl(static_cast<int>(static_cast<uint32_t>(v)), lane), hi = __shfl(static_cast<int>(v >> 32), lane);
-  return (static_cast<u64>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo);
-}
 __device__ __forceinline__ u64 lane_value(u64 v, int lane) {          // lane: uniform
   const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), lane), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), lane);
   return (static_cast<u64>(hi) << 32) | lo;

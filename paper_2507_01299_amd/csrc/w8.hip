@@ -661,11 +661,17 @@ void launch_tiles(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
 
 template <typename OUT>
 hipError_t launch_out(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
-  if (p.kind == 0 && !a.x16) launch_few<OUT, Held>(a, p, s);
-  else if (p.kind == 0 && a.x_bf16) launch_few<OUT, BF16>(a, p, s);
-  else if (p.kind == 0) launch_few<OUT, F16>(a, p, s);
-  else if (a.tiled) launch_tiles<OUT, true>(a, p, s);
-  else launch_tiles<OUT, false>(a, p, s);
+  if (p.kind == 0) {
+    if (!a.x16) launch_few<OUT, Held>(a, p, s);
+    else if (a.x_bf16) launch_few<OUT, BF16>(a, p, s);
+    else launch_few<OUT, F16>(a, p, s);
+  } else if (a.tiled) {
+    launch_tiles<OUT, true>(a, p, s);
+  } else if constexpr (!std::is_same<OUT, F32>::value) {
+    launch_tiles<OUT, false>(a, p, s);
+  } else {
+    return hipErrorInvalidValue;       // (fp32 logits are of rows that the library brought to 8 bits itself)
+  }
   return hipGetLastError();
 }
 

@@ -234,6 +234,41 @@ def test_score(api, dtype, n, d, V, top):
         assert np.all(np.abs(tops.double().cpu().numpy() - want[3]) <= 4 * b + REL * np.abs(want[3]))
 
 
+@pytest.mark.parametrize("tile", range(6))
+@pytest.mark.parametrize("n,d,V", [(17, 128, 1), (40, 264, 127), (33, 4104, 129), (150, 136, 5003), (300, 128, 100003), (1100, 64, 32001)])
+def test_score_without_alternatives(api, tile, n, d, V):
+    """With and without alternatives, whatever the tile and the number of given tokens: the same products, so the same logits.  A row of NaN stays alone; ids
+    that are padding, beyond the vocabulary, the same twice."""
+    print(f"score without alternatives {tile} {n}x{d}x{V}", flush=True)
+    g = torch.Generator().manual_seed(n + V)
+    x = torch.randn(n, d, generator=g).bfloat16().cuda()
+    x[n // 2, d - 1] = float("nan")
+    head = api.quantize_rows8((torch.randn(V, d, generator=g) * 0.5).bfloat16().cuda(), "bf16")[0], torch.full((-(-V // 128), -(-d // 512) * 4), 127, dtype=torch.uint8, device="cuda")
+    given = torch.randint(V, (n, 5), generator=g).int()
+    given[:, 1] = V - 1
+    given[3] = torch.tensor([-1, V, 0, 0, V // 2])
+    given[4, 2] = -2 ** 31
+    given[4, 3] = 2 ** 31 - 1
+    try:
+        api.set_tuning(11, tile)
+        work = api.score_w8_workspace(n, d, V, 1)
+        kept = [torch.full((n, 5), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")]
+        api.score_w8(*head, x, given.cuda(), kept[0], "bf16", work, entropy=kept[1], top_id=torch.empty(n, 1, dtype=torch.int32, device="cuda"), scale=0.7)
+        work = api.score_w8_workspace(n, d, V)
+        for few in (4, 1, 0, 5):
+            logp, entropy = torch.full((n, few), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+            api.score_w8(*head, x, given[:, :few].contiguous().cuda(), logp, "bf16", work, entropy=entropy, scale=0.7)
+            for got, want in ((logp, kept[0][:, :few]), (entropy, kept[1])):
+                assert torch.equal(got.isnan(), want.isnan())
+                got, want = got.double().nan_to_num(nan=0.0), want.double().nan_to_num(nan=0.0)
+                assert bool(((got - want).abs() <= 2 * (SUM + REL * want.abs())).all())
+            if few:
+                api.score_w8(*head, x, given[:, :few].contiguous().cuda(), logp, "bf16", work, scale=0.7)       # (no entropy)
+                assert torch.equal(logp.isnan(), kept[0][:, :few].isnan())
+    finally:
+        api.set_tuning(11, 0)
+
+
 def test_score_is_its_parts_behind_a_norm(api):
     """The whole call against its parts as a program would run them one by one, up to the parts' rounding of logits to 16 bits."""
     n, d, V = 20, 512, 2048
