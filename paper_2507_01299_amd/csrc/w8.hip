@@ -645,6 +645,7 @@ template <typename OUT, typename X>
 void launch_few(const Product8Args& a, const Product8Plan& p, hipStream_t s) {
   const dim3 grid(p.tiles_o);
   if (p.strips == 4) few_rows8_kernel<OUT, X, 4><<<grid, 64 * kFewWaves, 0, s>>>(a);
+  else if (p.strips == 2) few_rows8_kernel<OUT, X, 2><<<grid, 64 * kFewWaves, 0, s>>>(a);
   else few_rows8_kernel<OUT, X, 1><<<grid, 64 * kFewWaves, 0, s>>>(a);
 }
 
@@ -738,9 +739,12 @@ Product8Plan plan_product8(int n_rows, int d_in, int d_out) {
   if (n_rows <= kFewRows) {
     p.kind = 0;
     p.tiles_m = 1;
-    // Four strips a workgroup where that leaves one for each compute unit, or, where the rows' share counts, most of them.  Both sides in us:
-    // 4096 x 28672, 1 row 30.4 (one strip: 32.3), 16 rows 33 (49); 4096 x 11008, 1 row 16.7 (15.2), 16 rows 19 (23); 4096 x 4096, 1 row 13.5 (7.1).
-    p.strips = d_out >= 64 * (n_rows > 2 ? 160 : 256) ? 4 : 1;
+    // Four strips a workgroup where that leaves one for each compute unit, or, where the rows' share counts, most of them; else two where the rows'
+    // share counts more.  Both sides in us: 4096 x 28672, 1 row 30.4 (one strip: 32.3), 16 rows 33 (49); 4096 x 11008, 1 row 16.7 (15.2), 16 rows
+    // 19 (23), 4 rows 20.0 (17.4: one launch); 4096 x 4096, 1 row 13.5 (7.1).  Two: 8192 x 8192, 16 rows 25.0 (28.1), 8 rows 23.1 (23.7), 2 rows
+    // 22.8 (19.8); 28672 x 8192, 16 rows 75 (82).
+    const int most = d_out >= 64 * (n_rows > 4 ? 160 : 256) ? 4 : 2;
+    p.strips = most == 4 || (n_rows > 4 && d_out >= 32 * 224) ? most : 1;
     p.tiles_o = (d_out + 16 * p.strips - 1) / (16 * p.strips);
     return p;
   }

@@ -123,7 +123,7 @@ def test_weight_bit_for_bit(api, dtype, d_in, d_out):
 CUT = 2.0 ** -10
 SHAPES = [
     (1, 8, 8), (1, 128, 16), (2, 136, 24), (5, 4104, 136), (15, 512, 264), (16, 1032, 520), (16, 24, 1000),          # few rows
-    (3, 136, 10264), (16, 520, 10248), (1, 264, 16392), (9, 1160, 16416),                                              # of a wide weight
+    (3, 136, 10264), (16, 520, 10248), (1, 264, 16392), (9, 1160, 16416), (5, 136, 7176), (16, 1032, 8200),                                              # of a wide weight
     (17, 8, 8), (17, 136, 24), (33, 1032, 264), (64, 4104, 136), (64, 512, 1160),
     (65, 16, 8), (65, 520, 264), (100, 4104, 392), (129, 128, 136), (193, 1000, 520), (300, 2056, 1032),
     (1100, 136, 9992), (1025, 648, 4104), (257, 8200, 264),                                       # whole bands; many parts
@@ -227,8 +227,8 @@ def test_codes_of_others_with_extreme_scales(api, n):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,d_in,d_out", [(1, 8, 8), (1, 4104, 136), (3, 136, 24), (4, 4096, 264), (5, 4096, 264), (16, 1024, 40), (16, 1032, 40),
-                                          (1, 16384, 16), (1, 16392, 16), (1, 264, 16392), (1, 4096, 16392), (2, 4096, 16392), (4, 1000, 10264),
-                                          (9, 136, 10264), (40, 264, 136), (130, 520, 264)])
+                                          (1, 16384, 16), (1, 16392, 16), (1, 264, 16392), (1, 4096, 16392), (2, 4096, 16392), (4, 1000, 10264), (3, 4096, 10264),
+                                          (9, 136, 10264), (8, 1024, 7176), (40, 264, 136), (130, 520, 264)])
 def test_dense_is_its_parts(api, dtype, n, d_in, d_out):
     """Short rows are brought to 8 bits by the product itself, others before it: the same bits.  Rows lie apart, and one holds a NaN."""
     print(f"dense {dtype} {n}x{d_in}x{d_out}", flush=True)
