@@ -638,6 +638,7 @@ def scales_pitch8(d: int) -> int:
 
 
 _CODES = (torch.float8_e4m3fn, torch.uint8)
+_LOGITS = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
 
 
 def _held8(codes, scales, d_in: int, rows_of_block: int, device: int):
@@ -661,14 +662,32 @@ def _device_stream(*tensors):
     return device, torch._C._cuda_getCurrentRawStream(device)
 
 
+def _distance(t) -> int:
+    """Distance between the rows of a matrix.  The library's sizes are 32-bit: a larger one would arrive as its low 32 bits, another matrix."""
+    rows, width = t.shape
+    ld, one = t.stride()
+    if one != 1 and width != 1:
+        raise ValueError("the values of a row lie next to one another")
+    if (ld >> 31 and rows > 1) or rows >> 31 or width >> 31:
+        raise ValueError("sizes and distances between rows are below 2^31")
+    return ld
+
+
 def _matrix16(t, code: int) -> int:
     """Distance between the rows of a matrix of the type `code`."""
     if t.dtype is not torch_dtype(code) or t.dim() != 2:
         raise ValueError("rows are a matrix of the call's type")
-    ld, one = t.stride()
-    if one != 1 and t.shape[1] != 1:
-        raise ValueError("the values of a row lie next to one another")
-    return ld if t.shape[0] > 1 else max(ld, -(-t.shape[1] // 8) * 8)
+    ld = _distance(t)
+    # one row: whatever its tensor says of the distance to the next, one that the library takes
+    return ld if t.shape[0] > 1 else max(min(ld // 8 * 8, 1 << 20), -(-t.shape[1] // 8) * 8)
+
+
+def _logits(t):
+    """Distance between the rows of logits, and their type."""
+    if t.dtype not in _LOGITS or t.dim() != 2:
+        raise ValueError("logits are a matrix of float16, bfloat16 or float32")
+    ld = _distance(t)
+    return ld if t.shape[0] > 1 else t.shape[1], _LOGITS[t.dtype]
 
 
 def _norm8(rms, d: int, code: int):
@@ -681,9 +700,10 @@ def quantize_w8(W, dtype):
     """e4m3 codes (float8_e4m3fn [d_out, d_in up to 16]) and scale bytes (uint8 [d_out / 128 up, d_in / 128 up, up to 4]) of
     W [d_in, d_out]."""
     code = dtype_code(dtype)
-    d_in, d_out = W.shape
     _, stream = _device_stream(W)
-    if W.dtype is not torch_dtype(code) or not W.is_contiguous():
+    _matrix16(W, code)
+    d_in, d_out = W.shape
+    if not W.is_contiguous():
         raise ValueError("W is a contiguous matrix of the call's type")
     codes = torch.empty(d_out, codes_pitch8(d_in), dtype=torch.float8_e4m3fn, device=W.device)
     scales = torch.empty(-(-d_out // 128), scales_pitch8(d_in), dtype=torch.uint8, device=W.device)
@@ -694,9 +714,9 @@ def quantize_w8(W, dtype):
 def quantize_rows8(x, dtype, rms=None, rms_eps: float = -1.0):
     """Codes [n, d up to 16] and scale bytes [n, d / 128 up, up to 4] of x [n, d]; rms_eps >= 0: behind a norm (rms: its scale)."""
     code = dtype_code(dtype)
-    n, d = x.shape
     _, stream = _device_stream(x, rms)
     ld = _matrix16(x, code)
+    n, d = x.shape
     codes = torch.empty(n, codes_pitch8(d), dtype=torch.float8_e4m3fn, device=x.device)
     scales = torch.empty(n, scales_pitch8(d), dtype=torch.uint8, device=x.device)
     _check(lib().larosa_quantize_rows8(_ptr(x), ld, n, d, _norm8(rms, d, code), rms_eps, code, _ptr(codes), _ptr(scales), stream),
@@ -746,9 +766,6 @@ def dense_w8(w_codes, w_scales, x, y, dtype, ws: Workspace, rms=None, rms_eps: f
     return y
 
 
-_LOGITS = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
-
-
 def _outputs8(n: int, given, logp, entropy, top_id, top_logp):
     """Numbers of given and of top tokens."""
     n_given = 0 if given is None else given.shape[1]
@@ -761,6 +778,8 @@ def _outputs8(n: int, given, logp, entropy, top_id, top_logp):
         raise ValueError("entropy is a contiguous float32 vector, a value for each row")
     if (logp is None) != (given is None) and n_given:
         raise ValueError("given tokens and logp come together")
+    if n_given >> 31:
+        raise ValueError("fewer than 2^31 given tokens of a row")
     return n_given, n_top
 
 
@@ -774,12 +793,10 @@ def logprobs(logits, given, logp, ws: Workspace, entropy=None, top_id=None, top_
     """Log probabilities of the given tokens [n, n_given] under softmax(scale * logits [n, n_vocab]), the rows' entropy [n] and the most
     probable tokens top_id [n, n_top] with theirs, top_logp."""
     device, stream = _device_stream(logits, given, logp, entropy, top_id, top_logp, ws.buf)
+    ld, kind = _logits(logits)
     n, V = logits.shape
-    ld, one = logits.stride()
-    if logits.dtype not in _LOGITS or (one != 1 and V > 1):
-        raise ValueError("logits are float16, bfloat16 or float32, those of a row next to one another")
     n_given, n_top = _outputs8(n, given, logp, entropy, top_id, top_logp)
-    _check(lib().larosa_logprobs(_ptr(logits), ld if n > 1 else max(ld, V), n, V, _LOGITS[logits.dtype], scale, _ptr(given), n_given,
+    _check(lib().larosa_logprobs(_ptr(logits), ld, n, V, kind, scale, _ptr(given), n_given,
                                  _ptr(logp), _ptr(entropy), n_top, _ptr(top_id), _ptr(top_logp), ws.ptr, ws.nbytes, stream),
            "larosa_logprobs")
     return logp

@@ -153,3 +153,34 @@ def test_tiles_that_there_are(lib):
                 assert lib.larosa_product8_workspace_bytes(n, d_in, d_out) > 0
     finally:
         lib.larosa_set_tuning(11, 0)
+
+
+def strided(shape, stride, dtype=torch.float16):
+    """A matrix that takes no memory."""
+    return torch.empty_strided(shape, stride, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("shape,stride", [((2, 8), ((1 << 32) + 8, 1)), ((3, 64), ((1 << 31) + 64, 1)), (((1 << 32) + 5, 8), (8, 1)),
+                                          ((1, (1 << 32) + 64), ((1 << 32) + 64, 1)), ((1 << 31, 8), (8, 1))])
+def test_sizes_beyond_32_bits_are_refused(shape, stride):
+    """In an int argument 2^32 + 8 arrives as 8: rows of a wide tensor, such as the last token's logits of a long batch, would be read from
+    other places."""
+    from paper_2507_01299_amd import api
+    with pytest.raises(ValueError):
+        api._matrix16(strided(shape, stride), api.F16)
+    with pytest.raises(ValueError):
+        api._logits(strided(shape, stride, torch.float32))
+
+
+def test_one_row_of_a_matrix_of_any_distance():
+    """What a single row's tensor says of the distance to the next one counts for nothing."""
+    from paper_2507_01299_amd import api
+    for ld in (1, 64, 1001, 1 << 21, (1 << 31) + 4, (1 << 32) + 64):
+        one = api._matrix16(strided((1, 64), (ld, 1)), api.F16)
+        assert one % 8 == 0 and 64 <= one < 1 << 21
+        assert api._logits(strided((1, 65), (ld, 1), torch.bfloat16)) == (65, api.BF16)
+    assert api._matrix16(strided((2, 64), ((1 << 31) - 8, 1)), api.F16) == (1 << 31) - 8
+    assert api._logits(strided((2, 1), (7, 5))) == (7, api.F16)
+    for bad in (strided((2, 64), (64, 2)), strided((2, 64, 1), (64, 1, 1)), strided((2, 64), (64, 1), torch.float64)):
+        with pytest.raises(ValueError):
+            api._logits(bad)
