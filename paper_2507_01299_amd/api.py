@@ -690,7 +690,9 @@ def _logits(t):
     return ld if t.shape[0] > 1 else t.shape[1], _LOGITS[t.dtype]
 
 
-def _norm8(rms, d: int, code: int):
+def _norm8(rms, d: int, code: int, rms_eps: float = 0.0):
+    if rms is not None and not rms_eps >= 0:
+        raise ValueError("rms is the scale of a norm: rms_eps is at least 0 with it")
     if rms is not None and (rms.dtype is not torch_dtype(code) or rms.shape != (d,) or not rms.is_contiguous()):
         raise ValueError("rms is a contiguous vector of the call's type, a value for each channel")
     return _ptr(rms)
@@ -712,14 +714,15 @@ def quantize_w8(W, dtype):
 
 
 def quantize_rows8(x, dtype, rms=None, rms_eps: float = -1.0):
-    """Codes [n, d up to 16] and scale bytes [n, d / 128 up, up to 4] of x [n, d]; rms_eps >= 0: behind a norm (rms: its scale)."""
+    """Codes [n, d up to 16] and scale bytes [n, d / 128 up, up to 4] of x [n, d]; rms_eps >= 0: behind a norm (rms: its scale,
+    None = 1); without a norm there is no rms."""
     code = dtype_code(dtype)
     _, stream = _device_stream(x, rms)
     ld = _matrix16(x, code)
     n, d = x.shape
     codes = torch.empty(n, codes_pitch8(d), dtype=torch.float8_e4m3fn, device=x.device)
     scales = torch.empty(n, scales_pitch8(d), dtype=torch.uint8, device=x.device)
-    _check(lib().larosa_quantize_rows8(_ptr(x), ld, n, d, _norm8(rms, d, code), rms_eps, code, _ptr(codes), _ptr(scales), stream),
+    _check(lib().larosa_quantize_rows8(_ptr(x), ld, n, d, _norm8(rms, d, code, rms_eps), rms_eps, code, _ptr(codes), _ptr(scales), stream),
            "larosa_quantize_rows8")
     return codes, scales
 
@@ -761,7 +764,7 @@ def dense_w8(w_codes, w_scales, x, y, dtype, ws: Workspace, rms=None, rms_eps: f
     ld_x, ld_y = _matrix16(x, code), _matrix16(y, code)
     if y.shape != (n, w_codes.shape[0]):
         raise ValueError("y has a row for each row of x and a column for each output channel")
-    _check(lib().larosa_dense_w8(wc, wsc, _ptr(x), ld_x, _norm8(rms, d_in, code), rms_eps, _ptr(y), ld_y, n, d_in, y.shape[1], code,
+    _check(lib().larosa_dense_w8(wc, wsc, _ptr(x), ld_x, _norm8(rms, d_in, code, rms_eps), rms_eps, _ptr(y), ld_y, n, d_in, y.shape[1], code,
                                  ws.ptr, ws.nbytes, stream), "larosa_dense_w8")
     return y
 
@@ -815,7 +818,7 @@ def score_w8(w_codes, w_scales, x, given, logp, dtype, ws: Workspace, entropy=No
     wc, wsc = _held8(w_codes, w_scales, d_in, 128, device)
     ld_x = _matrix16(x, code)
     n_given, n_top = _outputs8(n, given, logp, entropy, top_id, top_logp)
-    _check(lib().larosa_score_w8(wc, wsc, _ptr(x), ld_x, _norm8(rms, d_in, code), rms_eps, n, d_in, w_codes.shape[0], code, scale,
+    _check(lib().larosa_score_w8(wc, wsc, _ptr(x), ld_x, _norm8(rms, d_in, code, rms_eps), rms_eps, n, d_in, w_codes.shape[0], code, scale,
                                  _ptr(given), n_given, _ptr(logp), _ptr(entropy), n_top, _ptr(top_id), _ptr(top_logp), ws.ptr,
                                  ws.nbytes, stream), "larosa_score_w8")
     return logp

@@ -184,3 +184,27 @@ def test_one_row_of_a_matrix_of_any_distance():
     for bad in (strided((2, 64), (64, 2)), strided((2, 64, 1), (64, 1, 1)), strided((2, 64), (64, 1), torch.float64)):
         with pytest.raises(ValueError):
             api._logits(bad)
+
+
+@pytest.mark.parametrize("eps", [None, -1.0, -1e-5, float("nan")])
+def test_a_norms_scale_without_a_norm_is_refused(monkeypatch, eps):
+    """rms given and rms_eps left at "no norm": the scale would be dropped in silence."""
+    from paper_2507_01299_amd import api
+
+    class Library:
+        def __getattr__(self, name):
+            def called(*args):
+                raise AssertionError(f"{name} was called")
+            return called
+    monkeypatch.setattr(api, "_device_stream", lambda *tensors: (-1, None))
+    monkeypatch.setattr(api, "lib", Library)
+    x, rms, y = torch.empty(2, 128, dtype=torch.float16), torch.empty(128, dtype=torch.float16), torch.empty(2, 256, dtype=torch.float16)
+    codes, scales = torch.empty(256, 128, dtype=torch.float8_e4m3fn), torch.empty(2, 4, dtype=torch.uint8)
+
+    class Work:
+        buf, ptr, nbytes = None, 0, 0
+    kw = dict(rms=rms) if eps is None else dict(rms=rms, rms_eps=eps)
+    for call in (lambda: api.quantize_rows8(x, "f16", **kw), lambda: api.dense_w8(codes, scales, x, y, "f16", Work, **kw),
+                 lambda: api.score_w8(codes, scales, x, torch.empty(2, 1, dtype=torch.int32), torch.empty(2, 1), "f16", Work, **kw)):
+        with pytest.raises(ValueError):
+            call()
