@@ -427,13 +427,13 @@ int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, in
                     int ld_y, int n_rows, int d_in, int d_out, larosa_dtype t, void* ws, size_t ws_bytes, void* stream);
 
 /* Log probabilities.  For each row of logits [n_rows, n_vocab] (type t, F32 too; rows ld apart, any ld >= n_vocab; aligned to their type), with
- * z = scale * logit (scale > 0: one over a temperature):
+ * z = scale * logit (0 < scale <= 2^126: one over a temperature):
  *   logp[r, i]  = z[given[r, i]] - ln sum exp z       given, logp [n_rows, n_given]; a negative id is padding: 0; an id >= n_vocab: NaN
  *   entropy[r]  = - sum p ln p, in nats               [n_rows], nullable
  *   top_id, top_logp [n_rows, n_top]: the n_top largest logits, ties to the lower id, with their log probabilities (top_logp nullable)
  * A logit of -infinity has probability 0; a row of nothing else gets logp -infinity and entropy 0.  A row that holds a NaN or +infinity gets
- * NaN everywhere and top_id -1.  Sums and statistics are fp32.  n_given >= 0, 0 <= n_top <= min(64, n_vocab); outputs that are not asked
- * for (n_given or n_top 0) may be NULL.
+ * NaN everywhere and top_id -1.  A logit counts as -infinity where its difference to the row's largest leaves fp32.  Sums and statistics
+ * are fp32.  n_given >= 0, 0 <= n_top <= min(64, n_vocab); outputs that are not asked for (n_given or n_top 0) may be NULL.
  * Workspace: larosa_logprobs_workspace_bytes, initialised by larosa_workspace_init; at most 2^24 rows of at most 2^28 logits. */
 size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, larosa_dtype t);
 int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_dtype t, float scale, const int32_t* given,

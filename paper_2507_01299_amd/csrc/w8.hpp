@@ -63,6 +63,7 @@ hipError_t launch_product8(const Product8Args& a, const Product8Plan& p, hipStre
 enum : int { kLogitsF16 = 0, kLogitsBF16 = 1, kLogitsF32 = 2 };
 constexpr int kTopMax = 64;
 constexpr int kVocabMax = 1 << 28;     // bytes of a row are below 2^31
+constexpr float kLogitScaleMax = 0x1p126f;     // scale / ln 2 is finite: infinity times a difference of 0 would be NaN
 struct LogprobsArgs {
   const void* logits;
   long ld;

@@ -81,7 +81,7 @@ int check_logprobs(int n_rows, int n_vocab, float scale, const void* given, int 
   if (n_given > 0 && (!given || !logp)) return LAROSA_EINVAL;
   if (n_top > 0 && !top_id) return LAROSA_EINVAL;
   if (!aligned(given, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(top_id, 4) || !aligned(top_logp, 4)) return LAROSA_EINVAL;
-  if (n_rows > kRowsMax8 || n_vocab > kVocabMax || n_top > kTopMax) return LAROSA_EUNSUPPORTED;
+  if (n_rows > kRowsMax8 || n_vocab > kVocabMax || n_top > kTopMax || scale > kLogitScaleMax) return LAROSA_EUNSUPPORTED;
   return LAROSA_OK;
 }
 

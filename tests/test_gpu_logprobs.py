@@ -151,6 +151,19 @@ def test_scale(api, scale):
         check(api, z, given, 9, s)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** 126, 1e30, 2.0 ** -126, 1e-42])
+@pytest.mark.parametrize("V", [50, 33000])
+def test_extreme_scales(api, V, scale):
+    """Next to the largest scale only the largest logit's equals count, next to 0 all logits count alike."""
+    s = float(np.float32(scale))
+    z = -torch.randint(0, 3, (4, V), generator=torch.Generator().manual_seed(V)).float()
+    z[1, ::3] = -float("inf")
+    z[2, 7] = 1.0
+    z[3] = -float("inf")
+    for dtype in ("bf16", "f32"):
+        check(api, z.to(TYPE[dtype]).cuda(), torch.tensor([[0, 1, 7, V - 1]] * 4), 6, s)
+
+
 def test_what_is_not_asked_for(api):
     z, given = draw(4, 5000, 8, "bf16")
     assert run(api, z, given[:, :0], 0)[0].shape == (4, 0)

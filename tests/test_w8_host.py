@@ -155,6 +155,14 @@ def test_tiles_that_there_are(lib):
         lib.larosa_set_tuning(11, 0)
 
 
+def test_scales_whose_exponent_would_overflow_are_refused(lib):
+    """scale / ln 2 leaves fp32 from 2.4e38 on, and infinity times the difference of two equal logits is NaN."""
+    for scale in (3e38, 2.4e38, 1.0000001 * 2.0 ** 126):
+        assert call(lib.larosa_logprobs, LOGPROBS, scale=scale) == EUNSUPPORTED
+        assert call(lib.larosa_score_w8, SCORE, scale=scale) == EUNSUPPORTED
+    assert call(lib.larosa_logprobs, LOGPROBS, scale=2.0 ** 126, work=None) == EWORKSPACE
+
+
 def strided(shape, stride, dtype=torch.float16):
     """A matrix that takes no memory."""
     return torch.empty_strided(shape, stride, dtype=dtype, device="meta")
