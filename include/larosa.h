@@ -415,8 +415,8 @@ int larosa_quantize_rows8(const void* x, int ld_x, int n_rows, int d, const void
 /* y[m, o] = sum_i x[m, i] W[o, i] over the values that rows and weight stand for; y [n_rows, d_out] (type t, rows ld_y apart, a multiple of
  * 8), rounded once.  d_out is a multiple of 8.  Sums are fp32; from 17 rows on the products of eight neighbours are added by the 8-bit matrix
  * instruction, which cuts them 13 bits below the largest one's exponent (about 2^-16 of the result's norm, with a few strong channels 2^-14.5).
- * Workspace: larosa_product8_workspace_bytes, initialised by larosa_workspace_init; fewer rows may need more of it than many
- * (sums go in parts), so a workspace for several numbers of rows is the largest of their answers.  Up to 2^23 tiles of 128 rows x 128 channels. */
+ * Workspace: larosa_product8_workspace_bytes, initialised by larosa_workspace_init; one for n_rows rows serves any smaller number of
+ * them too, here and in the calls below (the query looks at all of them: once for a workspace, not at every call).  Up to 2^23 tiles of 128 rows x 128 channels. */
 size_t larosa_product8_workspace_bytes(int n_rows, int d_in, int d_out);
 int larosa_product8(const void* w_codes, const void* w_scales, const void* x_codes, const void* x_scales, void* y, int ld_y,
                     int n_rows, int d_in, int d_out, larosa_dtype t, void* ws, size_t ws_bytes, void* stream);

@@ -29,7 +29,6 @@ constexpr int kGroup = 8;                      // logits of a group
 constexpr int kHoldersMax = 2048;              // of a slice: one of 262144 logits
 constexpr int kSmallSlice = 4096;              // up to here a wave's chunks are of one group a lane, so that all four have some
 constexpr int kLeastSlice = 4096, kLeastOfMany = 24576;   // few rows: no shorter slices, from 128 rows on
-constexpr int kWorkgroups = 512;               // and no more of them than this many in all
 
 __device__ __forceinline__ uint32_t& word_of(uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 struct Logits16 {
@@ -581,8 +580,8 @@ LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type) {
   const long places = static_cast<long>(n_vocab) + 7;                   // a row may start inside a group
   constexpr long kMost = kHoldersMax / 16 * 2048;                       // a slice's holders lie in LDS
   long slices = (places + kMost - 1) / kMost;
-  if (n_rows * slices < kWorkgroups) {                                  // few rows: slices for all compute units
-    const long fine = places / (n_rows < 128 ? kLeastSlice : kLeastOfMany), want = (kWorkgroups + n_rows - 1) / n_rows;
+  if (n_rows * slices < kWorkgroupsOfFew) {                             // few rows: slices for all compute units
+    const long fine = places / (n_rows < 128 ? kLeastSlice : kLeastOfMany), want = (kWorkgroupsOfFew + n_rows - 1) / n_rows;
     const long more = want < fine ? want : fine;
     if (more > slices) slices = more;
   }

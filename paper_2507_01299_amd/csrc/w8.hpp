@@ -53,7 +53,8 @@ struct Product8Plan {
   int tiles_m, tiles_o, splits, blocks_per;
   size_t partial_floats;
 };
-Product8Plan plan_product8(int n_rows, int d_in, int d_out);
+Product8Plan plan_product8(int n_rows, int d_in, int d_out);      // from 17 rows on the same for 64 k + 1 .. 64 k + 64 rows
+constexpr int kRowsOfParts8 = 32768;   // with more rows no sum goes in parts: their tiles, of any kind, fill more than half of the chip
 inline bool takes_rows16(const Product8Plan& p, int n_rows, int d_in) {
   return p.kind == 0 && n_rows * ((d_in + 127) / 128) * p.strips <= kShortRows / 128;
 }
@@ -62,6 +63,7 @@ hipError_t launch_product8(const Product8Args& a, const Product8Plan& p, hipStre
 // Log probabilities of logits [n_rows, ld], the first n_vocab of a row.
 enum : int { kLogitsF16 = 0, kLogitsBF16 = 1, kLogitsF32 = 2 };
 constexpr int kTopMax = 64;
+constexpr int kWorkgroupsOfFew = 512;  // fewer rows go in slices, up to this many workgroups in all
 constexpr int kVocabMax = 1 << 28;     // bytes of a row are below 2^31
 constexpr float kLogitScaleMax = 0x1p126f;     // scale / ln 2 is finite: infinity times a difference of 0 would be NaN
 struct LogprobsArgs {

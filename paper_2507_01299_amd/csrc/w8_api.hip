@@ -33,9 +33,8 @@ int check_rows(const void* x, int ld_x, int n_rows, int d, const void* rms) {
 }
 
 // A product of n rows of x: the rows to 8 bits at `codes` and `scales`, unless the product takes them as they are, then the product.
-int run_product(Product8Args a, const void* x, int ld_x, const void* rms, float rms_eps, larosa_dtype t, uint8_t* codes,
-                uint8_t* scales, hipStream_t s) {
-  const Product8Plan plan = plan_product8(a.n_rows, a.d_in, a.d_out);
+int run_product(Product8Args a, const Product8Plan& plan, const void* x, int ld_x, const void* rms, float rms_eps, larosa_dtype t,
+                uint8_t* codes, uint8_t* scales, hipStream_t s) {
   const uint16_t* const rows = static_cast<const uint16_t*>(x);
   if (rms_eps < 0.f && takes_rows16(plan, a.n_rows, a.d_in)) {
     a.x16 = rows;
@@ -68,6 +67,17 @@ struct Carver {
   }
 };
 
+// What the queries answer: the most that any number of rows up to n_rows asks for (fewer rows go in more parts or slices), so that a workspace for
+// the largest batch serves the smaller ones.  A call itself looks at its own need only.
+size_t partial_up_to(int n_rows, int d_in, int d_out) {
+  size_t most = 0;
+  for (int n = 64; n - 64 < n_rows && n <= kRowsOfParts8; n += 64) {
+    const size_t here = plan_product8(n < n_rows ? n : n_rows, d_in, d_out).partial_floats;
+    if (here > most) most = here;
+  }
+  return most;
+}
+
 struct RowsSpace { size_t codes, scales; };
 RowsSpace take_rows(Carver& c, int n_rows, int d) {
   const size_t codes = c.take(tiled_bytes8(n_rows, d));
@@ -97,6 +107,15 @@ int rows_at_once(const LogprobsPlan& p) {
 size_t logprobs_space(const LogprobsPlan& p, int n_rows) {
   const int n = rows_at_once(p) < n_rows ? rows_at_once(p) : n_rows;
   return round_up(p.sums_bytes * n, 256) + round_up(p.best_bytes * n, 256);
+}
+
+size_t logprobs_space_up_to(int n_rows, int n_vocab, int n_top, int type) {
+  size_t most = logprobs_space(plan_logprobs(n_rows, n_vocab, n_top, type), n_rows);
+  for (int n = 1; n < n_rows && n <= kWorkgroupsOfFew; ++n) {
+    const size_t here = logprobs_space(plan_logprobs(n, n_vocab, n_top, type), n);
+    if (here > most) most = here;
+  }
+  return most;
 }
 
 int run_logprobs(LogprobsArgs a, int n_rows, int type, const LogprobsPlan& p, unsigned* counters, char* space, hipStream_t s) {
@@ -134,20 +153,26 @@ int score_rows(int n_rows, int n_vocab) {
 }
 
 struct ScoreSpace { RowsSpace rows; size_t partial, logits, logprobs, end; int at_once; long ld; };
-ScoreSpace score_space(int n_rows, int d_in, int n_vocab, int n_top) {
+ScoreSpace score_space(int n_rows, int d_in, int n_vocab, int n_top, bool up_to = false) {
   ScoreSpace s{};
   Carver c;
   s.at_once = score_rows(n_rows, n_vocab);
   s.ld = static_cast<long>(round_up(n_vocab, 16));
   const int tail = n_rows % s.at_once;
   s.rows = take_rows(c, s.at_once, d_in);
-  size_t partial = plan_product8(s.at_once, d_in, n_vocab).partial_floats;
-  size_t probs = logprobs_space(plan_logprobs(s.at_once, n_vocab, n_top, kLogitsF32), s.at_once);
-  if (tail) {                                    // the last part may be divided otherwise
-    const size_t p = plan_product8(tail, d_in, n_vocab).partial_floats;
-    const size_t q = logprobs_space(plan_logprobs(tail, n_vocab, n_top, kLogitsF32), tail);
-    if (p > partial) partial = p;
-    if (q > probs) probs = q;
+  size_t partial, probs;
+  if (up_to) {
+    partial = partial_up_to(s.at_once, d_in, n_vocab);
+    probs = logprobs_space_up_to(s.at_once, n_vocab, n_top, kLogitsF32);
+  } else {
+    partial = plan_product8(s.at_once, d_in, n_vocab).partial_floats;
+    probs = logprobs_space(plan_logprobs(s.at_once, n_vocab, n_top, kLogitsF32), s.at_once);
+    if (tail) {                                  // the last part may be divided otherwise
+      const size_t p = plan_product8(tail, d_in, n_vocab).partial_floats;
+      const size_t q = logprobs_space(plan_logprobs(tail, n_vocab, n_top, kLogitsF32), tail);
+      if (p > partial) partial = p;
+      if (q > probs) probs = q;
+    }
   }
   s.partial = c.take(partial * sizeof(float));
   s.logits = c.take(static_cast<size_t>(s.at_once) * s.ld * sizeof(float));
@@ -199,7 +224,7 @@ int larosa_quantize_rows8(const void* x, int ld_x, int n_rows, int d, const void
 size_t larosa_product8_workspace_bytes(int n_rows, int d_in, int d_out) {
   if (check_product(n_rows, d_in, d_out)) return 0;
   Carver c;
-  c.take(plan_product8(n_rows, d_in, d_out).partial_floats * sizeof(float));
+  c.take(partial_up_to(n_rows, d_in, d_out) * sizeof(float));
   return c.at;
 }
 
@@ -210,17 +235,20 @@ int larosa_product8(const void* w_codes, const void* w_scales, const void* x_cod
   if (int rc = check_held(x_codes, x_scales)) return rc;
   if (int rc = check_product(n_rows, d_in, d_out)) return rc;
   if (ld_y > kOutMax8) return LAROSA_EUNSUPPORTED;
-  if (!ws || !aligned(ws, 256) || ws_bytes < larosa_product8_workspace_bytes(n_rows, d_in, d_out)) return LAROSA_EWORKSPACE;
+  const Product8Plan plan = plan_product8(n_rows, d_in, d_out);
+  Carver c;
+  c.take(plan.partial_floats * sizeof(float));
+  if (!ws || !aligned(ws, 256) || ws_bytes < c.at) return LAROSA_EWORKSPACE;
   const Product8Args a = product_args(w_codes, w_scales, x_codes, x_scales, y, ld_y, n_rows, d_in, d_out,
                                       t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, kCounterBytes);
-  return status_of(launch_product8(a, plan_product8(n_rows, d_in, d_out), stream_of(stream)));
+  return status_of(launch_product8(a, plan, stream_of(stream)));
 }
 
 size_t larosa_dense_w8_workspace_bytes(int n_rows, int d_in, int d_out) {
   if (check_product(n_rows, d_in, d_out)) return 0;
   Carver c;
   take_rows(c, n_rows, d_in);
-  c.take(plan_product8(n_rows, d_in, d_out).partial_floats * sizeof(float));
+  c.take(partial_up_to(n_rows, d_in, d_out) * sizeof(float));
   return c.at;
 }
 
@@ -231,13 +259,15 @@ int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, in
   if (int rc = check_product(n_rows, d_in, d_out)) return rc;
   if (int rc = check_rows(x, ld_x, n_rows, d_in, rms)) return rc;
   if (ld_y > kOutMax8) return LAROSA_EUNSUPPORTED;
-  if (!ws || !aligned(ws, 256) || ws_bytes < larosa_dense_w8_workspace_bytes(n_rows, d_in, d_out)) return LAROSA_EWORKSPACE;
+  const Product8Plan plan = plan_product8(n_rows, d_in, d_out);
   Carver c;
   const RowsSpace r = take_rows(c, n_rows, d_in);
+  const size_t partial = c.take(plan.partial_floats * sizeof(float));
+  if (!ws || !aligned(ws, 256) || ws_bytes < c.at) return LAROSA_EWORKSPACE;
   char* const w = static_cast<char*>(ws);
   const Product8Args a = product_args(w_codes, w_scales, w + r.codes, w + r.scales, y, ld_y, n_rows, d_in, d_out,
-                                      t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, c.at);
-  return run_product(a, x, ld_x, rms, rms_eps, t, reinterpret_cast<uint8_t*>(w + r.codes), reinterpret_cast<uint8_t*>(w + r.scales),
+                                      t == LAROSA_BF16 ? kOutBF16 : kOutF16, ws, partial);
+  return run_product(a, plan, x, ld_x, rms, rms_eps, t, reinterpret_cast<uint8_t*>(w + r.codes), reinterpret_cast<uint8_t*>(w + r.scales),
                      stream_of(stream));
 }
 
@@ -245,7 +275,7 @@ size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, laros
   if (!type16(t) && t != LAROSA_F32) return 0;
   if (check_logprobs(n_rows, n_vocab, 1.f, nullptr, 0, nullptr, nullptr, 0, nullptr, nullptr)) return 0;
   if (n_top < 0 || n_top > kTopMax || n_top > n_vocab) return 0;
-  return kCounterBytes + logprobs_space(plan_logprobs(n_rows, n_vocab, n_top, t), n_rows);
+  return kCounterBytes + logprobs_space_up_to(n_rows, n_vocab, n_top, t);
 }
 
 int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_dtype t, float scale, const int32_t* given,
@@ -253,7 +283,8 @@ int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_
                     size_t ws_bytes, void* stream) {
   if ((!type16(t) && t != LAROSA_F32) || !logits || !aligned(logits, t == LAROSA_F32 ? 4 : 2) || ld < n_vocab) return LAROSA_EINVAL;
   if (int rc = check_logprobs(n_rows, n_vocab, scale, given, n_given, logp, entropy, n_top, top_id, top_logp)) return rc;
-  if (!ws || !aligned(ws, 256) || ws_bytes < larosa_logprobs_workspace_bytes(n_rows, n_vocab, n_top, t)) return LAROSA_EWORKSPACE;
+  const LogprobsPlan plan = plan_logprobs(n_rows, n_vocab, n_top, t);
+  if (!ws || !aligned(ws, 256) || ws_bytes < kCounterBytes + logprobs_space(plan, n_rows)) return LAROSA_EWORKSPACE;
   LogprobsArgs a{};
   a.logits = logits;
   a.ld = ld;
@@ -262,13 +293,12 @@ int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_
   a.given = given; a.n_given = n_given; a.logp = logp;
   a.entropy = entropy;
   a.n_top = n_top; a.top_id = top_id; a.top_logp = top_logp;
-  return run_logprobs(a, n_rows, t, plan_logprobs(n_rows, n_vocab, n_top, t), static_cast<unsigned*>(ws),
-                      static_cast<char*>(ws) + kCounterBytes, stream_of(stream));
+  return run_logprobs(a, n_rows, t, plan, static_cast<unsigned*>(ws), static_cast<char*>(ws) + kCounterBytes, stream_of(stream));
 }
 
 size_t larosa_score_w8_workspace_bytes(int n_rows, int d_in, int n_vocab, int n_top) {
   if (check_product(n_rows, d_in, n_vocab) || n_top < 0 || n_top > kTopMax || n_top > n_vocab) return 0;
-  return score_space(n_rows, d_in, n_vocab, n_top).end;
+  return score_space(n_rows, d_in, n_vocab, n_top, true).end;
 }
 
 int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, int ld_x, const void* rms, float rms_eps, int n_rows,
@@ -288,7 +318,7 @@ int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, in
   for (int row = 0; row < n_rows; row += sp.at_once) {
     const int n = n_rows - row < sp.at_once ? n_rows - row : sp.at_once;
     const Product8Args a = product_args(w_codes, w_scales, codes, scales, w + sp.logits, sp.ld, n, d_in, n_vocab, kOutF32, ws, sp.partial);
-    if (int rc = run_product(a, static_cast<const uint16_t*>(x) + static_cast<long>(row) * ld_x, ld_x, rms, rms_eps, t, codes, scales, s)) return rc;
+    if (int rc = run_product(a, plan_product8(n, d_in, n_vocab), static_cast<const uint16_t*>(x) + static_cast<long>(row) * ld_x, ld_x, rms, rms_eps, t, codes, scales, s)) return rc;
     LogprobsArgs b{};
     b.logits = w + sp.logits;
     b.ld = sp.ld;

@@ -216,6 +216,36 @@ def test_two_streams_and_replays(api):
             assert torch.equal(jobs[0][k], jobs[1][k])
 
 
+class Guarded:
+    """A workspace of just the bytes that a query asks for, with a pattern behind them."""
+
+    def __init__(self, api, need):
+        self.nbytes = need
+        self.buf = torch.full((need + 256 + 65536,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 256
+        assert api.lib().larosa_workspace_init(self.ptr, need, torch.cuda.current_stream().cuda_stream) == 0
+
+    def whole(self):
+        behind = self.buf[self.ptr - self.buf.data_ptr() + self.nbytes:]
+        return bool((behind == 0xA5).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_one_workspace_for_every_batch(api, dtype):
+    """Sized for the most rows, used for fewer, which go in more slices."""
+    V, top = 50257, 20
+    z, given = draw(600, V, 5, dtype)
+    ws = Guarded(api, api.lib().larosa_logprobs_workspace_bytes(600, V, top, api.F32 if dtype == "f32" else api.F16))
+    for n in (600, 1, 7, 127, 128, 200, 511):
+        ids, tops = torch.empty(n, top, dtype=torch.int32, device="cuda"), torch.empty(n, top, device="cuda")
+        logp, entropy = torch.empty(n, 3, device="cuda"), torch.empty(n, device="cuda")
+        api.logprobs(z[:n], given[:n].int().cuda(), logp, ws, entropy=entropy, top_id=ids, top_logp=tops)
+        want = run(api, z[:n], given[:n], top)
+        for got, w in zip((logp, entropy, ids, tops), want):
+            assert np.array_equal(got.double().cpu().numpy(), w)
+        assert ws.whole()
+
+
 # ---- from hidden rows to log probabilities ---------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -280,6 +310,30 @@ def test_score_without_alternatives(api, tile, n, d, V):
                 assert torch.equal(logp.isnan(), kept[0][:, :few].isnan())
     finally:
         api.set_tuning(11, 0)
+
+
+@pytest.mark.parametrize("top", [0, 20])
+@pytest.mark.parametrize("d,V,rows", [(128, 32000, (1041, 1024, 17, 1, 100)), (4104, 1003, (700, 40, 257, 3))])
+def test_scores_stay_within_their_workspace(api, d, V, rows, top):
+    """Parts of the rows, the last one divided by itself (1041 rows: 1024 and 17, which go in slices), and smaller batches in the workspace of
+    the largest: nothing behind it is written, and every batch has the bits that it has in a workspace of its own."""
+    g = torch.Generator().manual_seed(V)
+    head = api.quantize_w8((torch.randn(d, V + (-V % 8), generator=g) * 0.2).half().cuda(), "f16")
+    head = head[0][:V], head[1]
+    x = torch.randn(rows[0], d, generator=g).half().cuda()
+    given = torch.randint(V, (rows[0], 2), generator=g).int().cuda()
+    ws = Guarded(api, api.lib().larosa_score_w8_workspace_bytes(rows[0], d, V, top))
+    for n in rows:
+        out = []
+        for work in (ws, Guarded(api, api.lib().larosa_score_w8_workspace_bytes(n, d, V, top))):
+            kw = dict(entropy=torch.full((n,), 7.0, device="cuda"))
+            if top:
+                kw.update(top_id=torch.empty(n, top, dtype=torch.int32, device="cuda"), top_logp=torch.empty(n, top, device="cuda"))
+            logp = torch.full((n, 2), 7.0, device="cuda")
+            api.score_w8(*head, x[:n], given[:n], logp, "f16", work, **kw)
+            assert work.whole()
+            out.append(dict(kw, logp=logp))
+        assert all(torch.equal(out[0][k], out[1][k]) for k in out[0])
 
 
 def test_score_is_its_parts_behind_a_norm(api):

@@ -265,6 +265,29 @@ def test_the_largest_values_of_the_type(api, n):
         assert np.all(np.abs(exact(got) - want) <= sums * most + STEP["bf16"] * (np.abs(want) + sums * most))
 
 
+def test_one_workspace_for_every_batch(api):
+    """Sized for the most rows, used for fewer, whose sums go in parts; nothing behind it is written."""
+    d_in, d_out, most = 8200, 520, 1100
+    g = torch.Generator().manual_seed(1)
+    x, W = torch.randn(most, d_in, generator=g).half().cuda(), torch.randn(d_in, d_out, generator=g).half().cuda()
+    wc, wsc = api.quantize_w8(W, "f16")
+    for name in ("dense_w8", "product8"):
+        need = getattr(api.lib(), f"larosa_{name}_workspace_bytes")(most, d_in, d_out)
+        ws = api.Workspace(need)
+        ws.buf = torch.full((need + 65536,), 0xA5, dtype=torch.uint8, device="cuda")
+        ws.ptr = ws.buf.data_ptr() + (-ws.buf.data_ptr()) % 256
+        behind = ws.buf[ws.ptr - ws.buf.data_ptr() + need:]
+        assert api.lib().larosa_workspace_init(ws.ptr, need, torch.cuda.current_stream().cuda_stream) == 0
+        for n in (1100, 1, 16, 17, 65, 200, 300, 700):
+            y, want = (torch.full((n, d_out), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+            api.dense_w8(wc, wsc, x[:n], want, "f16", api.dense_w8_workspace(n, d_in, d_out))
+            if name == "dense_w8":
+                api.dense_w8(wc, wsc, x[:n], y, "f16", ws)
+            else:
+                api.product8(wc, wsc, *api.quantize_rows8(x[:n], "f16"), d_in, y, "f16", ws)
+            assert torch.equal(y, want) and bool((behind == 0xA5).all())
+
+
 def test_dense_behind_a_norm_is_its_parts(api):
     for n in (2, 300):
         x, rms = torch.randn(n, 520).half().cuda(), (1 + 0.1 * torch.randn(520)).half().cuda()

@@ -116,6 +116,19 @@ def test_a_score_needs_room_for_its_last_part_too(lib):
         assert whole >= (1 << 20) + rows * (4096 + 32)
 
 
+def test_a_workspace_serves_smaller_numbers_of_rows(lib):
+    """Fewer rows go in more slices and parts; the query covers them, so one workspace for the largest batch does."""
+    for name, sizes, rows in (("logprobs", (128256, 20, 1), (1, 7, 64, 127, 128, 200, 511, 512, 600, 2048, 300000)),
+                              ("logprobs", (50257, 0, 2), (1, 2, 3, 5, 77, 127, 128, 129, 513)),
+                              ("product8", (11008, 4096), (1, 16, 17, 40, 100, 200, 333, 700, 1024, 4096, 32768, 1 << 17)),
+                              ("dense_w8", (8192, 264), (1, 17, 64, 65, 300, 2000, 40000)),
+                              ("score_w8", (8192, 32000, 20), (1, 5, 17, 100, 600, 1024, 1041, 2048, 5000))):
+        query = getattr(lib, f"larosa_{name}_workspace_bytes")
+        answers = [query(n, *sizes) for n in rows]
+        assert answers == sorted(answers), (name, sizes, answers)
+        assert answers[0] >= 1 << 20
+
+
 def test_binding_refuses_what_would_be_misread():
     from paper_2507_01299_amd import api
     codes, scales = torch.empty(256, 128, dtype=torch.float8_e4m3fn), torch.empty(2, 4, dtype=torch.uint8)
