@@ -116,6 +116,21 @@ def test_a_score_needs_room_for_its_last_part_too(lib):
         assert whole >= (1 << 20) + rows * (4096 + 32)
 
 
+@pytest.mark.parametrize("whole,tail,d,V,top,parts,slices", [
+    (1024, 17, 128, 32000, 20, False, True),         # of the logits of 17 rows each goes in slices, of 1024 none
+    (4096, 17, 8192, 8000, 0, True, False)])         # of the products of 17 rows the sums go in parts, of 4096 none
+def test_room_for_the_last_part_of_a_score(lib, whole, tail, d, V, top, parts, slices):
+    """Worked out by hand: counters, the whole part's rows and logits, and what only the last part asks for.  A workspace that lacks the latter is
+    refused."""
+    partial = lib.larosa_product8_workspace_bytes(tail, d, V) - (1 << 20)
+    probs = lib.larosa_logprobs_workspace_bytes(tail, V, top, 2) - (1 << 20)
+    assert (partial > 0, probs > 0) == (parts, slices)
+    need = (1 << 20) + whole * d + whole * -(-d // 512) * 4 + partial + whole * V * 4 + probs
+    assert lib.larosa_score_w8_workspace_bytes(whole + tail, d, V, top) >= need
+    sizes = dict(ld_x=d, n_rows=whole + tail, d_in=d, n_vocab=V, n_top=top)
+    assert call(lib.larosa_score_w8, SCORE, bytes=need - 1, **sizes) == EWORKSPACE
+
+
 def test_a_workspace_serves_smaller_numbers_of_rows(lib):
     """Fewer rows go in more slices and parts; the query covers them, so one workspace for the largest batch does."""
     for name, sizes, rows in (("logprobs", (128256, 20, 1), (1, 7, 64, 127, 128, 200, 511, 512, 600, 2048, 300000)),
