@@ -464,7 +464,7 @@ int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, in
  * that the gate|up launch builds (1, default) or selects for itself (0),
  * key 10 = workgroup tile of the offline contractions: 0 = chosen by size (default), 1 = 128 x 128, 2 = 256 x 256,
  * key 11 = workgroup tile (output channels x rows) of the products over 8-bit weights from 17 rows on: 0 = chosen by size (default),
- * 1 = 256 x 256, 2 = 256 x 192, 3 = 128 x 256, 4 = 128 x 128, 5 = 128 x 64.
+ * 1 = 256 x 256, 2 = 256 x 192, 3 = 128 x 256, 4 = 128 x 128, 5 = 128 x 64 (more than 2^23 of the tile asked for: LAROSA_EUNSUPPORTED).
  * Returns LAROSA_EINVAL for an unknown key or a value out of range. */
 int larosa_set_tuning(int key, int value);
 

@@ -733,6 +733,13 @@ float time8(const TileKind8& k, long jobs, int parts, int blocks_per, int d_in, 
   return (products > memory ? products : memory) + 2.5f * size * each + (parts > 1 ? 2.5f + 2.f * size * parts : 0.f);
 }
 
+// Tiles of 128 x 128 decide: there are no more of the larger ones, and those of 128 x 64 are left out where they are too many, unless the
+// tuning asks for them.
+bool plans_product8(int n_rows, int d_out) {
+  const long rows = tuning().product8_tiles == 5 && n_rows > kFewRows ? 64 : 128;
+  return ((n_rows + rows - 1) / rows) * ((d_out + 127L) / 128) <= kTilesMax8;
+}
+
 Product8Plan plan_product8(int n_rows, int d_in, int d_out) {
   Product8Plan p{};
   const int blocks = (d_in + 127) / 128;

@@ -55,6 +55,7 @@ struct Product8Plan {
 };
 Product8Plan plan_product8(int n_rows, int d_in, int d_out);      // from 17 rows on the same for 64 k + 1 .. 64 k + 64 rows
 constexpr int kRowsOfParts8 = 32768;   // with more rows no sum goes in parts: their tiles, of any kind, fill more than half of the chip
+bool plans_product8(int n_rows, int d_out);    // whether there is a plan: not more than kTilesMax8 tiles
 inline bool takes_rows16(const Product8Plan& p, int n_rows, int d_in) {
   return p.kind == 0 && n_rows * ((d_in + 127) / 128) * p.strips <= kShortRows / 128;
 }

@@ -54,7 +54,7 @@ int check_product(int n_rows, int d_in, int d_out) {
   if (n_rows < 1 || d_out < 1) return LAROSA_EINVAL;
   if (int rc = check_width(d_in)) return rc;
   if (n_rows > kRowsMax8 || d_out > kOutMax8) return LAROSA_EUNSUPPORTED;
-  return ((n_rows + 127L) / 128) * ((d_out + 127L) / 128) > kTilesMax8 ? LAROSA_EUNSUPPORTED : LAROSA_OK;
+  return plans_product8(n_rows, d_out) ? LAROSA_OK : LAROSA_EUNSUPPORTED;
 }
 
 // Workspace: arrival counters, then the pieces in this order, each from a multiple of 256 bytes on.

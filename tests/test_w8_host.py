@@ -191,6 +191,24 @@ def test_scales_whose_exponent_would_overflow_are_refused(lib):
     assert call(lib.larosa_logprobs, LOGPROBS, scale=2.0 ** 126, work=None) == EWORKSPACE
 
 
+def test_a_tile_that_would_be_too_many_is_refused(lib):
+    """2^23 tiles of 128 x 128 are 2^24 of 128 x 64: with that tile asked for there is no plan, neither for the query nor for the call."""
+    sizes = dict(n_rows=1 << 17, d_in=256, d_out=1 << 20, ld_y=1 << 20)
+    try:
+        for tile in (0, 1, 2, 3, 4):
+            assert lib.larosa_set_tuning(11, tile) == 0
+            assert lib.larosa_product8_workspace_bytes(1 << 17, 256, 1 << 20) > 0
+        assert lib.larosa_set_tuning(11, 5) == 0
+        assert lib.larosa_product8_workspace_bytes(1 << 17, 256, 1 << 20) == 0
+        assert lib.larosa_dense_w8_workspace_bytes(1 << 17, 256, 1 << 20) == 0
+        assert call(lib.larosa_product8, PRODUCT, **sizes) == EUNSUPPORTED
+        assert call(lib.larosa_dense_w8, DENSE, **sizes) == EUNSUPPORTED
+        assert lib.larosa_product8_workspace_bytes(1 << 16, 256, 1 << 20) > 0
+        assert lib.larosa_product8_workspace_bytes(16, 256, 1 << 20) > 0
+    finally:
+        lib.larosa_set_tuning(11, 0)
+
+
 def strided(shape, stride, dtype=torch.float16):
     """A matrix that takes no memory."""
     return torch.empty_strided(shape, stride, dtype=dtype, device="meta")
