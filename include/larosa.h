@@ -434,7 +434,7 @@ int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, in
  * A logit of -infinity has probability 0; a row of nothing else gets logp -infinity and entropy 0.  A row that holds a NaN or +infinity gets
  * NaN everywhere and top_id -1.  A logit counts as -infinity where its difference to the row's largest leaves fp32.  Sums and statistics
  * are fp32.  n_given >= 0, 0 <= n_top <= min(64, n_vocab); outputs that are not asked for (n_given or n_top 0) may be NULL.
- * Workspace: larosa_logprobs_workspace_bytes, initialised by larosa_workspace_init; at most 2^24 rows of at most 2^28 logits. */
+ * Workspace: larosa_logprobs_workspace_bytes (the same for every type), initialised by larosa_workspace_init; at most 2^24 rows of at most 2^28 logits. */
 size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, larosa_dtype t);
 int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_dtype t, float scale, const int32_t* given,
                     int n_given, float* logp, float* entropy, int n_top, int32_t* top_id, float* top_logp, void* ws,

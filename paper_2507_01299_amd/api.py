@@ -787,7 +787,7 @@ def _outputs8(n: int, given, logp, entropy, top_id, top_logp):
 
 
 def logprobs_workspace(n_rows: int, n_vocab: int, n_top: int = 0, dtype="bf16", device="cuda:0") -> Workspace:
-    """For logits of any type: dtype is only asked for because 32-bit logits take more room."""
+    """For n_rows rows or fewer; logits of every type take the same room."""
     code = F32 if dtype in (F32, "f32", torch.float32) else dtype_code(dtype)
     return _sized(lib().larosa_logprobs_workspace_bytes(n_rows, n_vocab, n_top, code), "larosa_logprobs_workspace_bytes", device)
 

@@ -575,7 +575,7 @@ hipError_t launch_type(const LogprobsArgs& a, hipStream_t s) {
 
 }  // namespace
 
-LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type) {
+LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top) {
   LogprobsPlan p{};
   const long places = static_cast<long>(n_vocab) + 7;                   // a row may start inside a group
   constexpr long kMost = kHoldersMax / 16 * 2048;                       // a slice's holders lie in LDS

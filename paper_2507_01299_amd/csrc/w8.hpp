@@ -85,7 +85,7 @@ struct LogprobsArgs {
   unsigned* counters;         // [n_rows] words, zero on entry and on exit
 };
 struct LogprobsPlan { int slices, slice_len; size_t sums_bytes, best_bytes; };
-LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top, int type);
+LogprobsPlan plan_logprobs(int n_rows, int n_vocab, int n_top);
 hipError_t launch_logprobs(const LogprobsArgs& a, int type, hipStream_t s);
 
 }  // namespace larosa

@@ -109,10 +109,10 @@ size_t logprobs_space(const LogprobsPlan& p, int n_rows) {
   return round_up(p.sums_bytes * n, 256) + round_up(p.best_bytes * n, 256);
 }
 
-size_t logprobs_space_up_to(int n_rows, int n_vocab, int n_top, int type) {
-  size_t most = logprobs_space(plan_logprobs(n_rows, n_vocab, n_top, type), n_rows);
+size_t logprobs_space_up_to(int n_rows, int n_vocab, int n_top) {
+  size_t most = logprobs_space(plan_logprobs(n_rows, n_vocab, n_top), n_rows);
   for (int n = 1; n < n_rows && n <= kWorkgroupsOfFew; ++n) {
-    const size_t here = logprobs_space(plan_logprobs(n, n_vocab, n_top, type), n);
+    const size_t here = logprobs_space(plan_logprobs(n, n_vocab, n_top), n);
     if (here > most) most = here;
   }
   return most;
@@ -163,13 +163,13 @@ ScoreSpace score_space(int n_rows, int d_in, int n_vocab, int n_top, bool up_to 
   size_t partial, probs;
   if (up_to) {
     partial = partial_up_to(s.at_once, d_in, n_vocab);
-    probs = logprobs_space_up_to(s.at_once, n_vocab, n_top, kLogitsF32);
+    probs = logprobs_space_up_to(s.at_once, n_vocab, n_top);
   } else {
     partial = plan_product8(s.at_once, d_in, n_vocab).partial_floats;
-    probs = logprobs_space(plan_logprobs(s.at_once, n_vocab, n_top, kLogitsF32), s.at_once);
+    probs = logprobs_space(plan_logprobs(s.at_once, n_vocab, n_top), s.at_once);
     if (tail) {                                  // the last part may be divided otherwise
       const size_t p = plan_product8(tail, d_in, n_vocab).partial_floats;
-      const size_t q = logprobs_space(plan_logprobs(tail, n_vocab, n_top, kLogitsF32), tail);
+      const size_t q = logprobs_space(plan_logprobs(tail, n_vocab, n_top), tail);
       if (p > partial) partial = p;
       if (q > probs) probs = q;
     }
@@ -275,7 +275,7 @@ size_t larosa_logprobs_workspace_bytes(int n_rows, int n_vocab, int n_top, laros
   if (!type16(t) && t != LAROSA_F32) return 0;
   if (check_logprobs(n_rows, n_vocab, 1.f, nullptr, 0, nullptr, nullptr, 0, nullptr, nullptr)) return 0;
   if (n_top < 0 || n_top > kTopMax || n_top > n_vocab) return 0;
-  return kCounterBytes + logprobs_space_up_to(n_rows, n_vocab, n_top, t);
+  return kCounterBytes + logprobs_space_up_to(n_rows, n_vocab, n_top);
 }
 
 int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_dtype t, float scale, const int32_t* given,
@@ -283,7 +283,7 @@ int larosa_logprobs(const void* logits, int ld, int n_rows, int n_vocab, larosa_
                     size_t ws_bytes, void* stream) {
   if ((!type16(t) && t != LAROSA_F32) || !logits || !aligned(logits, t == LAROSA_F32 ? 4 : 2) || ld < n_vocab) return LAROSA_EINVAL;
   if (int rc = check_logprobs(n_rows, n_vocab, scale, given, n_given, logp, entropy, n_top, top_id, top_logp)) return rc;
-  const LogprobsPlan plan = plan_logprobs(n_rows, n_vocab, n_top, t);
+  const LogprobsPlan plan = plan_logprobs(n_rows, n_vocab, n_top);
   if (!ws || !aligned(ws, 256) || ws_bytes < kCounterBytes + logprobs_space(plan, n_rows)) return LAROSA_EWORKSPACE;
   LogprobsArgs a{};
   a.logits = logits;
@@ -333,7 +333,7 @@ int larosa_score_w8(const void* w_codes, const void* w_scales, const void* x, in
     b.n_top = n_top;
     if (n_top) b.top_id = top_id + static_cast<size_t>(row) * n_top;
     if (n_top && top_logp) b.top_logp = top_logp + static_cast<size_t>(row) * n_top;
-    if (int rc = run_logprobs(b, n, kLogitsF32, plan_logprobs(n, n_vocab, n_top, kLogitsF32), static_cast<unsigned*>(ws),
+    if (int rc = run_logprobs(b, n, kLogitsF32, plan_logprobs(n, n_vocab, n_top), static_cast<unsigned*>(ws),
                               w + sp.logprobs, s))
       return rc;
   }

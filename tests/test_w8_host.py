@@ -209,6 +209,11 @@ def test_a_tile_that_would_be_too_many_is_refused(lib):
         lib.larosa_set_tuning(11, 0)
 
 
+def test_log_probabilities_take_the_same_room_for_every_type(lib):
+    for n, V, top in ((1, 32000, 5), (77, 50257, 8), (300, 128256, 0), (5, 300000, 64)):
+        assert len({lib.larosa_logprobs_workspace_bytes(n, V, top, t) for t in (0, 1, 2)}) == 1
+
+
 def strided(shape, stride, dtype=torch.float16):
     """A matrix that takes no memory."""
     return torch.empty_strided(shape, stride, dtype=dtype, device="meta")
