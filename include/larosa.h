@@ -404,7 +404,8 @@ int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, i
  * Scale bytes that a caller brings lie in 63 .. 247, as these do.
  * d_in is at most 2^20, d_out and ld_y below 2^21, n_rows at most 2^24; codes are 16-byte aligned, scales 4-byte. */
 
-/* W [d_in, d_out] (16-bit, type t, the layout of every weight of this library; d_out a multiple of 8) -> codes, scales. */
+/* W [d_in, d_out] (16-bit, type t, the layout of every weight of this library; d_out a multiple of 8) -> codes, scales.  An output head of any
+ * other number of tokens: fill W up with columns of zeros, which change no scale, and use the first n_vocab rows of the codes with all scales. */
 int larosa_quantize_w8(const void* W, int d_in, int d_out, larosa_dtype t, void* codes, void* scales, void* stream);
 
 /* x [n_rows, d] (16-bit, type t, rows ld_x apart, a multiple of 8) -> codes, scales.  rms_eps >= 0: behind a norm,

@@ -700,7 +700,8 @@ def _norm8(rms, d: int, code: int, rms_eps: float = 0.0):
 
 def quantize_w8(W, dtype):
     """e4m3 codes (float8_e4m3fn [d_out, d_in up to 16]) and scale bytes (uint8 [d_out / 128 up, d_in / 128 up, up to 4]) of
-    W [d_in, d_out]."""
+    W [d_in, d_out], d_out a multiple of 8.  An output head of n_vocab tokens, any number: of W filled up with columns of zeros,
+    (codes[:n_vocab], scales)."""
     code = dtype_code(dtype)
     _, stream = _device_stream(W)
     _matrix16(W, code)

@@ -312,6 +312,36 @@ def test_score_without_alternatives(api, tile, n, d, V):
         api.set_tuning(11, 0)
 
 
+def head_of(api, W, dtype):
+    """W [d, V], any V, as a head: columns of zeros up to the next multiple of 8, codes cut again."""
+    V = W.shape[1]
+    codes, scales = api.quantize_w8(torch.nn.functional.pad(W, (0, -V % 8)).to(TYPE[dtype]).cuda(), dtype)
+    return codes[:V], scales
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,d,V", [(3, 136, 1001), (20, 264, 4099), (2, 128, 32001), (5, 64, 50257)])
+def test_head_of_any_vocabulary(api, dtype, n, d, V):
+    """A head that this library made, of a vocabulary that is no multiple of 8: the codes of the weight itself, and log probabilities over its tokens
+    alone.  Sums of integers up to 2, so that logits are exact."""
+    g = torch.Generator().manual_seed(V)
+    x, W = torch.randint(-2, 3, (n, d), generator=g).float(), torch.randint(-2, 3, (d, V), generator=g).float()
+    head = head_of(api, W, dtype)
+    codes, scales = Q.quantize_weight(W.double().numpy())
+    assert np.array_equal(head[0].view(torch.uint8).cpu().numpy(), codes) and np.array_equal(head[1].cpu().numpy(), scales)
+    given = torch.randint(V, (n, 3), generator=g)
+    given[0] = torch.tensor([V - 1, V, -1])
+    logp, entropy = torch.empty(n, 3, device="cuda"), torch.empty(n, device="cuda")
+    ids, tops = torch.empty(n, 9, dtype=torch.int32, device="cuda"), torch.empty(n, 9, device="cuda")
+    api.score_w8(*head, x.to(TYPE[dtype]).cuda(), given.int().cuda(), logp, dtype, api.score_w8_workspace(n, d, V, 9), entropy=entropy, top_id=ids,
+                 top_logp=tops, scale=0.125)
+    want = Q.logprobs((x @ W).double().numpy(), given.numpy(), 9, 0.125)
+    near(logp.double().cpu().numpy(), want[0])
+    near(entropy.double().cpu().numpy(), want[1], rel=SUM)
+    assert np.array_equal(ids.cpu().numpy(), want[2])
+    near(tops.double().cpu().numpy(), want[3])
+
+
 @pytest.mark.parametrize("top", [0, 20])
 @pytest.mark.parametrize("d,V,rows", [(128, 32000, (1041, 1024, 17, 1, 100)), (4104, 1003, (700, 40, 257, 3))])
 def test_scores_stay_within_their_workspace(api, d, V, rows, top):
