@@ -188,6 +188,44 @@ def test_rows_by_the_launch(api):
     assert torch.equal(ids.long(), z.float().sort(dim=-1, descending=True, stable=True).indices[:, :2])
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_alike_logits_of_many_rows(api, dtype, top):
+    """Rows enough that none is cut, with more groups of 128 logits at the border than a wave has lanes: all alike, two values, a few above many."""
+    n, V = 130, 20011
+    z = torch.zeros(n, V)
+    z[1::3] = torch.randint(0, 2, (len(z[1::3]), V), generator=torch.Generator().manual_seed(top)).float()
+    z[2::3, ::999] = 1.0
+    z[2::3, 5] = -float("inf")
+    given = torch.arange(2 * n).view(n, 2)
+    check(api, z.to(TYPE[dtype]).cuda(), given, top)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("n,V,top", [(520, 140003, 64), (520, 270001, 9), (3, 300007, 64), (2, 1 << 20, 5)])
+def test_vocabularies_beyond_a_slice(api, dtype, n, V, top):
+    """Rows that are not cut though long (more groups than are read at once), and rows that have to be: more than 262137 tokens.  Few values, so that
+    equal ones lie everywhere.  Against 64 bits on the GPU.  A lane adds at most V / (256 slices) exponentials, in runs of 32: within SUM."""
+    print(f"logprobs {dtype} {n}x{V} top {top}", flush=True)
+    g = torch.Generator("cuda").manual_seed(V)
+    z = (torch.randint(-40, 9, (n, V), generator=g, device="cuda") / 4).to(TYPE[dtype])
+    z[0] = 1.0
+    given = torch.randint(V, (n, 2), generator=g, device="cuda").int()
+    logp, entropy = torch.empty(n, 2, device="cuda"), torch.empty(n, device="cuda")
+    ids, tops = torch.empty(n, top, dtype=torch.int32, device="cuda"), torch.empty(n, top, device="cuda")
+    ws = Guarded(api, api.lib().larosa_logprobs_workspace_bytes(n, V, top, api.F32))
+    api.logprobs(z, given, logp, ws, entropy=entropy, top_id=ids, top_logp=tops)
+    assert ws.whole()
+    for r in range(0, n, 130):
+        p = z[r:r + 130].double().log_softmax(-1)
+        best = z[r:r + 130].float().sort(dim=-1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(ids[r:r + 130].long(), best)
+        for got, want in ((logp, p.gather(1, given[r:r + 130].long())), (tops, p.gather(1, best))):
+            assert bool(((got[r:r + 130].double() - want).abs() <= SUM + REL * want.abs()).all())
+        want = -(p.exp() * p).sum(-1)
+        assert bool(((entropy[r:r + 130].double() - want).abs() <= SUM + SUM * want).all())
+
+
 def test_two_streams_and_replays(api):
     z, given = draw(6, 60000, 12, "f16")
     given = given.int().cuda()
@@ -336,6 +374,36 @@ def test_head_of_any_vocabulary(api, dtype, n, d, V):
     api.score_w8(*head, x.to(TYPE[dtype]).cuda(), given.int().cuda(), logp, dtype, api.score_w8_workspace(n, d, V, 9), entropy=entropy, top_id=ids,
                  top_logp=tops, scale=0.125)
     want = Q.logprobs((x @ W).double().numpy(), given.numpy(), 9, 0.125)
+    near(logp.double().cpu().numpy(), want[0])
+    near(entropy.double().cpu().numpy(), want[1], rel=SUM)
+    assert np.array_equal(ids.cpu().numpy(), want[2])
+    near(tops.double().cpu().numpy(), want[3])
+
+
+@pytest.mark.parametrize("tile", range(6))
+@pytest.mark.parametrize("n,d,V", [(17, 128, 1), (33, 4104, 129), (40, 8200, 1003), (150, 136, 5003), (300, 520, 2011), (600, 2056, 777)])
+def test_score_of_exact_logits(api, tile, n, d, V):
+    """32-bit logits of every tile, with the sums in one piece and in parts, against the oracle: integers up to 2, differently scaled in each row and each
+    block of the head, so that every logit is exact and only the softmax's own roundings are left."""
+    print(f"exact score {tile} {n}x{d}x{V}", flush=True)
+    g = torch.Generator().manual_seed(n + d + V)
+    x = torch.randint(-2, 3, (n, d), generator=g).float() * 2.0 ** torch.randint(-2, 2, (n, 1), generator=g)
+    W = torch.randint(-2, 3, (d, V), generator=g).float()
+    for o in range(0, V, 128):
+        W[:, o:o + 128] *= 2.0 ** ((o // 128) % 3 - 1)
+    top, scale = min(V, 7), 2.0 ** -6
+    given = torch.randint(V, (n, 2), generator=g)
+    given[-1] = torch.tensor([V - 1, -1])
+    logp, entropy = torch.full((n, 2), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+    ids, tops = torch.empty(n, top, dtype=torch.int32, device="cuda"), torch.empty(n, top, device="cuda")
+    head = head_of(api, W, "f16")
+    try:
+        api.set_tuning(11, tile)
+        api.score_w8(*head, x.half().cuda(), given.int().cuda(), logp, "f16", api.score_w8_workspace(n, d, V, top), entropy=entropy, top_id=ids,
+                     top_logp=tops, scale=scale)
+    finally:
+        api.set_tuning(11, 0)
+    want = Q.logprobs(x.double().numpy() @ W.double().numpy(), given.numpy(), top, scale)
     near(logp.double().cpu().numpy(), want[0])
     near(entropy.double().cpu().numpy(), want[1], rel=SUM)
     assert np.array_equal(ids.cpu().numpy(), want[2])

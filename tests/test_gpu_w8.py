@@ -115,6 +115,28 @@ def test_weight_bit_for_bit(api, dtype, d_in, d_out):
     same_held(api.quantize_w8(W.cuda(), dtype), Q.quantize_weight(exact(W)))
 
 
+@pytest.mark.parametrize("eps", [-1.0, 1e-5])
+def test_rows_by_the_launch(api, eps):
+    """More rows than one launch takes: each has the codes of its like among the first ones."""
+    n, d = (1 << 19) + 37, 24
+    base = (torch.randn(1000, d, generator=torch.Generator().manual_seed(1)) * 3).half().cuda()
+    x = base[torch.arange(n, device="cuda") % 1000]
+    codes, scales = api.quantize_rows8(x, "f16", rms_eps=eps)
+    first = api.quantize_rows8(base, "f16", rms_eps=eps)
+    at = torch.arange(n, device="cuda") % 1000
+    assert torch.equal(codes.view(torch.uint8), first[0].view(torch.uint8)[at]) and torch.equal(scales, first[1][at])
+
+
+def test_weight_of_many_blocks(api):
+    """More blocks than one side of a grid: the codes and scales of its panels, each made by itself."""
+    d_in, d_out = 12296, 12296
+    W = torch.randn(d_in, d_out, device="cuda", generator=torch.Generator("cuda").manual_seed(2)).bfloat16()
+    codes, scales = api.quantize_w8(W, "bf16")
+    for o in range(0, d_out, 1536):
+        c, s = api.quantize_w8(W[:, o:o + 1536].contiguous(), "bf16")
+        assert torch.equal(codes[o:o + 1536].view(torch.uint8), c.view(torch.uint8)) and torch.equal(scales[o // 128:o // 128 + 12], s)
+
+
 # ---- products ------------------------------------------------------------------------------------------------
 
 # The 8-bit instruction aligns the products of eight neighbours to the largest sum of two exponents and cuts them, towards zero, 13 bits below it (256 * 256
@@ -263,6 +285,17 @@ def test_the_largest_values_of_the_type(api, n):
     sums = (d_in + 8) * 2.0 ** -24 + (0 if n <= 16 else CUT)
     for got in (y, z):
         assert np.all(np.abs(exact(got) - want) <= sums * most + STEP["bf16"] * (np.abs(want) + sums * most))
+
+
+def test_product_of_more_rows_than_a_launch_quantises(api):
+    """Small integers, so that every result is exact."""
+    n, d_in, d_out = (1 << 19) + 37, 24, 16
+    g = torch.Generator("cuda").manual_seed(3)
+    x = torch.randint(-2, 3, (n, d_in), generator=g, device="cuda").half()
+    W = torch.randint(-2, 3, (d_in, d_out), generator=g, device="cuda").half()
+    y = torch.full((n + 1, d_out), 7.0, dtype=torch.float16, device="cuda")
+    api.dense_w8(*api.quantize_w8(W, "f16"), x, y[:n], "f16", api.dense_w8_workspace(n, d_in, d_out))
+    assert torch.equal(y[:n].float(), x.float() @ W.float()) and bool((y[n] == 7).all())
 
 
 def test_one_workspace_for_every_batch(api):
