@@ -662,32 +662,40 @@ def _device_stream(*tensors):
     return device, torch._C._cuda_getCurrentRawStream(device)
 
 
-def _distance(t) -> int:
-    """Distance between the rows of a matrix.  The library's sizes are 32-bit: a larger one would arrive as its low 32 bits, another matrix."""
-    rows, width = t.shape
-    ld, one = t.stride()
-    if one != 1 and width != 1:
-        raise ValueError("the values of a row lie next to one another")
-    if (ld >> 31 and rows > 1) or rows >> 31 or width >> 31:
-        raise ValueError("sizes and distances between rows are below 2^31")
-    return ld
+# The library's sizes and distances are 32-bit: a larger one would arrive as its low 32 bits, another matrix.
+_SIZE = 1 << 31
 
 
 def _matrix16(t, code: int) -> int:
     """Distance between the rows of a matrix of the type `code`."""
-    if t.dtype is not torch_dtype(code) or t.dim() != 2:
+    stride = t.stride()
+    if t.dtype is not torch_dtype(code) or len(stride) != 2:
         raise ValueError("rows are a matrix of the call's type")
-    ld = _distance(t)
-    # one row: whatever its tensor says of the distance to the next, one that the library takes
-    return ld if t.shape[0] > 1 else max(min(ld // 8 * 8, 1 << 20), -(-t.shape[1] // 8) * 8)
+    ld, one = stride
+    rows, width = t.shape
+    if one != 1 and width != 1:
+        raise ValueError("the values of a row lie next to one another")
+    if rows == 1:        # whatever its tensor says of the distance to a next one, one that the library takes
+        ld = max(min(ld // 8 * 8, 1 << 20), -(-width // 8) * 8)
+    if ld >= _SIZE or rows >= _SIZE:
+        raise ValueError("sizes and distances between rows are below 2^31")
+    return ld
 
 
 def _logits(t):
     """Distance between the rows of logits, and their type."""
-    if t.dtype not in _LOGITS or t.dim() != 2:
+    stride = t.stride()
+    if t.dtype not in _LOGITS or len(stride) != 2:
         raise ValueError("logits are a matrix of float16, bfloat16 or float32")
-    ld = _distance(t)
-    return ld if t.shape[0] > 1 else t.shape[1], _LOGITS[t.dtype]
+    ld, one = stride
+    rows, width = t.shape
+    if one != 1 and width != 1:
+        raise ValueError("the logits of a row lie next to one another")
+    if rows == 1:
+        ld = width
+    if ld >= _SIZE or rows >= _SIZE or width >= _SIZE:
+        raise ValueError("sizes and distances between rows are below 2^31")
+    return ld, _LOGITS[t.dtype]
 
 
 def _norm8(rms, d: int, code: int, rms_eps: float = 0.0):
