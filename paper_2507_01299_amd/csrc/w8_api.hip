@@ -142,13 +142,12 @@ int run_logprobs(LogprobsArgs a, int n_rows, int type, const LogprobsPlan& p, un
   return LAROSA_OK;
 }
 
-// Rows whose logits lie in the workspace at once: 128 MiB, which stay in the memory-side cache, and at least 16 rows (a multiple of
-// 256 where there are as many).
+// Rows whose logits lie in the workspace at once: 128 MiB, which stay in the memory-side cache; a multiple of 256 where there are as many, and 16
+// of the largest vocabulary (kOutMax8).
 int score_rows(int n_rows, int n_vocab) {
   const long ld = static_cast<long>(round_up(n_vocab, 16));
   long n = (128L << 20) / (ld * 4);
   if (n >= 256) n = n / 256 * 256;
-  if (n < 16) n = 16;
   return n < n_rows ? static_cast<int>(n) : n_rows;
 }
 

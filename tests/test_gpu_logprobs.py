@@ -410,6 +410,28 @@ def test_score_of_exact_logits(api, tile, n, d, V):
     near(tops.double().cpu().numpy(), want[3])
 
 
+def test_score_over_the_largest_vocabulary(api):
+    """2^21 - 16 tokens: 16 rows at once, then the other four.  Small integers, so that logits are exact."""
+    n, d, V, top = 20, 16, (1 << 21) - 16, 9
+    g = torch.Generator("cuda").manual_seed(4)
+    x = torch.randint(-2, 3, (n, d), generator=g, device="cuda").bfloat16()
+    W = torch.randint(-2, 3, (d, V), generator=g, device="cuda").bfloat16()
+    given = torch.randint(V, (n, 2), generator=g, device="cuda").int()
+    logp, entropy = torch.empty(n, 2, device="cuda"), torch.empty(n, device="cuda")
+    ids, tops = torch.empty(n, top, dtype=torch.int32, device="cuda"), torch.empty(n, top, device="cuda")
+    ws = Guarded(api, api.lib().larosa_score_w8_workspace_bytes(n, d, V, top))
+    api.score_w8(*api.quantize_w8(W, "bf16"), x, given, logp, "bf16", ws, entropy=entropy, top_id=ids, top_logp=tops, scale=0.5)
+    assert ws.whole()
+    z = x.float() @ W.float()
+    p = (0.5 * z.double()).log_softmax(-1)
+    best = z.sort(dim=-1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(ids.long(), best)
+    for got, want in ((logp, p.gather(1, given.long())), (tops, p.gather(1, best))):
+        assert bool(((got.double() - want).abs() <= SUM + REL * want.abs()).all())
+    want = -(p.exp() * p).sum(-1)
+    assert bool(((entropy.double() - want).abs() <= SUM + SUM * want).all())
+
+
 @pytest.mark.parametrize("top", [0, 20])
 @pytest.mark.parametrize("d,V,rows", [(128, 32000, (1041, 1024, 17, 1, 100)), (4104, 1003, (700, 40, 257, 3))])
 def test_scores_stay_within_their_workspace(api, d, V, rows, top):
