@@ -409,20 +409,22 @@ int larosa_layer_forward_kv4(const larosa_layer* L, const larosa_kv4_cache* C, i
 int larosa_quantize_w8(const void* W, int d_in, int d_out, larosa_dtype t, void* codes, void* scales, void* stream);
 
 /* x [n_rows, d] (16-bit, type t, rows ld_x apart, a multiple of 8) -> codes, scales.  rms_eps >= 0: behind a norm,
- * x / sqrt(mean(x^2) + rms_eps) * rms (rms [d] or NULL = 1), in fp32 and not rounded before the codes; rms_eps < 0: as they are. */
+ * x / sqrt(mean(x^2) + rms_eps) * rms (rms [d] or NULL = 1), in fp32 and not rounded before the codes; rms_eps < 0: as they are (rms is
+ * not read). */
 int larosa_quantize_rows8(const void* x, int ld_x, int n_rows, int d, const void* rms, float rms_eps, larosa_dtype t, void* codes,
                           void* scales, void* stream);
 
 /* y[m, o] = sum_i x[m, i] W[o, i] over the values that rows and weight stand for; y [n_rows, d_out] (type t, rows ld_y apart, a multiple of
  * 8), rounded once.  d_out is a multiple of 8.  Sums are fp32; from 17 rows on the products of eight neighbours are added by the 8-bit matrix
  * instruction, which cuts them 13 bits below the largest one's exponent (about 2^-16 of the result's norm, with a few strong channels 2^-14.5).
+ * So a row's last bits depend on how many rows are with it; the same call gives the same bits every time.
  * Workspace: larosa_product8_workspace_bytes, initialised by larosa_workspace_init; one for n_rows rows serves any smaller number of
  * them too, here and in the calls below (the query looks at all of them: once for a workspace, not at every call).  Up to 2^23 tiles of 128 rows x 128 channels. */
 size_t larosa_product8_workspace_bytes(int n_rows, int d_in, int d_out);
 int larosa_product8(const void* w_codes, const void* w_scales, const void* x_codes, const void* x_scales, void* y, int ld_y,
                     int n_rows, int d_in, int d_out, larosa_dtype t, void* ws, size_t ws_bytes, void* stream);
 
-/* larosa_quantize_rows8 into the workspace and larosa_product8: x, y and rms in type t. */
+/* larosa_quantize_rows8 into the workspace and larosa_product8: x, y and rms in type t; y must not overlap x. */
 size_t larosa_dense_w8_workspace_bytes(int n_rows, int d_in, int d_out);
 int larosa_dense_w8(const void* w_codes, const void* w_scales, const void* x, int ld_x, const void* rms, float rms_eps, void* y,
                     int ld_y, int n_rows, int d_in, int d_out, larosa_dtype t, void* ws, size_t ws_bytes, void* stream);
